@@ -329,6 +329,118 @@ fqt_status fqt_gemm_s4s4_bf6(const int8_t* A, const int8_t* B, int64_t M, int64_
                              int64_t ldb, int64_t* C, void* ws, size_t ws_bytes, fqt_stream_t s);
 size_t fqt_gemm_s4s4_bf6_workspace(int64_t M, int64_t N, int64_t K);
 
+/* ---------------------------------------------------------------------------
+ * Floating-point operators around the layers of a feed-forward training step:
+ * layer norm, layers in 8-bit floating point, gradient norm and clipping.
+ *
+ * Matrices are row-major with unit column stride and any row pitch (ld*, in
+ * elements; an input's rows may overlap, pitch 0 repeats one row), at any
+ * element-aligned address.  `type` is the type of the activations and their
+ * gradients; parameters and their gradients are float32.  Arithmetic is
+ * float32 or wider and every output is rounded once.  Outputs must not
+ * overlap inputs.  NaN and infinities propagate as the formulas have them, so
+ * these entry points record no data status.
+ * ------------------------------------------------------------------------- */
+typedef enum { FQT_F32 = 0, FQT_BF16 = 1, FQT_F16 = 2 } fqt_dtype;
+
+/* Layer norm over the columns of X [rows, cols]:
+ *   mean_i = 1/cols sum_j x_ij, rstd_i = 1 / sqrt(1/cols sum_j (x_ij - mean_i)^2 + eps)
+ *   Y_ij = (x_ij - mean_i) rstd_i gamma_j + beta_j
+ * gamma, beta [cols] may be NULL (ones, zeros); mean, rstd [rows] are what the
+ * backward reads and may be NULL.  eps >= 0.                                 */
+fqt_status fqt_layernorm_forward(const void* X, fqt_dtype type, int64_t rows, int64_t cols, int64_t ldx,
+                                 const float* gamma, const float* beta, float eps, void* Y, int64_t ldy, float* mean,
+                                 float* rstd, fqt_stream_t s);
+
+/* Its gradient: with xh = (x - mean) rstd and c = g gamma,
+ *   grad_X = rstd (c - mean_j(c) - xh mean_j(c xh))
+ *   grad_gamma_j = sum_i g_ij xh_ij,  grad_beta_j = sum_i g_ij
+ * grad_gamma and grad_beta may be NULL (both: no workspace needed).  The sums
+ * over rows run in a fixed order.                                           */
+fqt_status fqt_layernorm_backward(const void* G, int64_t ldg, const void* X, int64_t ldx, fqt_dtype type, int64_t rows,
+                                  int64_t cols, const float* mean, const float* rstd, const float* gamma, void* grad_X,
+                                  int64_t ldgx, float* grad_gamma, float* grad_beta, void* ws, size_t ws_bytes,
+                                  fqt_stream_t s);
+size_t fqt_layernorm_backward_workspace(int64_t rows, int64_t cols);
+
+/* One operand of an 8-bit floating point product, [rows, K]: codes with 4
+ * exponent and 3 mantissa bits (largest value 448, no infinity, NaN 0x7F) and
+ * one scale for each row and block of 128 along K.
+ *   q    [rows, fqt_fp8_pitch(K)], 16-byte aligned; whole blocks, zero codes
+ *        past K.
+ *   exp  fqt_fp8_exp_bytes(rows, K) bytes, 4-byte aligned: E + 127 of row r
+ *        and block b at [b / 4][r][b % 4] (127 past the last block); 255 is NaN.
+ *   k_major  0: the codes lie row by row.  1: column by column, [pitch(K)][rows]
+ *        (an operand that was made by transposing a view); products accept it
+ *        and lay it out in their workspace first.
+ * An element stands for q 2^E.                                             */
+typedef struct {
+  uint8_t* q;
+  uint8_t* exp;
+  int32_t k_major;
+} fqt_fp8;
+size_t fqt_fp8_pitch(int64_t K);
+size_t fqt_fp8_exp_bytes(int64_t rows, int64_t K);
+
+/* Block quantizer.  E is the least integer >= -127 with max|block| <= 448 2^E
+ * (0 for an empty block), and the code is that of x 2^-E: rounded to nearest,
+ * ties to even, or (stochastic != 0) unbiased with one 24-bit uniform u of the
+ * element as in the other quantizers: up iff u < frac 2^24, frac the part of a
+ * step of the format that x 2^-E lies above the value below it.
+ *   by_row  operand of x [rows, K = cols], blocks of 1 x 128, random stream 1
+ *   by_col  operand of x^T [cols, K = rows], blocks of 128 x 1, stream 0
+ * (either may be NULL), both from one read of x.  tile != 0: one scale for
+ * each 128 x 128 tile of x, the same in both operands (weights).  A block that
+ * holds a NaN or an infinity becomes NaN as a whole (exp 255).             */
+fqt_status fqt_fp8_quantize(const void* x, fqt_dtype type, int64_t rows, int64_t cols, int64_t ldx, int tile,
+                            int stochastic, uint64_t seed, const fqt_fp8* by_row, const fqt_fp8* by_col,
+                            fqt_stream_t s);
+
+/* C [M, N] = A [M, K] B [N, K]^T of two operands, accumulated in float32 on
+ * the scaled matrix cores; optionally C = max(C, 0) (relu != 0) and C = 0
+ * where mask [M, N] (of C's type) is not positive.                         */
+fqt_status fqt_fp8_gemm(const fqt_fp8* A, const fqt_fp8* B, int64_t M, int64_t N, int64_t K, fqt_dtype type, int relu,
+                        const void* mask, int64_t ldmask, void* C, int64_t ldc, void* ws, size_t ws_bytes,
+                        fqt_stream_t s);
+size_t fqt_fp8_gemm_workspace(int64_t M, int64_t N, int64_t K);
+
+/* Linear layer forward in 8-bit floating point: Y [N, d_out] = Q(X) W8^T with
+ * X [N, d_in] quantized here to nearest in blocks of 1 x 128 and W8 [d_out,
+ * K = d_in] the weights' codes (fqt_fp8_quantize with tile, by_row);
+ * optionally Y = max(Y, 0).  X8t (may be NULL) receives the operand of X^T
+ * [d_in, K = N], which the backward's grad_W reads.                        */
+fqt_status fqt_fp8_linear_forward(const void* X, fqt_dtype type, int64_t N, int64_t d_in, int64_t ldx,
+                                  const fqt_fp8* W8, int64_t d_out, int relu, void* Y, int64_t ldy,
+                                  const fqt_fp8* X8t, void* ws, size_t ws_bytes, fqt_stream_t s);
+size_t fqt_fp8_linear_forward_workspace(int64_t N, int64_t d_in, int64_t d_out);
+
+/* Its backward, with two independent quantizations of G [N, d_out] as in App.
+ * E's bifurcation, stochastic by default (Sec. 2.2: an unbiased gradient):
+ *   grad_W [d_out, d_in] = Q_b1(G)^T X8t^T   (G^T in blocks along N, stream 0)
+ *   grad_X [N, d_in]     = Q_b2(G) W8t^T     (G in blocks along d_out, stream 1)
+ * X8t [d_in, K = N] from the forward, W8t [d_in, K = d_out] the weights'
+ * by_col operand.  grad_W or grad_X may be NULL (not formed; its operand may
+ * then be NULL too).  relu_input [N, d_in] (may be NULL): X was the output of
+ * a ReLU, and grad_X is zero where it is not positive.                     */
+fqt_status fqt_fp8_linear_backward(const void* G, fqt_dtype type, int64_t N, int64_t d_out, int64_t ldg,
+                                   const fqt_fp8* X8t, const fqt_fp8* W8t, int64_t d_in, int stochastic, uint64_t seed,
+                                   const void* relu_input, int64_t ldr, float* grad_W, void* grad_X, int64_t ldgx,
+                                   void* ws, size_t ws_bytes, fqt_stream_t s);
+size_t fqt_fp8_linear_backward_workspace(int64_t N, int64_t d_in, int64_t d_out);
+
+/* Global gradient norm and clipping over `count` contiguous tensors:
+ *   n = sqrt(sum over all tensors of g^2),  out = g max_norm / n if n > max_norm, else g
+ * grads, outs, sizes (elements, 0 allowed) and types (fqt_dtype) are HOST
+ * arrays, read before the call returns; outs NULL or outs[i] = grads[i]: in
+ * place, and nothing is written where nothing is clipped.  norm (device, may
+ * be NULL) receives n.  Squares are summed in float64 in a fixed order.  A
+ * norm that is not finite scales nothing.  max_norm > 0 (infinity: only the
+ * norm).  Calls whose table of sizes passes 2^31 chunks of 16384 elements in 96
+ * tensors return FQT_EUNSUPPORTED.                                         */
+fqt_status fqt_grad_norm_clip(const void* const* grads, void* const* outs, const int64_t* sizes, const int32_t* types,
+                              int64_t count, double max_norm, float* norm, void* ws, size_t ws_bytes, fqt_stream_t s);
+size_t fqt_grad_norm_clip_workspace(int64_t count);
+
 /* Waits for `s`, then reports the data status recorded in `ws` by the last
  * call that used it: FQT_OK or FQT_ENONFINITE (FQT_EDEVICE if the wait or
  * copy fails).                                                              */

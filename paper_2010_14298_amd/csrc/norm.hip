@@ -1,0 +1,382 @@
+// Layer norm over the last axis, forward and backward.
+//
+//   mean = 1/D sum x,  var = 1/D sum (x - mean)^2,  r = 1 / sqrt(var + eps)
+//   xh = (x - mean) r,  y = xh gamma + beta
+//   c = g gamma,  gx = r (c - mean(c) - xh mean(c xh))
+//   ggamma = sum over rows of g xh,  gbeta = sum over rows of g
+//
+// A team of threads (a wave, or a block) holds its whole row in registers:
+// one read of each input, one write of each output.  Statistics, sums and
+// parameter gradients are float32; the outputs are rounded once.
+#include "train_kernels.h"
+
+namespace fqt {
+
+// Elements of a row that each thread of a team of TPR threads holds: NV
+// vectors of VEC, vector v at column (v TPR + t) VEC.
+template <int TPR_, int VEC_, int NV_>
+struct Team {
+  static constexpr int TPR = TPR_, VEC = VEC_, NV = NV_;
+  static constexpr int THREADS = TPR < 256 ? 256 : TPR;
+  static constexpr int PER_BLOCK = THREADS / TPR;  // rows at a time
+  static constexpr int WAVES = TPR / 64;
+  static constexpr int64_t COLS = (int64_t)TPR * VEC * NV;
+};
+
+// Sums of N values over the team, in every thread.
+template <class C, int N>
+__device__ __forceinline__ void team_sum(float (&v)[N], float (*sh)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+  if constexpr (C::WAVES > 1) {
+    const int wave = threadIdx.x >> 6;
+    __syncthreads();  // the last sums have been read
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) sh[wave][i] = v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      v[i] = 0.0f;
+#pragma unroll
+      for (int w = 0; w < C::WAVES; ++w) v[i] += sh[w][i];
+    }
+  }
+}
+
+template <class T, class C>
+__global__ __launch_bounds__(C::THREADS) void norm_forward_kernel(NormParams p) {
+  __shared__ float sh[C::WAVES][1];
+  const int t = threadIdx.x % C::TPR;
+  const int64_t row = (int64_t)blockIdx.x * C::PER_BLOCK + threadIdx.x / C::TPR;
+  if (C::PER_BLOCK > 1 && row >= p.rows) return;  // whole waves, and no barrier below
+  const T* x = static_cast<const T*>(p.x) + row * p.ldx;
+  float v[C::NV][C::VEC];
+  float s[1] = {0.0f};
+#pragma unroll
+  for (int k = 0; k < C::NV; ++k) {
+    const int64_t col = (int64_t)(k * C::TPR + t) * C::VEC;
+    load_part<T, C::VEC>(x + col, p.cols - col, v[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < C::NV; ++k)
+#pragma unroll
+    for (int i = 0; i < C::VEC; ++i) s[0] += v[k][i];
+  team_sum<C, 1>(s, sh);
+  const float inv = 1.0f / (float)p.cols;
+  const float mean = s[0] * inv;
+  s[0] = 0.0f;
+#pragma unroll
+  for (int k = 0; k < C::NV; ++k) {
+    const int64_t col = (int64_t)(k * C::TPR + t) * C::VEC;
+#pragma unroll
+    for (int i = 0; i < C::VEC; ++i) {
+      const float d = col + i < p.cols ? v[k][i] - mean : 0.0f;
+      s[0] = fmaf(d, d, s[0]);
+    }
+  }
+  team_sum<C, 1>(s, sh);
+  const float rstd = 1.0f / sqrtf(fmaf(s[0], inv, p.eps));
+  if (t == 0) {
+    if (p.mean) p.mean[row] = mean;
+    if (p.rstd) p.rstd[row] = rstd;
+  }
+  T* y = static_cast<T*>(p.y) + row * p.ldy;
+#pragma unroll
+  for (int k = 0; k < C::NV; ++k) {
+    const int64_t col = (int64_t)(k * C::TPR + t) * C::VEC;
+    float ga[C::VEC], be[C::VEC], o[C::VEC];
+#pragma unroll
+    for (int i = 0; i < C::VEC; ++i) {
+      ga[i] = 1.0f;
+      be[i] = 0.0f;
+    }
+    if (p.gamma) load_part<float, C::VEC>(p.gamma + col, p.cols - col, ga);
+    if (p.beta) load_part<float, C::VEC>(p.beta + col, p.cols - col, be);
+#pragma unroll
+    for (int i = 0; i < C::VEC; ++i) o[i] = fmaf((v[k][i] - mean) * rstd, ga[i], be[i]);
+    store_part<T, C::VEC>(y + col, p.cols - col, o);
+  }
+}
+
+// Rows longer than a team's registers: the row is read three times (sum,
+// squares, output), the later ones from the caches.
+template <class T, class C>
+__global__ __launch_bounds__(C::THREADS) void norm_forward_long_kernel(NormParams p) {
+  __shared__ float sh[C::WAVES][1];
+  const int64_t row = blockIdx.x;
+  const T* x = static_cast<const T*>(p.x) + row * p.ldx;
+  const int64_t step = (int64_t)C::TPR * C::VEC, first = (int64_t)threadIdx.x * C::VEC;
+  float v[C::VEC];
+  float s[1] = {0.0f};
+  for (int64_t col = first; col < p.cols; col += step) {
+    load_part<T, C::VEC>(x + col, p.cols - col, v);
+#pragma unroll
+    for (int i = 0; i < C::VEC; ++i) s[0] += v[i];
+  }
+  team_sum<C, 1>(s, sh);
+  const float inv = 1.0f / (float)p.cols;
+  const float mean = s[0] * inv;
+  s[0] = 0.0f;
+  for (int64_t col = first; col < p.cols; col += step) {
+    load_part<T, C::VEC>(x + col, p.cols - col, v);
+#pragma unroll
+    for (int i = 0; i < C::VEC; ++i) {
+      const float d = col + i < p.cols ? v[i] - mean : 0.0f;
+      s[0] = fmaf(d, d, s[0]);
+    }
+  }
+  team_sum<C, 1>(s, sh);
+  const float rstd = 1.0f / sqrtf(fmaf(s[0], inv, p.eps));
+  if (threadIdx.x == 0) {
+    if (p.mean) p.mean[row] = mean;
+    if (p.rstd) p.rstd[row] = rstd;
+  }
+  T* y = static_cast<T*>(p.y) + row * p.ldy;
+  for (int64_t col = first; col < p.cols; col += step) {
+    load_part<T, C::VEC>(x + col, p.cols - col, v);
+#pragma unroll
+    for (int i = 0; i < C::VEC; ++i)
+      if (col + i < p.cols)
+        v[i] = fmaf((v[i] - mean) * rstd, p.gamma ? p.gamma[col + i] : 1.0f, p.beta ? p.beta[col + i] : 0.0f);
+    store_part<T, C::VEC>(y + col, p.cols - col, v);
+  }
+}
+
+// Backward: each team takes every (teams)-th row and keeps its columns' sums
+// of g xh and g in registers; at the end the block adds its teams' sums in
+// order and writes one partial row of each.
+template <class T, class C>
+__global__ __launch_bounds__(C::THREADS) void norm_backward_kernel(NormParams p) {
+  __shared__ float sh[C::WAVES][2];
+  __shared__ float col_sum[C::PER_BLOCK > 1 ? 2 * C::COLS : 1];
+  const int t = threadIdx.x % C::TPR, team = threadIdx.x / C::TPR;
+  const float inv = 1.0f / (float)p.cols;
+  float ga[C::NV][C::VEC], sg[C::NV][C::VEC], sb[C::NV][C::VEC];
+#pragma unroll
+  for (int k = 0; k < C::NV; ++k) {
+    const int64_t col = (int64_t)(k * C::TPR + t) * C::VEC;
+#pragma unroll
+    for (int i = 0; i < C::VEC; ++i) {
+      ga[k][i] = 1.0f;
+      sg[k][i] = sb[k][i] = 0.0f;
+    }
+    if (p.gamma) load_part<float, C::VEC>(p.gamma + col, p.cols - col, ga[k]);
+  }
+  // PER_BLOCK == 1: every thread of the block has the same trip count, so the
+  // barriers inside team_sum meet
+  for (int64_t row = (int64_t)blockIdx.x * C::PER_BLOCK + team; row < p.rows; row += (int64_t)gridDim.x * C::PER_BLOCK) {
+    const T* x = static_cast<const T*>(p.x) + row * p.ldx;
+    const T* g = static_cast<const T*>(p.g) + row * p.ldg;
+    const float mean = p.mean[row], rstd = p.rstd[row];
+    float xh[C::NV][C::VEC], gv[C::NV][C::VEC];
+    float s[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < C::NV; ++k) {
+      const int64_t col = (int64_t)(k * C::TPR + t) * C::VEC;
+      load_part<T, C::VEC>(x + col, p.cols - col, xh[k]);
+      load_part<T, C::VEC>(g + col, p.cols - col, gv[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < C::NV; ++k)
+#pragma unroll
+      for (int i = 0; i < C::VEC; ++i) {
+        // columns past the end have g = 0, so whatever xh is there adds nothing
+        xh[k][i] = (xh[k][i] - mean) * rstd;
+        sg[k][i] = fmaf(gv[k][i], xh[k][i], sg[k][i]);
+        sb[k][i] += gv[k][i];
+        gv[k][i] *= ga[k][i];
+        s[0] += gv[k][i];
+        s[1] = fmaf(gv[k][i], xh[k][i], s[1]);
+      }
+    team_sum<C, 2>(s, sh);
+    const float a = s[0] * inv, b = s[1] * inv;
+    T* y = static_cast<T*>(p.y) + row * p.ldy;
+#pragma unroll
+    for (int k = 0; k < C::NV; ++k) {
+      const int64_t col = (int64_t)(k * C::TPR + t) * C::VEC;
+      float o[C::VEC];
+#pragma unroll
+      for (int i = 0; i < C::VEC; ++i) o[i] = rstd * ((gv[k][i] - a) - xh[k][i] * b);
+      store_part<T, C::VEC>(y + col, p.cols - col, o);
+    }
+  }
+  if (!p.grad_gamma && !p.grad_beta) return;
+  float* part = p.part + (int64_t)blockIdx.x * 2 * p.cols;
+  if constexpr (C::PER_BLOCK > 1) {
+    for (int w = 0; w < C::PER_BLOCK; ++w) {
+      if (team == w) {
+#pragma unroll
+        for (int k = 0; k < C::NV; ++k)
+#pragma unroll
+          for (int i = 0; i < C::VEC; ++i) {
+            const int col = (k * C::TPR + t) * C::VEC + i;
+            if (w > 0) {
+              sg[k][i] += col_sum[col];
+              sb[k][i] += col_sum[C::COLS + col];
+            }
+            if (w + 1 < C::PER_BLOCK) {
+              col_sum[col] = sg[k][i];
+              col_sum[C::COLS + col] = sb[k][i];
+            }
+          }
+      }
+      __syncthreads();
+    }
+    if (team != C::PER_BLOCK - 1) return;
+  }
+#pragma unroll
+  for (int k = 0; k < C::NV; ++k) {
+    const int64_t col = (int64_t)(k * C::TPR + t) * C::VEC;
+    store_part<float, C::VEC>(part + col, p.cols - col, sg[k]);
+    store_part<float, C::VEC>(part + p.cols + col, p.cols - col, sb[k]);
+  }
+}
+
+// Rows longer than a team's registers: inputs read twice, no parameter sums.
+template <class T, class C>
+__global__ __launch_bounds__(C::THREADS) void norm_backward_long_kernel(NormParams p) {
+  __shared__ float sh[C::WAVES][2];
+  const int64_t row = blockIdx.x;
+  const T* x = static_cast<const T*>(p.x) + row * p.ldx;
+  const T* g = static_cast<const T*>(p.g) + row * p.ldg;
+  T* y = static_cast<T*>(p.y) + row * p.ldy;
+  const float mean = p.mean[row], rstd = p.rstd[row], inv = 1.0f / (float)p.cols;
+  const int64_t step = (int64_t)C::TPR * C::VEC, first = (int64_t)threadIdx.x * C::VEC;
+  float xv[C::VEC], gv[C::VEC];
+  float s[2] = {0.0f, 0.0f};
+  for (int64_t col = first; col < p.cols; col += step) {
+    load_part<T, C::VEC>(x + col, p.cols - col, xv);
+    load_part<T, C::VEC>(g + col, p.cols - col, gv);
+#pragma unroll
+    for (int i = 0; i < C::VEC; ++i) {
+      const float c = gv[i] * (p.gamma && col + i < p.cols ? p.gamma[col + i] : 1.0f);
+      s[0] += c;
+      s[1] = fmaf(c, (xv[i] - mean) * rstd, s[1]);
+    }
+  }
+  team_sum<C, 2>(s, sh);
+  const float a = s[0] * inv, b = s[1] * inv;
+  for (int64_t col = first; col < p.cols; col += step) {
+    load_part<T, C::VEC>(x + col, p.cols - col, xv);
+    load_part<T, C::VEC>(g + col, p.cols - col, gv);
+#pragma unroll
+    for (int i = 0; i < C::VEC; ++i) {
+      const float c = gv[i] * (p.gamma && col + i < p.cols ? p.gamma[col + i] : 1.0f);
+      gv[i] = rstd * ((c - a) - (xv[i] - mean) * rstd * b);
+    }
+    store_part<T, C::VEC>(y + col, p.cols - col, gv);
+  }
+}
+
+// The parameter sums of long rows: a block takes 256 columns of a run of rows.
+constexpr int LONG_RUNS = 64;
+template <class T>
+__global__ __launch_bounds__(256) void norm_columns_kernel(NormParams p) {
+  const int64_t col = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (col >= p.cols) return;
+  float sg = 0.0f, sb = 0.0f;
+  for (int64_t row = blockIdx.y; row < p.rows; row += gridDim.y) {
+    const float g = (float)static_cast<const T*>(p.g)[row * p.ldg + col];
+    const float x = (float)static_cast<const T*>(p.x)[row * p.ldx + col];
+    sg = fmaf(g, (x - p.mean[row]) * p.rstd[row], sg);
+    sb += g;
+  }
+  p.part[(int64_t)blockIdx.y * 2 * p.cols + col] = sg;
+  p.part[((int64_t)blockIdx.y * 2 + 1) * p.cols + col] = sb;
+}
+
+// The partial rows added up: 64 columns a block, one wave a run of partials,
+// the waves' sums in order.
+constexpr int REDUCE_WAVES = 16;
+__global__ __launch_bounds__(64 * REDUCE_WAVES) void norm_reduce_kernel(const float* part, int64_t parts, int64_t cols,
+                                                                         float* grad_gamma, float* grad_beta) {
+  __shared__ float sh[REDUCE_WAVES][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t col = (int64_t)blockIdx.x * 64 + lane;  // of 2 * cols: gamma's, then beta's
+  float s = 0.0f;
+  if (col < 2 * cols) {
+#pragma unroll 4
+    for (int64_t i = wave; i < parts; i += REDUCE_WAVES) s += part[i * 2 * cols + col];
+  }
+  sh[wave][lane] = s;
+  __syncthreads();
+  if (wave == 0 && col < 2 * cols) {
+    for (int w = 1; w < REDUCE_WAVES; ++w) s += sh[w][lane];
+    if (col < cols) {
+      if (grad_gamma) grad_gamma[col] = s;
+    } else if (grad_beta) {
+      grad_beta[col - cols] = s;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// launches
+// ---------------------------------------------------------------------------
+// Teams by row length; 16 elements a thread.
+template <class T, class F>
+static hipError_t with_team(int64_t cols, F f) {
+  constexpr int V = 16 / (int)sizeof(T);  // elements of 16 bytes
+  constexpr int H = V / 2;
+  if (cols <= 64 * 4) return f(Team<64, H, 4 / H>{});
+  if (cols <= 64 * 8) return f(Team<64, V, 8 / V>{});
+  if (cols <= 64 * 16) return f(Team<64, V, 16 / V>{});
+  if (cols <= 256 * 8) return f(Team<256, V, 8 / V>{});
+  if (cols <= 256 * 16) return f(Team<256, V, 16 / V>{});
+  if (cols <= 512 * 16) return f(Team<512, V, 16 / V>{});
+  return f(Team<1024, V, 16 / V>{});
+}
+constexpr int64_t TEAM_COLS = 1024 * 16;
+
+hipError_t launch_norm_forward(fqt_dtype type, const NormParams& p, hipStream_t s) {
+  return with_type(type, [&](auto e) {
+    using T = decltype(e);
+    return with_team<T>(p.cols, [&](auto c) {
+      using C = decltype(c);
+      const int64_t blocks = (p.rows + C::PER_BLOCK - 1) / C::PER_BLOCK;
+      if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+      if (p.cols <= TEAM_COLS)
+        hipLaunchKernelGGL((norm_forward_kernel<T, C>), dim3((unsigned)blocks), dim3(C::THREADS), 0, s, p);
+      else if constexpr (C::TPR == 1024)
+        hipLaunchKernelGGL((norm_forward_long_kernel<T, C>), dim3((unsigned)blocks), dim3(C::THREADS), 0, s, p);
+      return hipGetLastError();
+    });
+  });
+}
+
+constexpr int64_t BACKWARD_BLOCKS = 1024;
+static int64_t backward_blocks(int64_t rows, int64_t cols) {
+  if (cols > TEAM_COLS) return rows < LONG_RUNS ? rows : LONG_RUNS;
+  const int64_t teams = cols <= 64 * 16 ? (rows + 3) / 4 : rows;
+  return teams < BACKWARD_BLOCKS ? teams : BACKWARD_BLOCKS;
+}
+int64_t norm_backward_partials(int64_t rows, int64_t cols) { return backward_blocks(rows, cols) * 2 * cols; }
+
+hipError_t launch_norm_backward(fqt_dtype type, const NormParams& p, hipStream_t s) {
+  const bool sums = p.grad_gamma || p.grad_beta;
+  const int64_t blocks = backward_blocks(p.rows, p.cols);
+  if (p.rows > 0x7FFFFFFF) return hipErrorInvalidValue;
+  const hipError_t e = with_type(type, [&](auto el) {
+    using T = decltype(el);
+    return with_team<T>(p.cols, [&](auto c) {
+      using C = decltype(c);
+      if (p.cols <= TEAM_COLS) {
+        hipLaunchKernelGGL((norm_backward_kernel<T, C>), dim3((unsigned)blocks), dim3(C::THREADS), 0, s, p);
+      } else if constexpr (C::TPR == 1024) {
+        hipLaunchKernelGGL((norm_backward_long_kernel<T, C>), dim3((unsigned)p.rows), dim3(C::THREADS), 0, s, p);
+        if (sums)
+          hipLaunchKernelGGL((norm_columns_kernel<T>), dim3((unsigned)((p.cols + 255) / 256), (unsigned)blocks),
+                             dim3(256), 0, s, p);
+      }
+      return hipGetLastError();
+    });
+  });
+  if (e != hipSuccess || !sums) return e;
+  hipLaunchKernelGGL(norm_reduce_kernel, dim3((unsigned)((2 * p.cols + 63) / 64)), dim3(64 * REDUCE_WAVES), 0, s,
+                     p.part, blocks, p.cols, p.grad_gamma, p.grad_beta);
+  return hipGetLastError();
+}
+
+}  // namespace fqt

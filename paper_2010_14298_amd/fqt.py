@@ -6,6 +6,7 @@ device pointers and the current HIP stream, allocates outputs and the
 workspace with torch, and raises on any non-OK status.  There is no CPU
 fallback: if the library is not built or cannot load, every call raises.
 """
+import array
 import ctypes
 import os
 
@@ -56,6 +57,10 @@ class ConvShape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int) for n in ("n", "c", "h", "w", "o", "kh", "kw", "stride", "pad", "ho", "wo")]
 
 
+class Fp8(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("exp", ctypes.c_void_p), ("k_major", ctypes.c_int32)]
+
+
 EXPORTS = [
     "fqt_quantize_ptq", "fqt_quantize_psq", "fqt_quantize_psq_noalloc", "fqt_quantize_bhq", "fqt_quantize_shift", "fqt_quantize_workspace",
     "fqt_quantize_seeds",
@@ -64,6 +69,11 @@ EXPORTS = [
     "fqt_linear_forward", "fqt_linear_forward_workspace",
     "fqt_conv_backward_im2col", "fqt_conv_backward_workspace",
     "fqt_gemm_s8s8_s64", "fqt_gemm_workspace", "fqt_gemm_s4s4_bf6", "fqt_gemm_s4s4_bf6_workspace",
+    "fqt_layernorm_forward", "fqt_layernorm_backward", "fqt_layernorm_backward_workspace",
+    "fqt_fp8_pitch", "fqt_fp8_exp_bytes", "fqt_fp8_quantize", "fqt_fp8_gemm", "fqt_fp8_gemm_workspace",
+    "fqt_fp8_linear_forward", "fqt_fp8_linear_forward_workspace",
+    "fqt_fp8_linear_backward", "fqt_fp8_linear_backward_workspace",
+    "fqt_grad_norm_clip", "fqt_grad_norm_clip_workspace",
     "fqt_probe_mfma_i8", "fqt_probe_copy",
     "fqt_workspace_status", "fqt_status_str", "fqt_version",
 ]
@@ -84,6 +94,8 @@ def load(path=LIB_PATH):
     qtp = ctypes.POINTER(QTensor)
     cfgp = ctypes.POINTER(BwdCfg)
     shp = ctypes.POINTER(ConvShape)
+    f8p = ctypes.POINTER(Fp8)
+    f32 = ctypes.c_float
     sig = {
         "fqt_quantize_ptq": ([vp, i64, i64, i32, i32, u64, u32, i32, qtp, vp, sz, vp], i32),
         "fqt_quantize_psq": ([vp, i64, i64, i32, u64, u32, qtp, vp, sz, vp], i32),
@@ -104,6 +116,21 @@ def load(path=LIB_PATH):
         "fqt_gemm_workspace": ([i64, i64, i64], sz),
         "fqt_gemm_s4s4_bf6": ([vp, vp, i64, i64, i64, i64, i64, vp, vp, sz, vp], i32),
         "fqt_gemm_s4s4_bf6_workspace": ([i64, i64, i64], sz),
+        "fqt_layernorm_forward": ([vp, i32, i64, i64, i64, vp, vp, f32, vp, i64, vp, vp, vp], i32),
+        "fqt_layernorm_backward": ([vp, i64, vp, i64, i32, i64, i64, vp, vp, vp, vp, i64, vp, vp, vp, sz, vp], i32),
+        "fqt_layernorm_backward_workspace": ([i64, i64], sz),
+        "fqt_fp8_pitch": ([i64], sz),
+        "fqt_fp8_exp_bytes": ([i64, i64], sz),
+        "fqt_fp8_quantize": ([vp, i32, i64, i64, i64, i32, i32, u64, f8p, f8p, vp], i32),
+        "fqt_fp8_gemm": ([f8p, f8p, i64, i64, i64, i32, i32, vp, i64, vp, i64, vp, sz, vp], i32),
+        "fqt_fp8_gemm_workspace": ([i64, i64, i64], sz),
+        "fqt_fp8_linear_forward": ([vp, i32, i64, i64, i64, f8p, i64, i32, vp, i64, f8p, vp, sz, vp], i32),
+        "fqt_fp8_linear_forward_workspace": ([i64, i64, i64], sz),
+        "fqt_fp8_linear_backward": ([vp, i32, i64, i64, i64, f8p, f8p, i64, i32, u64, vp, i64, vp, vp, i64, vp, sz,
+                                     vp], i32),
+        "fqt_fp8_linear_backward_workspace": ([i64, i64, i64], sz),
+        "fqt_grad_norm_clip": ([vp, vp, vp, vp, i64, ctypes.c_double, vp, vp, sz, vp], i32),
+        "fqt_grad_norm_clip_workspace": ([i64], sz),
         "fqt_probe_mfma_i8": ([i64, vp, ctypes.POINTER(ctypes.c_double), vp], i32),
         "fqt_probe_copy": ([vp, vp, sz, vp], i32),
         "fqt_workspace_status": ([vp, vp], i32),
@@ -419,6 +446,225 @@ def fqt_gemm_s4s4_bf6(A, B, ws=None, C=None):
                                   ws.numel(), _stream())
     _check("fqt_gemm_s4s4_bf6", rc)
     return C, ws
+
+
+# ----------------------------------------------------------------------------
+# floating-point operators around the layers
+# ----------------------------------------------------------------------------
+FQT_F32, FQT_BF16, FQT_F16 = 0, 1, 2
+TYPES = {torch.float32: FQT_F32, torch.bfloat16: FQT_BF16, torch.float16: FQT_F16}
+
+
+def _here(t, name):
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current CUDA device")
+    return t
+
+
+def _matrix(x, name, shape=None, dtype=None):
+    """(pointer, type, rows, cols, row pitch) of a 2-d activation tensor."""
+    if x.dim() != 2 or x.dtype not in TYPES or (dtype is not None and x.dtype != dtype):
+        raise ValueError(f"{name} must be a 2-d float32, bfloat16 or float16 tensor of the call's type")
+    if shape is not None and x.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(x.shape)}, not {tuple(shape)}")
+    rows, cols = x.shape
+    ld, step = x.stride()
+    if step != 1 and cols != 1:
+        raise ValueError(f"{name} must have unit column stride")
+    return _here(x, name).data_ptr(), TYPES[x.dtype], rows, cols, ld if rows > 1 else max(ld, cols)
+
+
+def _vector(x, name, n):
+    """Pointer of a contiguous float32 [n] tensor (None: NULL)."""
+    if x is None:
+        return None
+    if x.dtype != torch.float32 or x.shape != (n,) or not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous float32 tensor of {n} elements")
+    return _here(x, name).data_ptr()
+
+
+def fqt_layernorm_forward(X, gamma=None, beta=None, eps=1e-5, Y=None):
+    """Layer norm over the columns of X [rows, cols]; returns (Y, mean, rstd)."""
+    px, dt, rows, cols, ldx = _matrix(X, "X")
+    if Y is None:
+        Y = torch.empty((rows, cols), dtype=X.dtype, device=X.device)
+    py, _, _, _, ldy = _matrix(Y, "Y", X.shape, X.dtype)
+    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=X.device).unbind(0)
+    rc = load().fqt_layernorm_forward(px, dt, rows, cols, ldx, _vector(gamma, "gamma", cols),
+                                      _vector(beta, "beta", cols), eps, py, ldy, mean.data_ptr(), rstd.data_ptr(),
+                                      _stream())
+    _check("fqt_layernorm_forward", rc)
+    return Y, mean, rstd
+
+
+def fqt_layernorm_backward_workspace(rows, cols):
+    return load().fqt_layernorm_backward_workspace(rows, cols)
+
+
+def fqt_layernorm_backward(G, X, mean, rstd, gamma=None, grad_X=None, params=True, ws=None):
+    """Gradient of fqt_layernorm_forward; returns (grad_X, grad_gamma, grad_beta, ws).  params=False forms grad_X
+    only (the others are None)."""
+    pg, dt, rows, cols, ldg = _matrix(G, "G")
+    px, _, _, _, ldx = _matrix(X, "X", G.shape, G.dtype)
+    if grad_X is None:
+        grad_X = torch.empty((rows, cols), dtype=G.dtype, device=G.device)
+    py, _, _, _, ldgx = _matrix(grad_X, "grad_X", G.shape, G.dtype)
+    gg = gb = None
+    if params:
+        gg, gb = torch.empty((2, cols), dtype=torch.float32, device=G.device).unbind(0)
+        if ws is None:
+            ws = _workspace(fqt_layernorm_backward_workspace(rows, cols), G.device)
+    rc = load().fqt_layernorm_backward(pg, ldg, px, ldx, dt, rows, cols, _vector(mean, "mean", rows),
+                                       _vector(rstd, "rstd", rows), _vector(gamma, "gamma", cols), py, ldgx,
+                                       _vector(gg, "grad_gamma", cols), _vector(gb, "grad_beta", cols),
+                                       ws.data_ptr() if ws is not None else None, ws.numel() if ws is not None else 0,
+                                       _stream())
+    _check("fqt_layernorm_backward", rc)
+    return grad_X, gg, gb, ws
+
+
+def fp8_operand(rows, K, device):
+    """An empty operand of an 8-bit floating point product, [rows, K]: dict(q=codes [rows, K padded to whole
+    blocks of 128], exp=scale bytes [blocks / 4, rows, 4], K=K).  Products also take q whose transpose is
+    contiguous."""
+    blocks = (K + 127) // 128
+    return dict(q=torch.empty((rows, blocks * 128), dtype=torch.float8_e4m3fn, device=device),
+                exp=torch.empty(((blocks + 3) // 4, rows, 4), dtype=torch.uint8, device=device), K=K)
+
+
+def _fp8(a, name, rows=None, K=None):
+    """The C struct of an operand (None: NULL), checked against the rows and K that the call needs."""
+    if a is None:
+        return None
+    q, e, k = a["q"], a["exp"], a["K"]
+    blocks = (k + 127) // 128
+    if (q.dtype != torch.float8_e4m3fn or e.dtype != torch.uint8 or q.dim() != 2 or q.shape[1] != blocks * 128
+            or e.shape != ((blocks + 3) // 4, q.shape[0], 4) or not e.is_contiguous()):
+        raise ValueError(f"{name} is not an operand as fp8_operand lays it out")
+    if (rows is not None and q.shape[0] != rows) or (K is not None and k != K):
+        raise ValueError(f"{name} is [{q.shape[0]}, {k}], not [{rows}, {K}]")
+    k_major = not q.is_contiguous()
+    if k_major and not q.t().is_contiguous():
+        raise ValueError(f"{name}: codes must be contiguous by row or by column")
+    _here(e, name)
+    return Fp8(_here(q, name).data_ptr(), e.data_ptr(), int(k_major))
+
+
+def fqt_fp8_quantize(x, tile=False, by_row=True, by_col=False, stochastic=False, seed=0):
+    """Operands of x [rows, cols]: (x [rows, K = cols] or None, x^T [cols, K = rows] or None), from one read."""
+    px, dt, rows, cols, ldx = _matrix(x, "x")
+    a = fp8_operand(rows, cols, x.device) if by_row else None
+    b = fp8_operand(cols, rows, x.device) if by_col else None
+    rc = load().fqt_fp8_quantize(px, dt, rows, cols, ldx, int(bool(tile)), int(bool(stochastic)), seed,
+                                 _fp8(a, "by_row"), _fp8(b, "by_col"), _stream())
+    _check("fqt_fp8_quantize", rc)
+    return a, b
+
+
+def fqt_fp8_gemm_workspace(M, N, K):
+    return load().fqt_fp8_gemm_workspace(M, N, K)
+
+
+def fqt_fp8_gemm(A, B, dtype=torch.float32, relu=False, mask=None, C=None, ws=None):
+    """C [M, N] = A [M, K] B [N, K]^T of two operands; relu: max(C, 0); mask: zero where mask <= 0.
+    Returns (C, ws)."""
+    M, N, K = A["q"].shape[0], B["q"].shape[0], A["K"]
+    if C is None:
+        C = torch.empty((M, N), dtype=dtype, device=A["q"].device)
+    pc, dt, _, _, ldc = _matrix(C, "C", (M, N))
+    pm, _, _, _, ldm = _matrix(mask, "mask", (M, N), C.dtype) if mask is not None else (None,) * 4 + (0,)
+    if ws is None:
+        ws = _workspace(fqt_fp8_gemm_workspace(M, N, K), C.device)
+    rc = load().fqt_fp8_gemm(_fp8(A, "A"), _fp8(B, "B", N, K), M, N, K, dt, int(bool(relu)), pm, ldm, pc, ldc,
+                             ws.data_ptr(), ws.numel(), _stream())
+    _check("fqt_fp8_gemm", rc)
+    return C, ws
+
+
+def fqt_fp8_linear_forward_workspace(N, d_in, d_out):
+    return load().fqt_fp8_linear_forward_workspace(N, d_in, d_out)
+
+
+def fqt_fp8_linear_forward(X, W8, relu=False, save=True, Y=None, ws=None):
+    """Y = Q(X) W8^T (then max(., 0) when relu), W8 the weights' by_row operand (tile=True).  save: also the operand
+    of X^T that the backward reads.  Returns (Y, X8t or None, ws)."""
+    px, dt, N, d_in, ldx = _matrix(X, "X")
+    d_out = W8["q"].shape[0]
+    w8 = _fp8(W8, "W8", d_out, d_in)
+    if Y is None:
+        Y = torch.empty((N, d_out), dtype=X.dtype, device=X.device)
+    py, _, _, _, ldy = _matrix(Y, "Y", (N, d_out), X.dtype)
+    X8t = fp8_operand(d_in, N, X.device) if save else None
+    if ws is None:
+        ws = _workspace(fqt_fp8_linear_forward_workspace(N, d_in, d_out), X.device)
+    rc = load().fqt_fp8_linear_forward(px, dt, N, d_in, ldx, w8, d_out, int(bool(relu)), py, ldy, _fp8(X8t, "X8t"),
+                                       ws.data_ptr(), ws.numel(), _stream())
+    _check("fqt_fp8_linear_forward", rc)
+    return Y, X8t, ws
+
+
+def fqt_fp8_linear_backward_workspace(N, d_in, d_out):
+    return load().fqt_fp8_linear_backward_workspace(N, d_in, d_out)
+
+
+def fqt_fp8_linear_backward(G, X8t, W8t, seed=0, stochastic=True, relu_input=None, input_grad=True, grad_W=None,
+                            grad_X=None, ws=None):
+    """grad_W = Q_b1(G)^T X8t^T (float32) and grad_X = Q_b2(G) W8t^T (G's type; zero where relu_input <= 0).
+    input_grad=False forms grad_W only (grad_X is None; W8t may be None).  Returns (grad_W, grad_X, ws)."""
+    pg, dt, N, d_out, ldg = _matrix(G, "G")
+    d_in = X8t["q"].shape[0]
+    x8t = _fp8(X8t, "X8t", d_in, N)
+    w8t = _fp8(W8t, "W8t", d_in, d_out)
+    if grad_W is None:
+        grad_W = torch.empty((d_out, d_in), dtype=torch.float32, device=G.device)
+    if (grad_W.dtype != torch.float32 or grad_W.shape != (d_out, d_in) or not grad_W.is_contiguous()):
+        raise ValueError("grad_W must be a contiguous float32 tensor [d_out, d_in]")
+    px, ldgx = None, 0
+    if not input_grad:
+        grad_X = None
+    else:
+        if grad_X is None:
+            grad_X = torch.empty((N, d_in), dtype=G.dtype, device=G.device)
+        px, _, _, _, ldgx = _matrix(grad_X, "grad_X", (N, d_in), G.dtype)
+    pr, ldr = None, 0
+    if relu_input is not None:
+        pr, _, _, _, ldr = _matrix(relu_input, "relu_input", (N, d_in), G.dtype)
+    if ws is None:
+        ws = _workspace(fqt_fp8_linear_backward_workspace(N, d_in, d_out), G.device)
+    rc = load().fqt_fp8_linear_backward(pg, dt, N, d_out, ldg, x8t, w8t, d_in, int(bool(stochastic)), seed, pr, ldr,
+                                        _here(grad_W, "grad_W").data_ptr(), px, ldgx, ws.data_ptr(), ws.numel(),
+                                        _stream())
+    _check("fqt_fp8_linear_backward", rc)
+    return grad_W, grad_X, ws
+
+
+def fqt_grad_norm_clip_workspace(count):
+    return load().fqt_grad_norm_clip_workspace(count)
+
+
+def fqt_grad_norm_clip(grads, max_norm, outs=None, ws=None):
+    """Global norm of the tensors in grads; each is scaled by max_norm / norm where norm > max_norm, in place or
+    into outs.  Returns (norm, ws); norm is a float32 device scalar."""
+    count = len(grads)
+    dev = torch.cuda.current_device()
+    for t in grads if outs is None else [*grads, *outs]:
+        if t.get_device() != dev or t.dtype not in TYPES or not t.is_contiguous():
+            raise ValueError("gradients must be contiguous float32, bfloat16 or float16 tensors on the current device")
+    sizes = [t.numel() for t in grads]
+    types = [TYPES[t.dtype] for t in grads]
+    if outs is not None and ([t.numel() for t in outs] != sizes or [TYPES[t.dtype] for t in outs] != types):
+        raise ValueError("outs must match grads in number, size and type")
+    g = array.array("Q", [t.data_ptr() for t in grads])
+    o = array.array("Q", [t.data_ptr() for t in outs]) if outs is not None else None
+    n, ty = array.array("q", sizes), array.array("i", types)
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    if ws is None:
+        ws = _workspace(fqt_grad_norm_clip_workspace(count), norm.device)
+    rc = load().fqt_grad_norm_clip(g.buffer_info()[0], o.buffer_info()[0] if o is not None else None,
+                                   n.buffer_info()[0], ty.buffer_info()[0], count, max_norm, norm.data_ptr(),
+                                   ws.data_ptr(), ws.numel(), _stream())
+    _check("fqt_grad_norm_clip", rc)
+    return norm, ws
 
 
 def fqt_workspace_status(ws):

@@ -20,192 +20,402 @@
 namespace fqt {
 
 constexpr int TILE = FP8_BLOCK;
-constexpr int QT = 256;           // threads of a tile: 32 column quads x 8 row groups
+constexpr int QT = 256;                  // threads of a tile: 32 column quads x 8 row groups
 constexpr int GROUP = TILE / (QT / 32);  // rows of one thread: 16
 
-// E + 127 from the bits of the largest magnitude; 255 for NaN / Inf.
-__device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
-  if (top == 0u) return 127u;
-  if (top >= 0x7f800000u) return 255u;
-  const int b = (int)(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
-  return b < 0 ? 0u : (uint32_t)b;
-}
-// 2^-E.  (E + 127 = 255: the codes are replaced afterwards.)
-__device__ __forceinline__ float scale_down(uint32_t byte) {
-  return __uint_as_float((byte == 255u ? 127u : 254u - byte) << 23);
-}
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
-// Two nearest-even codes into the low or high half of w.
-template <bool HI>
-__device__ __forceinline__ uint32_t cvt2(float a, float b, uint32_t w) {
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, (int)w, HI);
+template <class To, class From>
+__device__ __forceinline__ To as(From v) {
+  return __builtin_bit_cast(To, v);
 }
+__device__ __forceinline__ uint32_t pk_max(uint32_t a, uint32_t b) {
+  return as<uint32_t>(__builtin_elementwise_max(as<u16x2>(a), as<u16x2>(b)));
+}
+struct PkMax {
+  __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return pk_max(a, b); }
+};
 
-// Stochastic code of y, |y| <= 448.  In units of the step 2^(max(E8, -6) - 3)
-// times 2^-24, t 2^24 is an integer for |y| >= 2^-6 (24-bit significands
-// with 20 bits below the step) and is rounded up to one below; adding
-// 2^24 - 1 - u carries into bit 24 exactly when u < frac(t) 2^24.
-__device__ __forceinline__ uint32_t stochastic_code(float y, uint32_t word) {
-  const uint32_t bits = __float_as_uint(y), mag = bits & 0x7fffffffu;
-  const bool small = mag < 0x3c800000u;  // 2^-6
-  const uint32_t tn = ((mag & 0x7fffffu) | 0x800000u) << 4;
-  const uint32_t ts = (uint32_t)ceilf(__uint_as_float(mag) * 8589934592.0f);  // 2^9 2^24
-  const uint32_t r = ((small ? ts : tn) + (~word & 0xffffffu)) >> 24;
-  const uint32_t base = small ? 0u : ((mag >> 23) - 121u) << 3;
-  return base + r + ((bits >> 24) & 0x80u);
+// Four neighbouring elements as they were loaded, their magnitudes as 16-bit
+// keys (two to a word) that sort like the magnitudes, NaN above infinity
+// above the rest, and their codes.  A key decides the block's scale, so a
+// float32 magnitude may be rounded up to 16 bits (sign, exponent, 7 bits): the
+// bound 1.75 2^p is a key itself.
+template <class T>
+struct Quad;
+
+template <>
+struct Quad<float> {
+  float v[4];
+  __device__ __forceinline__ void load(const float* p, int64_t n) { load_part<float, 4>(p, n, v); }
+  static __device__ __forceinline__ uint32_t key(uint32_t m) {
+    const uint32_t up = (m + 0xffffu) >> 16;
+    return m >= 0x7f800000u ? m >> 16 : (up < 0x7f7fu ? up : 0x7f7fu);
+  }
+  // running maxima: the row's in one value, the columns' in four
+  typedef uint32_t RowTop;
+  struct ColTop {
+    uint32_t m[4];
+  };
+  __device__ __forceinline__ void top(RowTop& r, ColTop& c) const {
+    r = 0u;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t m = __float_as_uint(v[j]) & 0x7fffffffu;
+      r = r > m ? r : m;
+      c.m[j] = c.m[j] > m ? c.m[j] : m;
+    }
+  }
+  static __device__ __forceinline__ uint32_t row_key(RowTop r) { return key(r); }
+  static __device__ __forceinline__ void col_keys(const ColTop& c, uint32_t (&w)[2]) {
+    w[0] = key(c.m[0]) | key(c.m[1]) << 16;
+    w[1] = key(c.m[2]) | key(c.m[3]) << 16;
+  }
+  static __device__ __forceinline__ uint32_t bf_keys(uint32_t w) { return w; }
+  __device__ __forceinline__ float at(int j) const { return v[j]; }
+  // nearest codes of this row's quad, and of column j over four rows
+  __device__ __forceinline__ uint32_t row_codes(float scale) const {
+    s16x2 w = {0, 0};
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, v[0], v[1], scale, false);
+    return as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, v[2], v[3], scale, true));
+  }
+  static __device__ __forceinline__ uint32_t col_codes(const Quad* q, int j, float scale) {
+    s16x2 w = {0, 0};
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, q[0].v[j], q[1].v[j], scale, false);
+    return as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, q[2].v[j], q[3].v[j], scale, true));
+  }
+};
+
+// 16-bit types: two elements a word throughout.
+template <class T>
+struct Quad16 {
+  uint32_t w[2];
+  __device__ __forceinline__ void load(const T* p, int64_t n) {
+    if (n >= 4) {
+      const auto v = *reinterpret_cast<const typename Packed<uint16_t, 4>::type*>(p);
+      w[0] = v[0] | (uint32_t)v[1] << 16;
+      w[1] = v[2] | (uint32_t)v[3] << 16;
+    } else {
+      const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+      w[0] = (n > 0 ? h[0] : 0u) | (n > 1 ? (uint32_t)h[1] << 16 : 0u);
+      w[1] = n > 2 ? h[2] : 0u;
+    }
+  }
+  typedef uint32_t RowTop;
+  struct ColTop {
+    uint32_t m[2];
+  };
+  __device__ __forceinline__ void top(RowTop& r, ColTop& c) const {
+    const uint32_t a = w[0] & 0x7fff7fffu, b = w[1] & 0x7fff7fffu;
+    c.m[0] = pk_max(c.m[0], a);
+    c.m[1] = pk_max(c.m[1], b);
+    r = pk_max(a, b);
+  }
+  static __device__ __forceinline__ uint32_t row_key(RowTop r) { return r >> 16 > (r & 0xffffu) ? r >> 16 : r & 0xffffu; }
+  static __device__ __forceinline__ void col_keys(const ColTop& c, uint32_t (&k)[2]) {
+    k[0] = c.m[0];
+    k[1] = c.m[1];
+  }
+  // the words of rows a and b: element j of each
+  static __device__ __forceinline__ uint32_t pair(uint32_t a, uint32_t b, int j) {
+    return __builtin_amdgcn_perm(b, a, (j & 1) ? 0x07060302u : 0x05040100u);
+  }
+};
+
+template <>
+struct Quad<__bf16> : Quad16<__bf16> {
+  static __device__ __forceinline__ uint32_t bf_keys(uint32_t k) { return k; }
+  __device__ __forceinline__ float at(int j) const {
+    return __uint_as_float((j & 1) ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
+  }
+  __device__ __forceinline__ uint32_t row_codes(float scale) const {
+    s16x2 o = {0, 0};
+    o = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(o, as<bf16x2>(w[0]), scale, false);
+    return as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(o, as<bf16x2>(w[1]), scale, true));
+  }
+  static __device__ __forceinline__ uint32_t col_codes(const Quad* q, int j, float scale) {
+    s16x2 o = {0, 0};
+    o = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(o, as<bf16x2>(pair(q[0].w[j >> 1], q[1].w[j >> 1], j)), scale, false);
+    return as<uint32_t>(
+        __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(o, as<bf16x2>(pair(q[2].w[j >> 1], q[3].w[j >> 1], j)), scale, true));
+  }
+};
+
+template <>
+struct Quad<_Float16> : Quad16<_Float16> {
+  // a float16 magnitude as the upper half of a float32, rounded up like Quad<float>'s
+  static __device__ __forceinline__ uint32_t bf_keys(uint32_t k) {
+    const f16x2 v = as<f16x2>(k);
+    return Quad<float>::key(__float_as_uint((float)v[0])) | Quad<float>::key(__float_as_uint((float)v[1])) << 16;
+  }
+  __device__ __forceinline__ float at(int j) const { return (float)as<f16x2>(w[j >> 1])[j & 1]; }
+  __device__ __forceinline__ uint32_t row_codes(float scale) const {
+    s16x2 o = {0, 0};
+    o = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(o, as<f16x2>(w[0]), scale, false);
+    return as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_fp8_f16(o, as<f16x2>(w[1]), scale, true));
+  }
+  static __device__ __forceinline__ uint32_t col_codes(const Quad* q, int j, float scale) {
+    s16x2 o = {0, 0};
+    o = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(o, as<f16x2>(pair(q[0].w[j >> 1], q[1].w[j >> 1], j)), scale, false);
+    return as<uint32_t>(
+        __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(o, as<f16x2>(pair(q[2].w[j >> 1], q[3].w[j >> 1], j)), scale, true));
+  }
+};
+
+// E + 127 of a block whose largest magnitude has the given key (0: 0, a block
+// of zeros; 247 where it should be NaN's 255), two at a time: the exponent,
+// one more above 1.75 2^p, less the format's 8, and not below 0.
+__device__ __forceinline__ uint32_t scale_bytes(uint32_t keys) {
+  const u16x2 e = (as<u16x2>(keys) + (unsigned short)0x1f) >> (unsigned short)7;
+  return as<uint32_t>(__builtin_elementwise_sub_sat(e, u16x2{8, 8}));
+}
+constexpr uint32_t NAN_KEY = 0x7f80u;  // keys from here on: infinity, NaN
+__device__ __forceinline__ uint8_t stored_byte(uint32_t key, uint32_t byte) {
+  return (uint8_t)(key == 0u ? 127u : (key >= NAN_KEY ? 255u : byte));
+}
+// 2^E, and its inverse.  (Byte 0 is the subnormal 2^-127.)
+__device__ __forceinline__ float scale_up(uint32_t byte) { return __uint_as_float(byte ? byte << 23 : 0x400000u); }
+__device__ __forceinline__ float scale_down(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+
+// Stochastic codes of four elements v 2^-E, |v 2^-E| <= 448, from the low 24
+// bits u of a word each.  With m the bits of |v 2^-E|: from 2^-6 on, the part
+// below the format's three mantissa bits is m's low 20 bits, so u < frac 2^24
+// says that u >> 4 is below them: adding the complement of u >> 4 carries into
+// the code, bits 20 and up, exactly then (less the exponents' difference of
+// 120; an element that is zero stays below and saturates to code 0).  Below
+// 2^-6 the step is 2^-9: ceil(|v 2^-E| 2^9 2^24) plus the complement of u
+// carries into bit 24.  Codes are formed in the top byte, with the sign.
+__device__ __forceinline__ uint32_t quad_codes(const float (&v)[4], const float (&down)[4], const u32x4& u) {
+  const uint32_t word[4] = {u.x, u.y, u.z, u.w};
+  uint32_t m[4], c[4], least = ~0u;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    m[j] = __float_as_uint(__builtin_fabsf(v[j]) * down[j]);
+    least = least < m[j] - 1u ? least : m[j] - 1u;
+    c[j] = __builtin_elementwise_sub_sat(m[j] + (~word[j] >> 4 & 0xfffffu), 120u << 23) << 4;
+  }
+  // rare: one element in thousands lies that far below its block's largest
+  if (__builtin_amdgcn_ballot_w64(least < 0x3c7fffffu) != 0) {  // 0 < |v 2^-E| < 2^-6
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t t = (uint32_t)ceilf(__uint_as_float(m[j]) * 8589934592.0f) + (~word[j] & 0xffffffu);
+      c[j] = m[j] < 0x3c800000u ? t : c[j];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) c[j] = (c[j] & 0x7fffffffu) | (__float_as_uint(v[j]) & 0x80000000u);
+  const uint32_t lo = __builtin_amdgcn_perm(c[1], c[0], 0x0c0c0703u);
+  uint32_t w = lo | __builtin_amdgcn_perm(c[3], c[2], 0x07030c0cu);
+  asm volatile("" : "+v"(w));  // packed here: the compiler would keep all rows' codes apart to the end
+  return w;
+}
+// 4 x 4 bytes turned over: byte k of o[j] is byte j of r[k].
+__device__ __forceinline__ void turn4(const uint32_t* r, uint32_t (&o)[4]) {
+  const uint32_t lo0 = __builtin_amdgcn_perm(r[1], r[0], 0x05010400u), hi0 = __builtin_amdgcn_perm(r[1], r[0], 0x07030602u);
+  const uint32_t lo1 = __builtin_amdgcn_perm(r[3], r[2], 0x05010400u), hi1 = __builtin_amdgcn_perm(r[3], r[2], 0x07030602u);
+  o[0] = __builtin_amdgcn_perm(lo1, lo0, 0x05040100u);
+  o[1] = __builtin_amdgcn_perm(lo1, lo0, 0x07060302u);
+  o[2] = __builtin_amdgcn_perm(hi1, hi0, 0x05040100u);
+  o[3] = __builtin_amdgcn_perm(hi1, hi0, 0x07060302u);
+}
+// The random words of elements e .. e + 3.
+__device__ __forceinline__ u32x4 quad_words(uint64_t e, uint64_t seed, uint32_t stream, bool whole) {
+  u32x4 u = philox_of_block(e >> 2, seed, stream);
+  if (!whole) {  // rows of a length off four: the quad may span two random blocks
+    const int o = (int)(e & 3);
+    const u32x4 n = philox_of_block((e >> 2) + 1, seed, stream);
+    if (o != 0)
+      u = o == 1 ? u32x4{u.y, u.z, u.w, n.x} : (o == 2 ? u32x4{u.z, u.w, n.x, n.y} : u32x4{u.w, n.x, n.y, n.z});
+  }
+  return u;
 }
 
 template <class T, bool ROW, bool COL, bool SQUARE, bool SR>
 __global__ __launch_bounds__(QT) void fp8_tile_kernel(Fp8QuantParams p) {
-  __shared__ uint32_t col_top[QT / 32][TILE];
+  __shared__ uint32_t col_top[QT / 32][TILE / 2];
+  __shared__ __attribute__((aligned(8))) uint16_t keys[2][TILE];  // of the rows, of the columns
   __shared__ __attribute__((aligned(16))) uint8_t turned[COL ? TILE * TILE : 16];
   const int tid = threadIdx.x, quad = tid & 31, grp = tid >> 5;
-  const int64_t row_blocks = fp8_blocks(p.rows);
-  const int64_t rb = (int64_t)blockIdx.x % row_blocks, cb = (int64_t)blockIdx.x / row_blocks;
-  const int64_t r0 = rb * TILE, c0 = cb * TILE;
+  const uint32_t row_blocks = (uint32_t)fp8_blocks(p.rows);
+  const uint32_t cb = blockIdx.x / row_blocks, rb = blockIdx.x - cb * row_blocks;
+  const int64_t r0 = (int64_t)rb * TILE, c0 = (int64_t)cb * TILE;
   const int64_t row = r0 + grp * GROUP, col = c0 + 4 * quad;
   const T* x = static_cast<const T*>(p.x) + row * p.ldx + col;
-  float v[GROUP][4];
+  Quad<T> v[GROUP];
 #pragma unroll
-  for (int i = 0; i < GROUP; ++i) load_part<T, 4>(x + i * p.ldx, row + i < p.rows ? p.cols - col : 0, v[i]);
+  for (int i = 0; i < GROUP; ++i) v[i].load(x + i * p.ldx, row + i < p.rows ? p.cols - col : 0);
 
-  // maxima of magnitudes, as integers (NaN above infinity above the rest)
-  uint32_t rt[GROUP], ct[4] = {0u, 0u, 0u, 0u};
+  // keys of the rows (two to a word) and columns
+  typename Quad<T>::ColTop ct{};
+  uint32_t rk[GROUP / 2], ck[2];
 #pragma unroll
-  for (int i = 0; i < GROUP; ++i) {
-    rt[i] = 0u;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t m = __float_as_uint(v[i][j]) & 0x7fffffffu;
-      if (ROW && !SQUARE) rt[i] = rt[i] > m ? rt[i] : m;
-      ct[j] = ct[j] > m ? ct[j] : m;
-    }
+  for (int i = 0; i < GROUP; i += 2) {
+    typename Quad<T>::RowTop a, b;
+    v[i].top(a, ct);
+    v[i + 1].top(b, ct);
+    if (ROW && !SQUARE) rk[i / 2] = Quad<T>::row_key(a) | Quad<T>::row_key(b) << 16;
   }
+  Quad<T>::col_keys(ct, ck);
   if constexpr (COL || SQUARE) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) col_top[grp][4 * quad + j] = ct[j];
+    *reinterpret_cast<uint2*>(&col_top[grp][2 * quad]) = make_uint2(ck[0], ck[1]);
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-#pragma unroll
-      for (int k = 0; k < QT / 32; ++k) {
-        const uint32_t m = col_top[k][4 * quad + j];
-        ct[j] = ct[j] > m ? ct[j] : m;
-      }
+    for (int k = 0; k < QT / 32; ++k) {
+      const uint2 m = *reinterpret_cast<const uint2*>(&col_top[k][2 * quad]);
+      ck[0] = pk_max(ck[0], m.x);
+      ck[1] = pk_max(ck[1], m.y);
     }
   }
-  uint32_t rbyte[GROUP], cbyte[4];
+  // the scale bytes of a line of blocks: one thread each, from the keys in LDS
+  auto store_bytes = [&](uint8_t* exp, int64_t lines, int64_t line, uint32_t b, uint32_t blocks,
+                         uint32_t k) __attribute__((always_inline)) {
+    if (line >= lines) return;
+    uint8_t* e = exp + ((int64_t)(b >> 2) * lines + line) * 4;
+    e[b & 3] = stored_byte(k, scale_bytes(k) & 0xffffu);
+    if (b == blocks - 1)  // the blocks that fill up the last four
+      for (uint32_t i = (b & 3) + 1; i < 4; ++i) e[i] = 127;
+  };
   if constexpr (SQUARE) {
-    uint32_t m = ct[0] > ct[1] ? ct[0] : ct[1];
-    const uint32_t n = ct[2] > ct[3] ? ct[2] : ct[3];
-    const uint32_t b = scale_byte(half_reduce(m > n ? m : n, MaxU{}));
+    const uint32_t m = half_reduce(pk_max(ck[0], ck[1]), PkMax{});
+    const uint32_t one = Quad<T>::bf_keys(pk_max(m, m >> 16 | m << 16));
+    ck[0] = ck[1] = one;
 #pragma unroll
-    for (int i = 0; i < GROUP; ++i) rbyte[i] = b;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) cbyte[j] = b;
+    for (int i = 0; i < GROUP / 2; ++i) rk[i] = one;
   } else {
+    if constexpr (ROW) {
 #pragma unroll
-    for (int i = 0; i < GROUP; ++i) rbyte[i] = ROW ? scale_byte(half_reduce(rt[i], MaxU{})) : 127u;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) cbyte[j] = scale_byte(ct[j]);
+      for (int i = 0; i < GROUP / 2; ++i) rk[i] = Quad<T>::bf_keys(half_reduce(rk[i], PkMax{}));
+    }
+    ck[0] = Quad<T>::bf_keys(ck[0]);
+    ck[1] = Quad<T>::bf_keys(ck[1]);
   }
-
-  if constexpr (ROW) {
-    const int64_t pitch = fp8_pitch(p.cols), kb = fp8_blocks(p.cols);
+  if (ROW && quad == 0) {
 #pragma unroll
-    for (int i = 0; i < GROUP; ++i) {
-      const float s = scale_down(rbyte[i]);
-      uint32_t w = 0u;
-      if constexpr (SR) {
-        const uint64_t e = (uint64_t)(row + i) * (uint64_t)p.cols + (uint64_t)col;
-        u32x4 u = philox_of_block(e >> 2, p.seed, 1u);
-        const int o = (int)(e & 3);
-        if (o != 0) {  // the quad spans two random blocks
-          const u32x4 n = philox_of_block((e >> 2) + 1, p.seed, 1u);
-          u = o == 1 ? u32x4{u.y, u.z, u.w, n.x} : (o == 2 ? u32x4{u.z, u.w, n.x, n.y} : u32x4{u.w, n.x, n.y, n.z});
+    for (int i = 0; i < GROUP / 2; i += 2)
+      *reinterpret_cast<uint2*>(&keys[0][grp * GROUP + 2 * i]) = make_uint2(rk[i], rk[i + 1]);
+  }
+  if (COL && grp == 0) *reinterpret_cast<uint2*>(&keys[1][4 * quad]) = make_uint2(ck[0], ck[1]);
+  __syncthreads();
+  if (ROW && tid < TILE) store_bytes(p.e_row, p.rows, r0 + tid, cb, (uint32_t)fp8_blocks(p.cols), keys[0][tid]);
+  if (COL && tid >= QT - TILE)
+    store_bytes(p.e_col, p.cols, c0 + tid - (QT - TILE), rb, row_blocks, keys[1][tid - (QT - TILE)]);
+  const bool whole = (p.cols & 3) == 0;  // a quad's elements share one random block
+
+  uint32_t key[4], byte[4], w[4][GROUP / 4];  // the columns'
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int sh = 16 * (j & 1);
+    key[j] = ck[j / 2] >> sh & 0xffffu;
+    byte[j] = scale_bytes(ck[j / 2]) >> sh & 0xffffu;
+  }
+  const int64_t row_pitch = fp8_pitch(p.cols);
+  uint8_t* const q_row = p.q_row + row * row_pitch + col;
+  auto store_row = [&](int i, uint32_t key, uint32_t codes) __attribute__((always_inline)) {
+    if (row + i < p.rows) *reinterpret_cast<uint32_t*>(q_row + i * row_pitch) = key >= NAN_KEY ? 0x7f7f7f7fu : codes;
+  };
+  if constexpr (SR) {
+    // both operands' codes of a row together: what their random words share is
+    // not kept over all rows
+#pragma unroll
+    for (int i = 0; i < GROUP; i += 4) {
+      uint32_t r[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float f[4] = {v[i + k].at(0), v[i + k].at(1), v[i + k].at(2), v[i + k].at(3)};
+        const uint64_t e = (uint64_t)(row + i + k) * (uint64_t)p.cols + (uint64_t)col;
+        if constexpr (ROW) {
+          const int sh = 16 * (k & 1);
+          const uint32_t rkey = rk[(i + k) / 2] >> sh & 0xffffu, rbyte = scale_bytes(rk[(i + k) / 2]) >> sh & 0xffffu;
+          const float s = scale_down(rbyte);
+          const float down[4] = {s, s, s, s};
+          store_row(i + k, rkey, quad_codes(f, down, quad_words(e, p.seed, 1u, whole)));
         }
-        w = stochastic_code(v[i][0] * s, u.x) | stochastic_code(v[i][1] * s, u.y) << 8 |
-            stochastic_code(v[i][2] * s, u.z) << 16 | stochastic_code(v[i][3] * s, u.w) << 24;
-      } else {
-        w = cvt2<true>(v[i][2] * s, v[i][3] * s, cvt2<false>(v[i][0] * s, v[i][1] * s, 0u));
-      }
-      if (rbyte[i] == 255u) w = 0x7f7f7f7fu;
-      if (row + i < p.rows) {
-        *reinterpret_cast<uint32_t*>(p.q_row + (row + i) * pitch + col) = w;
-        if (quad == 0) {
-          uint8_t* e = p.e_row + ((cb >> 2) * p.rows + row + i) * 4;
-          e[cb & 3] = (uint8_t)rbyte[i];
-          if (cb == kb - 1)  // the blocks that fill up the last four
-            for (int64_t b = (cb & 3) + 1; b < 4; ++b) e[b] = 127;
+        if constexpr (COL) {
+          const float down[4] = {scale_down(byte[0]), scale_down(byte[1]), scale_down(byte[2]), scale_down(byte[3])};
+          r[k] = quad_codes(f, down, quad_words(e, p.seed, 0u, whole));
         }
+        __builtin_amdgcn_sched_barrier(0);  // one row at a time: fewer registers, more waves
       }
+      if constexpr (COL) {
+        uint32_t o[4];
+        turn4(r, o);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j][i / 4] = o[j];
+      }
+    }
+  } else {
+    if constexpr (ROW) {
+#pragma unroll
+      for (int i = 0; i < GROUP; ++i) {
+        const int sh = 16 * (i & 1);
+        const uint32_t rbyte = scale_bytes(rk[i / 2]) >> sh & 0xffffu;
+        store_row(i, rk[i / 2] >> sh & 0xffffu, v[i].row_codes(scale_up(rbyte)));
+      }
+    }
+    if constexpr (COL) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < GROUP; i += 4) w[j][i / 4] = Quad<T>::col_codes(v + i, j, scale_up(byte[j]));
     }
   }
   if constexpr (COL) {
-    const int64_t pitch = fp8_pitch(p.rows), kb = row_blocks;
+    const int64_t pitch = fp8_pitch(p.rows);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float s = scale_down(cbyte[j]);
-      uint32_t w[GROUP / 4];
-#pragma unroll
-      for (int i = 0; i < GROUP / 4; ++i) {
-        if constexpr (SR) {
-          w[i] = 0u;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const uint64_t e = (uint64_t)(row + 4 * i + k) * (uint64_t)p.cols + (uint64_t)(col + j);
-            const u32x4 u = philox_of_block(e >> 2, p.seed, 0u);
-            const int o = (int)(e & 3);
-            const uint32_t word = o == 0 ? u.x : (o == 1 ? u.y : (o == 2 ? u.z : u.w));
-            w[i] |= stochastic_code(v[4 * i + k][j] * s, word) << (8 * k);
-          }
-        } else {
-          w[i] = cvt2<true>(v[4 * i + 2][j] * s, v[4 * i + 3][j] * s,
-                            cvt2<false>(v[4 * i][j] * s, v[4 * i + 1][j] * s, 0u));
-        }
-        if (cbyte[j] == 255u) w[i] = 0x7f7f7f7fu;
-      }
+      if (key[j] >= NAN_KEY) w[j][0] = w[j][1] = w[j][2] = w[j][3] = 0x7f7f7f7fu;
       // column 4 quad + j, rows 16 grp ..: chunk index swizzled by the quad so
       // that eight lanes' 16-byte words fall on distinct banks
       *reinterpret_cast<uint4*>(turned + (4 * quad + j) * TILE + 16 * (grp ^ (quad & 7))) =
-          make_uint4(w[0], w[1], w[2], w[3]);
-    }
-    if (grp == 0) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (col + j < p.cols) {
-          uint8_t* e = p.e_col + ((rb >> 2) * p.cols + col + j) * 4;
-          e[rb & 3] = (uint8_t)cbyte[j];
-          if (rb == kb - 1)
-            for (int64_t b = (rb & 3) + 1; b < 4; ++b) e[b] = 127;
-        }
+          make_uint4(w[j][0], w[j][1], w[j][2], w[j][3]);
     }
     __syncthreads();
     // eight lanes store one column's 128-byte block
 #pragma unroll
     for (int k = 0; k < TILE * TILE / 16 / QT; ++k) {
       const int c = (tid >> 3) + k * (QT / 8), chunk = tid & 7;
-      const uint4 w = *reinterpret_cast<const uint4*>(turned + c * TILE + 16 * (chunk ^ ((c >> 2) & 7)));
-      if (c0 + c < p.cols) *reinterpret_cast<uint4*>(p.q_col + (c0 + c) * pitch + r0 + 16 * chunk) = w;
+      const uint4 o = *reinterpret_cast<const uint4*>(turned + c * TILE + 16 * (chunk ^ ((c >> 2) & 7)));
+      if (c0 + c < p.cols) *reinterpret_cast<uint4*>(p.q_col + (c0 + c) * pitch + r0 + 16 * chunk) = o;
     }
   }
 }
 
 // Codes laid out column by column, [pitch][rows], into rows [rows][pitch]:
-// 128 x 128 bytes a block, turned over in LDS.
+// 128 x 128 bytes a block; a thread turns 4 x 4 bytes over in registers, LDS
+// gathers rows of 128.
 __global__ __launch_bounds__(QT) void fp8_turn_kernel(const uint8_t* src, int64_t rows, int64_t pitch, uint8_t* dst) {
-  __shared__ uint8_t sh[TILE][TILE + 4];
+  __shared__ uint32_t sh[TILE][TILE / 4 + 1];
   const int64_t kblocks = pitch / TILE;
   const int64_t k0 = (int64_t)blockIdx.x % kblocks * TILE, r0 = (int64_t)blockIdx.x / kblocks * TILE;
-  for (int i = threadIdx.x; i < TILE * TILE; i += QT) {
-    const int k = i / TILE, r = i % TILE;
-    if (r0 + r < rows) sh[r][k] = src[(k0 + k) * rows + r0 + r];
+  const int quad = threadIdx.x & 31, grp = threadIdx.x >> 5;
+  const int64_t row = r0 + 4 * quad, left = rows - row;
+  uint32_t in[GROUP];
+#pragma unroll
+  for (int i = 0; i < GROUP; ++i) {
+    const uint8_t* p = src + (k0 + grp * GROUP + i) * rows + row;
+    if (left >= 4) {
+      __builtin_memcpy(&in[i], p, 4);
+    } else {
+      in[i] = (left > 0 ? p[0] : 0u) | (left > 1 ? (uint32_t)p[1] << 8 : 0u) | (left > 2 ? (uint32_t)p[2] << 16 : 0u);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < GROUP; i += 4) {
+    uint32_t o[4];
+    turn4(in + i, o);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sh[4 * quad + j][(grp * GROUP + i) / 4] = o[j];
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < TILE * TILE / 4; i += QT) {
-    const int r = i / (TILE / 4), k = 4 * (i % (TILE / 4));
+#pragma unroll
+  for (int i = 0; i < TILE * TILE / 16 / QT; ++i) {
+    const int r = (threadIdx.x >> 3) + i * (QT / 8), c = 4 * (threadIdx.x & 7);
     if (r0 + r < rows)
-      *reinterpret_cast<uint32_t*>(dst + (r0 + r) * pitch + k0 + k) = *reinterpret_cast<const uint32_t*>(&sh[r][k]);
+      *reinterpret_cast<uint4*>(dst + (r0 + r) * pitch + k0 + 4 * c) =
+          make_uint4(sh[r][c], sh[r][c + 1], sh[r][c + 2], sh[r][c + 3]);
   }
 }
 

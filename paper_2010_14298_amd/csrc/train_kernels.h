@@ -75,7 +75,7 @@ inline bool valid_type(fqt_dtype t) { return t == FQT_F32 || t == FQT_BF16 || t 
 // ---------------------------------------------------------------------------
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp(uint32_t v) {
-  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false);
+  return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xf, 0xf, true);
 }
 constexpr int DPP_ROR = 0x120;  // + n: rotate right by n inside 16 lanes
 

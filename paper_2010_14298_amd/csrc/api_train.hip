@@ -24,6 +24,8 @@ struct Carver {
 
 constexpr int64_t MAX_SIDE = (int64_t)1 << 31;   // rows or columns of a matrix
 bool side(int64_t n) { return n >= 1 && n < MAX_SIDE; }
+// the products address a tile of 256 rows of codes with 31-bit offsets
+constexpr int64_t MAX_CONTRACTION = (int64_t)1 << 23;
 size_t type_bytes(fqt_dtype t) { return t == FQT_F32 ? 4 : 2; }
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 // an input matrix: element-aligned; its rows may overlap (ld 0: one row for all)
@@ -214,6 +216,7 @@ fqt_status fqt_fp8_gemm(const fqt_fp8* A, const fqt_fp8* B, int64_t M, int64_t N
   if (!valid_type(type) || !side(M) || !side(N) || !side(K) || !operand(A) || !operand(B)) return FQT_EINVAL;
   if (!output(C, type, N, ldc) || (mask && !input(mask, type, ldmask)) || (relu != 0 && relu != 1))
     return FQT_EINVAL;
+  if (K > MAX_CONTRACTION) return FQT_EUNSUPPORTED;
   if (!ws || !aligned(ws, 16) || ws_bytes < fqt_fp8_gemm_workspace(M, N, K)) return FQT_EWORKSPACE;
   Carver c(ws);
   const GemmWs w = carve_gemm(c, M, N, K);
@@ -248,21 +251,26 @@ fqt_status fqt_fp8_linear_forward(const void* X, fqt_dtype type, int64_t N, int6
   if (!valid_type(type) || !side(N) || !side(d_in) || !side(d_out) || !operand(W8)) return FQT_EINVAL;
   if (!input(X, type, ldx) || !output(Y, type, d_out, ldy) || (relu != 0 && relu != 1)) return FQT_EINVAL;
   if (X8t && !written(X8t)) return FQT_EINVAL;
+  if (d_in > MAX_CONTRACTION) return FQT_EUNSUPPORTED;
   if (!ws || !aligned(ws, 16) || ws_bytes < fqt_fp8_linear_forward_workspace(N, d_in, d_out)) return FQT_EWORKSPACE;
   Carver c(ws);
   const ForwardWs w = carve_forward(c, N, d_in, d_out);
+  // few rows are quantized by the product itself
+  const bool raw = fp8_rows_raw(N);
   Fp8QuantParams q{};
   q.x = X;
   q.rows = N;
   q.cols = d_in;
   q.ldx = ldx;
-  q.q_row = w.x.q;
-  q.e_row = w.x.e;
+  if (!raw) {
+    q.q_row = w.x.q;
+    q.e_row = w.x.e;
+  }
   if (X8t) {
     q.q_col = X8t->q;
     q.e_col = X8t->exp;
   }
-  FQT_TRY(launch_fp8_quantize(type, q, s));
+  if (q.q_row || q.q_col) FQT_TRY(launch_fp8_quantize(type, q, s));
   Fp8GemmParams p{};
   p.A = w.x.q;
   p.eA = w.x.e;
@@ -275,7 +283,10 @@ fqt_status fqt_fp8_linear_forward(const void* X, fqt_dtype type, int64_t N, int6
   p.ldc = ldy;
   p.relu = relu;
   p.part = w.part;
-  FQT_TRY(launch_fp8_gemm(type, p, s));
+  if (raw)
+    FQT_TRY(launch_fp8_rows(type, p, X, ldx, s));
+  else
+    FQT_TRY(launch_fp8_gemm(type, p, s));
   return FQT_OK;
 }
 
@@ -295,6 +306,7 @@ fqt_status fqt_fp8_linear_backward(const void* G, fqt_dtype type, int64_t N, int
   if (grad_W && (!operand(X8t) || !aligned(grad_W, 4))) return FQT_EINVAL;
   if (grad_X && (!operand(W8t) || !output(grad_X, type, d_in, ldgx))) return FQT_EINVAL;
   if (relu_input && !input(relu_input, type, ldr)) return FQT_EINVAL;
+  if ((grad_W && N > MAX_CONTRACTION) || (grad_X && d_out > MAX_CONTRACTION)) return FQT_EUNSUPPORTED;
   if (!ws || !aligned(ws, 16) || ws_bytes < fqt_fp8_linear_backward_workspace(N, d_in, d_out)) return FQT_EWORKSPACE;
   Carver c(ws);
   const BackwardWs w = carve_backward(c, N, d_in, d_out);

@@ -12,22 +12,22 @@
 //     (v_cvt_scalef32_pk_bf16_fp8, exact) and go through
 //     v_mfma_f32_32x32x16_bf16 at half the rate, which sums to 1.5e-7.
 // The output is rounded once.
-#include "train_kernels.h"
+#include "fp8_codes.h"
 
 namespace fqt {
 
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef int v4i __attribute__((ext_vector_type(4)));
+typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v2b __attribute__((ext_vector_type(2)));
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(1))) void gmem_void;
 typedef __attribute__((address_space(3))) void lmem_void;
 
-// Block tile BM x BN in eight waves of WM x WN.
-template <int BM_, int BN_, int WM_, int WN_>
-struct Fp8Tile {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+// The large tile: 256 x 256 in eight waves of 128 x 64.
+struct LargeTile {
+  static constexpr int BM = 256, BN = 256, WM = 128, WN = 64;
   static constexpr int WAVES_N = BN / WN, WAVES = (BM / WM) * WAVES_N, THREADS = WAVES * 64;
   static constexpr int IT = WM / 32, JT = WN / 32;
   static constexpr int HALF = (BM + BN) * 64;               // half a stage (64 along K) of codes, A then B
@@ -53,9 +53,9 @@ __device__ __forceinline__ void block_tile(int64_t id, int64_t tm, int64_t tn, i
 }
 
 // Stores a wave's 32-row strip of outputs that lies in LDS as float32.
-template <class T, class C, bool NT>
+template <class T, int WN, int OUT_LD, bool NT>
 __device__ __forceinline__ void store_strip(const Fp8GemmParams& p, const float* strip, int64_t row0, int64_t col0) {
-  constexpr int V = 16 / (int)sizeof(T), LANES = C::WN / V, ROWS = 64 / LANES;
+  constexpr int V = 16 / (int)sizeof(T), LANES = WN / V, ROWS = 64 / LANES;
   const int lane = threadIdx.x & 63, lr = lane / LANES, lc = (lane % LANES) * V;
 #pragma unroll
   for (int r = 0; r < 32; r += ROWS) {
@@ -63,7 +63,7 @@ __device__ __forceinline__ void store_strip(const Fp8GemmParams& p, const float*
     if (row >= p.M || col >= p.N) continue;
     float o[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) o[i] = strip[(r + lr) * C::OUT_LD + lc + i];
+    for (int i = 0; i < V; ++i) o[i] = strip[(r + lr) * OUT_LD + lc + i];
     if (p.relu) {
 #pragma unroll
       for (int i = 0; i < V; ++i) o[i] = o[i] < 0.0f ? 0.0f : o[i];
@@ -130,6 +130,22 @@ __device__ __forceinline__ void meet() {
   asm volatile("" ::: "memory");
 }
 
+// Instruction order of a widened multiply segment: QS steps of MF matrix
+// instructions, whose operands take CV conversions each.  The first step's
+// conversions go in front, the next step's between the matrix instructions,
+// in the 32 cycles that each of those keeps the matrix cores busy.
+template <int QS, int MF, int CV>
+__device__ __forceinline__ void interleave() {
+  __builtin_amdgcn_sched_group_barrier(0x2, CV, 0);  // VALU
+#pragma unroll
+  for (int q = 0; q < QS; ++q)
+#pragma unroll
+    for (int m = 0; m < MF; ++m) {
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);  // MFMA
+      if (q + 1 < QS) __builtin_amdgcn_sched_group_barrier(0x2, CV / MF, 0);
+    }
+}
+
 // The K loop works in half stages of 64 along K, each with a buffer of its
 // own (two stages, four buffers), filled by direct loads to LDS.  Rows of 64
 // bytes, the 16-byte chunk index XOR-ed with (r / 4) mod 4, so that the 16
@@ -145,8 +161,9 @@ __device__ __forceinline__ void meet() {
 // the loads of (t + 2, 0); read (t + 1, 0) issues those of (t + 2, 1).  Loads
 // have to be complete before the waves in front read them, so every wave
 // waits for the half stage after next at the end of its read segment.
-template <class T, class C, bool NT>
-__global__ __launch_bounds__(C::THREADS) void fp8_gemm_kernel(Fp8GemmParams p) {
+template <class T, bool WIDE, bool NT>
+__global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(Fp8GemmParams p) {
+  using C = LargeTile;
   // separate arrays, so that a pending load into one does not hold up reads of another
   __shared__ __attribute__((aligned(16))) uint8_t h00[C::HALF], h01[C::HALF], h10[C::HALF], h11[C::HALF];
   __shared__ int e0[C::BM + C::BN], e1[C::BM + C::BN];
@@ -224,7 +241,7 @@ __global__ __launch_bounds__(C::THREADS) void fp8_gemm_kernel(Fp8GemmParams p) {
   };
   auto multiply = [&]() __attribute__((always_inline)) {
     __builtin_amdgcn_s_setprio(1);
-    if constexpr (sizeof(T) == 2) {
+    if constexpr (!WIDE) {
 #pragma unroll
       for (int i = 0; i < C::IT; ++i)
 #pragma unroll
@@ -249,6 +266,7 @@ __global__ __launch_bounds__(C::THREADS) void fp8_gemm_kernel(Fp8GemmParams p) {
           for (int j = 0; j < C::JT; ++j)
             acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wa[i], wb[j], acc[i][j], 0, 0, 0);
       }
+      interleave<4, C::IT * C::JT, 4 * (C::IT + C::JT)>();
     }
     __builtin_amdgcn_s_setprio(0);
     // the products belong to this segment: keep the compiler from moving them past the barrier
@@ -328,40 +346,521 @@ __global__ __launch_bounds__(C::THREADS) void fp8_gemm_kernel(Fp8GemmParams p) {
       for (int r = 0; r < 16; ++r)
         strip[(8 * (r >> 2) + 4 * half + (r & 3)) * C::OUT_LD + j * 32 + lrow] = acc[i][j][r];
     __builtin_amdgcn_wave_barrier();
-    store_strip<T, C, NT>(p, strip, m0 + wm * C::WM + i * 32, n0 + wn * C::WN);
+    store_strip<T, C::WN, C::OUT_LD, NT>(p, strip, m0 + wm * C::WM + i * 32, n0 + wn * C::WN);
     __builtin_amdgcn_wave_barrier();
   }
 }
 
-using Fp8Large = Fp8Tile<256, 256, 128, 64>;
-using Fp8Mid = Fp8Tile<256, 128, 64, 64>;
-using Fp8Small = Fp8Tile<128, 128, 64, 32>;
+// ---------------------------------------------------------------------------
+// The pipelined loop: every wave reads the next step's operands from LDS while
+// it multiplies the current ones; one barrier a stage of 128 along K.  KG = 2:
+// half of the waves take the first half of each stage along K, half the
+// second, and their sums meet in LDS at the end, so that a wave's tile is
+// twice as large and reads (and widens) less for each product.  NS whole
+// stages of 128-byte rows in LDS, the 16-byte chunk index XOR-ed with (r / 2)
+// mod 8.  SPLIT: blockIdx.y takes `chunk` stages and leaves float32 sums in
+// p.part.
+// ---------------------------------------------------------------------------
+template <int BM_, int BN_, int WM_, int WN_, int KG_, int NS_>
+struct PipeTile {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KG = KG_, NS = NS_;
+  static constexpr int WAVES_N = BN / WN, PLANE = (BM / WM) * WAVES_N;  // waves over the output
+  static constexpr int IT = WM / 32, JT = WN / 32, STEPS = 2 / KG;      // steps of 64 along K a stage and wave
+  static constexpr int CODES = (BM + BN) * FP8_BLOCK;
+  static constexpr int INS = (BM + BN) / 64;                            // 1 KB loads of a wave and stage, eight rows each
+  static constexpr int E_SEGS = (BM + BN) / 64;
+  static constexpr int OUT_LD = WN + 8;
+  static_assert(PLANE * KG == 8 && E_SEGS <= 8 && NS >= 2 && NS <= 4, "eight waves");
+};
 
-int64_t fp8_gemm_partials(int64_t, int64_t, int64_t) { return 0; }
+// WIDE: through bfloat16.  T: the stored type (SPLIT: float).
+template <class T, class C, bool WIDE, bool SPLIT, bool NT>
+__global__ __launch_bounds__(512) void fp8_gemm_pipe_kernel(Fp8GemmParams p, int chunk) {
+  __shared__ __attribute__((aligned(16))) uint8_t q0[C::CODES], q1[C::CODES], q2[C::NS > 2 ? C::CODES : 16],
+      q3[C::NS > 3 ? C::CODES : 16];
+  __shared__ int x0[C::BM + C::BN], x1[C::BM + C::BN], x2[C::NS > 2 ? C::BM + C::BN : 4], x3[C::NS > 3 ? C::BM + C::BN : 4];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kg = wave / C::PLANE, wm = wave % C::PLANE / C::WAVES_N, wn = wave % C::WAVES_N;
+  int64_t tm, tn;
+  block_tile(blockIdx.x, (p.M + C::BM - 1) / C::BM, (p.N + C::BN - 1) / C::BN, tm, tn);
+  const int64_t m0 = tm * C::BM, n0 = tn * C::BN;
+  const int64_t pitch = fp8_pitch(p.K);
+  const int all = (int)fp8_blocks(p.K), first = SPLIT ? (int)blockIdx.y * chunk : 0;
+  const int nk = SPLIT && first + chunk < all ? chunk : all - first;
+  const int lastA = p.M - 1 - m0 < C::BM - 1 ? (int)(p.M - 1 - m0) : C::BM - 1;
+  const int lastB = p.N - 1 - n0 < C::BN - 1 ? (int)(p.N - 1 - n0) : C::BN - 1;
+  const Rows rowsA(p.A + m0 * pitch + (int64_t)first * FP8_BLOCK), rowsB(p.B + n0 * pitch + (int64_t)first * FP8_BLOCK);
+  // this wave's 1 KB loads, eight rows each: of A, then of B
+  int src[C::INS];
+#pragma unroll
+  for (int i = 0; i < C::INS; ++i) {
+    const int at = 8 * (wave * C::INS + i), r = at + (lane >> 3);
+    const bool a = at < C::BM;
+    const int row = a ? r : r - C::BM, last = a ? lastA : lastB;
+    src[i] = (row < last ? row : last) * (int)pitch + 16 * ((lane & 7) ^ ((r >> 1) & 7));
+  }
+  // scale words: a run of 64 rows a wave (fewer runs than waves: some twice)
+  const int seg = wave % C::E_SEGS;
+  const bool eA = seg * 64 < C::BM;
+  const int er = seg * 64 - (eA ? 0 : C::BM) + lane, elast = eA ? lastA : lastB;
+  const uint8_t* const ebase = eA ? p.eA + m0 * 4 : p.eB + n0 * 4;
+  const int64_t estep = (eA ? p.M : p.N) * 4;
+  const int esrc = 4 * (er < elast ? er : elast);
+  auto load = [&](uint8_t* d, int* e, int t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < C::INS; ++i)
+      (8 * (wave * C::INS + i) < C::BM ? rowsA : rowsB).to_lds16(d + (wave * C::INS + i) * 1024, src[i], t * FP8_BLOCK);
+    Rows(ebase + ((first + t) >> 2) * estep).to_lds4(e + seg * 64, esrc);
+  };
+  constexpr int PER = C::INS + 1;  // loads of a stage and wave
+  v16f acc[C::IT][C::JT];
+#pragma unroll
+  for (int i = 0; i < C::IT; ++i)
+#pragma unroll
+    for (int j = 0; j < C::JT; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+  const int lrow = lane & 31, half = lane >> 5, sw = (lrow >> 1) & 7;
+  const int offA = (wm * C::WM + lrow) * FP8_BLOCK, offB = (C::BM + wn * C::WN + lrow) * FP8_BLOCK;
+  struct Operands {
+    v8i a[C::IT], b[C::JT];
+    int sa[C::IT], sb[C::JT];
+  } set0, set1;
+  // the operands of one step: codes 64 kk .. + 63 of the stage, and its scales
+  auto read = [&](Operands& o, const uint8_t* st, const int* e, int t, int kk) __attribute__((always_inline)) {
+    const int c0 = 16 * ((4 * kk + 2 * half) ^ sw), c1 = 16 * ((4 * kk + 2 * half + 1) ^ sw);
+    const int sh = 8 * ((first + t) & 3);
+    auto frag = [&](const uint8_t* q) __attribute__((always_inline)) {
+      const v4i x = *reinterpret_cast<const v4i*>(q + c0);
+      const v4i y = *reinterpret_cast<const v4i*>(q + c1);
+      return v8i{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+    };
+#pragma unroll
+    for (int i = 0; i < C::IT; ++i) {
+      o.a[i] = frag(st + offA + i * 32 * FP8_BLOCK);
+      o.sa[i] = e[wm * C::WM + i * 32 + lrow] >> sh;
+    }
+#pragma unroll
+    for (int j = 0; j < C::JT; ++j) {
+      o.b[j] = frag(st + offB + j * 32 * FP8_BLOCK);
+      o.sb[j] = e[C::BM + wn * C::WN + j * 32 + lrow] >> sh;
+    }
+  };
+  auto multiply = [&](const Operands& o) __attribute__((always_inline)) {
+    if constexpr (!WIDE) {
+#pragma unroll
+      for (int i = 0; i < C::IT; ++i)
+#pragma unroll
+        for (int j = 0; j < C::JT; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(o.a[i], o.b[j], acc[i][j], 0, 0, 0, o.sa[i], 0,
+                                                                      o.sb[j]);
+    } else {
+      float fa[C::IT], fb[C::JT];
+#pragma unroll
+      for (int i = 0; i < C::IT; ++i) fa[i] = scale_of(o.sa[i], 0);
+#pragma unroll
+      for (int j = 0; j < C::JT; ++j) fb[j] = scale_of(o.sb[j], 0);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        v8b wa[C::IT], wb[C::JT];
+#pragma unroll
+        for (int j = 0; j < C::JT; ++j) wb[j] = widen(o.b[j][2 * q], o.b[j][2 * q + 1], fb[j]);
+#pragma unroll
+        for (int i = 0; i < C::IT; ++i) wa[i] = widen(o.a[i][2 * q], o.a[i][2 * q + 1], fa[i]);
+#pragma unroll
+        for (int i = 0; i < C::IT; ++i)
+#pragma unroll
+          for (int j = 0; j < C::JT; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wa[i], wb[j], acc[i][j], 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < C::IT; ++i)
+#pragma unroll
+      for (int j = 0; j < C::JT; ++j) asm volatile("" : "+v"(acc[i][j]));
+  };
+  // Stage t, whose first step's operands are in `cur`; q, e: its buffer, qn, en:
+  // the next one's.  The barrier says that stage t + 1 has landed and that
+  // everyone has read stage t, whose buffer then takes stage t + NS.
+  auto stage = [&](auto inner, int t, Operands& cur, Operands& nxt, uint8_t* q, int* e, const uint8_t* qn,
+                   const int* en) __attribute__((always_inline)) {
+    if constexpr (C::STEPS == 2) {
+      read(nxt, q, e, t, 1);
+      multiply(cur);
+    }
+    if (inner) {
+      wait_loads<(C::NS - 2) * PER>();
+    } else if (t + 1 < nk) {
+      const int later = nk - t - 2;  // stages behind t + 1 that are under way
+      if (C::NS > 3 && later >= 2)
+        wait_loads<2 * PER>();
+      else if (C::NS > 2 && later >= 1)
+        wait_loads<PER>();
+      else
+        wait_loads<0>();
+    }
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    meet();
+    if (inner || t + 1 < nk) read(C::STEPS == 2 ? cur : nxt, qn, en, t + 1, C::STEPS == 2 ? 0 : kg);
+    if (inner || t + C::NS < nk) load(q, e, t + C::NS);
+    multiply(C::STEPS == 2 ? nxt : cur);
+  };
+  load(q0, x0, 0);
+  if (nk > 1) load(q1, x1, 1);
+  if (C::NS > 2 && nk > 2) load(q2, x2, 2);
+  if (C::NS > 3 && nk > 3) load(q3, x3, 3);
+  if (nk >= C::NS)
+    wait_loads<(C::NS - 1) * PER>();
+  else
+    wait_loads<0>();
+  meet();
+  read(set0, q0, x0, 0, C::STEPS == 2 ? 0 : kg);
+  constexpr std::true_type inner{};
+  constexpr std::false_type last{};
+  // with one step a stage the operand sets swap every stage, with two they end as they began
+  Operands& odd = C::STEPS == 2 ? set0 : set1;
+  Operands& even = C::STEPS == 2 ? set1 : set0;
+  int t = 0;
+  auto turn = [&](auto in) __attribute__((always_inline)) {
+    auto go = [&](int k, Operands& c, Operands& n, uint8_t* q, int* e, const uint8_t* qn, const int* en)
+                  __attribute__((always_inline)) {
+      if (in || t + k < nk) stage(in, t + k, c, n, q, e, qn, en);
+    };
+    if constexpr (C::NS == 2) {
+      go(0, set0, set1, q0, x0, q1, x1);
+      go(1, odd, even, q1, x1, q0, x0);
+    } else if constexpr (C::NS == 3) {
+      go(0, set0, set1, q0, x0, q1, x1);
+      go(1, odd, even, q1, x1, q2, x2);
+      go(2, set0, set1, q2, x2, q0, x0);
+      if constexpr (C::STEPS == 1) {
+        go(3, odd, even, q0, x0, q1, x1);
+        go(4, set0, set1, q1, x1, q2, x2);
+        go(5, odd, even, q2, x2, q0, x0);
+      }
+    } else {
+      go(0, set0, set1, q0, x0, q1, x1);
+      go(1, odd, even, q1, x1, q2, x2);
+      go(2, set0, set1, q2, x2, q3, x3);
+      go(3, odd, even, q3, x3, q0, x0);
+    }
+  };
+  constexpr int TURN = C::NS == 3 && C::STEPS == 1 ? 6 : C::NS;  // stages of a turn
+  for (; t + TURN - 1 + C::NS < nk; t += TURN) turn(inner);
+  for (; t < nk; t += TURN) turn(last);
+  __syncthreads();
+  if constexpr (C::KG == 2) {
+    // the two halves of K: each wave hands half of its rows to its partner
+    constexpr int HI = C::IT / 2, BYTES = HI * C::JT * 4096, FIT = C::CODES / BYTES;
+    static_assert(FIT * C::NS >= 8, "the exchange fits the stage buffers");
+    auto room = [&](int w) __attribute__((always_inline)) {
+      uint8_t* const b = w / FIT == 0 ? q0 : (w / FIT == 1 ? q1 : (w / FIT == 2 ? q2 : q3));
+      return reinterpret_cast<float4*>(b + w % FIT * BYTES) + lane;
+    };
+    float4* const give = room(wave);
+#pragma unroll
+    for (int i = 0; i < HI; ++i)
+#pragma unroll
+      for (int j = 0; j < C::JT; ++j) {
+        const v16f lo = acc[i][j], hi = acc[HI + i][j], v = kg ? lo : hi;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          give[((i * C::JT + j) * 4 + r) * 64] = make_float4(v[4 * r], v[4 * r + 1], v[4 * r + 2], v[4 * r + 3]);
+      }
+    __syncthreads();
+    const float4* const take = room(wave ^ 4);
+#pragma unroll
+    for (int i = 0; i < HI; ++i)
+#pragma unroll
+      for (int j = 0; j < C::JT; ++j) {
+        const v16f lo = acc[i][j], hi = acc[HI + i][j];
+        v16f v = kg ? hi : lo;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float4 o = take[((i * C::JT + j) * 4 + r) * 64];
+          v[4 * r] += o.x;
+          v[4 * r + 1] += o.y;
+          v[4 * r + 2] += o.z;
+          v[4 * r + 3] += o.w;
+        }
+        acc[i][j] = v;
+      }
+    __syncthreads();
+  }
+  constexpr int STRIPS = C::IT / C::KG, STRIP = 32 * C::OUT_LD * 4, FIT = C::CODES / STRIP;
+  static_assert(FIT * C::NS >= 8, "the output strips fit the stage buffers");
+  uint8_t* const own = (wave / FIT == 0 ? q0 : (wave / FIT == 1 ? q1 : (wave / FIT == 2 ? q2 : q3))) + wave % FIT * STRIP;
+  float* const strip = reinterpret_cast<float*>(own);
+#pragma unroll
+  for (int i = 0; i < STRIPS; ++i) {
+#pragma unroll
+    for (int j = 0; j < C::JT; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        strip[(8 * (r >> 2) + 4 * half + (r & 3)) * C::OUT_LD + j * 32 + lrow] = acc[i][j][r];
+    __builtin_amdgcn_wave_barrier();
+    const int64_t row0 = m0 + wm * C::WM + (kg * STRIPS + i) * 32, col0 = n0 + wn * C::WN;
+    if constexpr (SPLIT) {
+      Fp8GemmParams o = p;
+      o.C = p.part + (int64_t)blockIdx.y * p.M * p.N;
+      o.ldc = p.N;
+      o.relu = 0;
+      o.mask = nullptr;
+      store_strip<float, C::WN, C::OUT_LD, false>(o, strip, row0, col0);
+    } else {
+      store_strip<T, C::WN, C::OUT_LD, NT>(p, strip, row0, col0);
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
 
-template <class C>
-static int64_t tiles_of(int64_t M, int64_t N) {
-  return ((M + C::BM - 1) / C::BM) * ((N + C::BN - 1) / C::BN);
+// The parts of a split product added in order, with the product's epilogue.
+template <class T>
+__global__ __launch_bounds__(256) void fp8_split_sum_kernel(Fp8GemmParams p, int splits) {
+  const int64_t quads = (p.N + 3) / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= p.M * quads) return;
+  const int64_t row = i / quads, col = i % quads * 4, n = p.N - col;
+  float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int s = 0; s < splits; ++s) {
+    float v[4];
+    load_part<float, 4>(p.part + (s * p.M + row) * p.N + col, n, v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] += v[j];
+  }
+  if (p.relu) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] = o[j] < 0.0f ? 0.0f : o[j];
+  }
+  if (p.mask) {
+    float m[4];
+    load_part<T, 4>(static_cast<const T*>(p.mask) + row * p.ldmask + col, n, m);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] = m[j] > 0.0f ? o[j] : 0.0f;
+  }
+  store_part<T, 4>(static_cast<T*>(p.C) + row * p.ldc + col, n, o);
+}
+
+// ---------------------------------------------------------------------------
+// Few rows of A (serving: single tokens): the weights stream from memory to
+// registers once, 16 outputs a block, its waves take every eighth block of K
+// and add up in LDS.  A from raw rows (X is quantized here, in registers: every
+// block of threads needs all of it, but it is small) or from codes.
+// v_mfma_scale_f32_16x16x128_f8f6f4: lane l holds row l % 16, codes
+// 32 (l / 16) .. + 31 of a block.
+// ---------------------------------------------------------------------------
+constexpr int ROW_WAVES = 8;
+
+template <class X>
+__device__ __forceinline__ v8i row_block(const X* x, int64_t left, int& byte) {
+  Quad<X> v[8];
+  uint32_t key = 0u;
+  typename Quad<X>::ColTop unused{};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i].load(x + 4 * i, left - 4 * i);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    typename Quad<X>::RowTop r;
+    v[i].top(r, unused);
+    const uint32_t k = Quad<X>::row_key(r);
+    key = key > k ? key : k;
+  }
+  auto s = __builtin_amdgcn_permlane16_swap(key, key, false, false);
+  key = s[0] > s[1] ? s[0] : s[1];
+  s = __builtin_amdgcn_permlane32_swap(key, key, false, false);
+  key = Quad<X>::bf_keys(s[0] > s[1] ? s[0] : s[1]) & 0xffffu;
+  const uint32_t e = scale_bytes(key) & 0xffffu;
+  byte = (int)(key >= NAN_KEY ? 255u : e);
+  v8i q;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) q[i] = key >= NAN_KEY ? 0x7f7f7f7f : (int)v[i].row_codes(scale_up(e));
+  return q;
+}
+__device__ __forceinline__ v8i code_block(const uint8_t* q) {
+  const v4i a = *reinterpret_cast<const v4i*>(q), b = *reinterpret_cast<const v4i*>(q + 16);
+  return v8i{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+}
+
+// X: the raw rows' type, or void: codes.  MT: 16 MT >= M.
+template <class T, class X, int MT>
+__global__ __launch_bounds__(64 * ROW_WAVES) void fp8_rows_kernel(Fp8GemmParams p, const void* x, int64_t ldx) {
+  __shared__ float sum[ROW_WAVES][MT][256];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, g = lane >> 4;
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const int64_t n = n0 + r < p.N ? n0 + r : p.N - 1;
+  const int64_t pitch = fp8_pitch(p.K);
+  const int nk = (int)fp8_blocks(p.K);
+  const uint8_t* const w = p.B + n * pitch + 32 * g;
+  v4f acc[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) acc[m] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  // the weights two turns ahead
+  v8i b0{}, b1{};
+  int s0 = 127, s1 = 127;
+  auto weights = [&](int k, v8i& b, int& sb) __attribute__((always_inline)) {
+    if (k >= nk) return;
+    b = code_block(w + (int64_t)k * FP8_BLOCK);
+    sb = p.eB[((int64_t)(k >> 2) * p.N + n) * 4 + (k & 3)];
+  };
+  weights(wave, b0, s0);
+  weights(wave + ROW_WAVES, b1, s1);
+  for (int k = wave; k < nk; k += ROW_WAVES) {
+    const v8i b = b0;
+    const int sb = s0;
+    b0 = b1;
+    s0 = s1;
+    weights(k + 2 * ROW_WAVES, b1, s1);
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      const int64_t row = 16 * m + r;
+      v8i a{0, 0, 0, 0, 0, 0, 0, 0};
+      int sa = 127;
+      if constexpr (std::is_void<X>::value) {
+        if (row < p.M) {
+          a = code_block(p.A + row * pitch + (int64_t)k * FP8_BLOCK + 32 * g);
+          sa = p.eA[((int64_t)(k >> 2) * p.M + row) * 4 + (k & 3)];
+        }
+      } else {
+        const int64_t at = (int64_t)k * FP8_BLOCK + 32 * g;
+        a = row_block(static_cast<const X*>(x) + (row < p.M ? row : 0) * ldx + at, row < p.M ? p.K - at : 0, sa);
+      }
+      if constexpr (sizeof(T) == 2) {
+        acc[m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, acc[m], 0, 0, 0, sb, 0, sa);
+      } else {
+        const float fa = scale_of(sa, 0), fb = scale_of(sb, 0);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(b[2 * q], b[2 * q + 1], fb),
+                                                           widen(a[2 * q], a[2 * q + 1], fa), acc[m], 0, 0, 0);
+      }
+    }
+  }
+  // lane: output columns n0 + 4 g .., row r
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[wave][m][r * 16 + 4 * g + i] = acc[m][i];
+  __syncthreads();
+  for (int i = threadIdx.x; i < MT * 256; i += 64 * ROW_WAVES) {
+    const int64_t row = i >> 4, col = n0 + (i & 15);
+    if (row >= p.M || col >= p.N) continue;
+    float o = 0.0f;
+#pragma unroll
+    for (int v = 0; v < ROW_WAVES; ++v) o += sum[v][i >> 8][i & 255];
+    if (p.relu) o = o < 0.0f ? 0.0f : o;
+    if (p.mask) o = (float)static_cast<const T*>(p.mask)[row * p.ldmask + col] > 0.0f ? o : 0.0f;
+    static_cast<T*>(p.C)[row * p.ldc + col] = (T)o;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// launches
+// ---------------------------------------------------------------------------
+using MidTile = PipeTile<256, 128, 64, 64, 1, 3>;
+using SmallTile = PipeTile<128, 128, 64, 64, 2, 4>;
+
+static int64_t tiles_of(int64_t M, int64_t N, int64_t bm, int64_t bn) {
+  return ((M + bm - 1) / bm) * ((N + bn - 1) / bn);
+}
+
+// Which tile, and for small tiles into how many parts along K the product is
+// split: the least estimated time of turns x (stages x c + t0), turns the
+// tiles (times parts) over 256 units of one block each, plus the pass that adds
+// the parts.  Measured on one product a turn (us a stage of 128, 16-bit /
+// float32 outputs): small 0.53 / 0.94 (4096 x 1024 x 8192), mid 1.05 / 1.77
+// (8192 x 1024 x 4096), large 1.85 / 3.3 (4096 x 4096 x 4096).
+struct Plan {
+  enum Tile { SMALL, MID, LARGE } tile;
+  int splits, chunk;  // parts along K, stages of each
+};
+static Plan plan_of(int64_t M, int64_t N, int64_t K, bool wide) {
+  const int64_t nk = fp8_blocks(K);
+  const double c[3] = {wide ? 0.94 : 0.53, wide ? 1.77 : 1.05, wide ? 3.3 : 1.85}, t0[3] = {4.0, 5.0, 8.0};
+  auto turns = [](int64_t blocks) { return (double)((blocks + 255) / 256); };
+  const int64_t small = tiles_of(M, N, SmallTile::BM, SmallTile::BN);
+  Plan best{Plan::LARGE, 1, (int)nk};
+  double least = turns(tiles_of(M, N, LargeTile::BM, LargeTile::BN)) * ((double)nk * c[2] + t0[2]);
+  const double mid = turns(tiles_of(M, N, MidTile::BM, MidTile::BN)) * ((double)nk * c[1] + t0[1]);
+  if (mid < least) {
+    least = mid;
+    best.tile = Plan::MID;
+  }
+  for (int s : {1, 2, 3, 4, 6, 8, 12, 16}) {
+    const int64_t chunk = (nk + s - 1) / s, parts = (nk + chunk - 1) / chunk;
+    if (parts != s) continue;
+    double t = turns(small * s) * ((double)chunk * c[0] + t0[0]);
+    if (s > 1) t += 4.0 + (double)(M * N) * 8.0 * s / 4.0e6;  // written and read at about 4 TB/s
+    if (t < least) {
+      least = t;
+      best = Plan{Plan::SMALL, s, (int)chunk};
+    }
+  }
+  return best;
+}
+
+// Up to 64 rows stream the weights (fp8_rows_kernel); up to 16 also quantize them there.
+constexpr int64_t ROWS_MAX = 64, ROWS_RAW_MAX = 16;
+bool fp8_rows_raw(int64_t M) { return M <= ROWS_RAW_MAX; }
+
+int64_t fp8_gemm_partials(int64_t M, int64_t N, int64_t K) {
+  if (M <= ROWS_MAX) return 0;
+  int64_t s = 0;
+  for (bool wide : {false, true}) {
+    const Plan p = plan_of(M, N, K, wide);
+    if (p.splits > 1 && p.splits > s) s = p.splits;
+  }
+  return s * M * N;
+}
+
+hipError_t launch_fp8_rows(fqt_dtype type, const Fp8GemmParams& p, const void* x, int64_t ldx, hipStream_t s) {
+  return with_type(type, [&](auto e) {
+    using T = decltype(e);
+    const int64_t blocks = (p.N + 15) / 16;
+    if (blocks > 0x7FFFFFFF || p.M > (x ? ROWS_RAW_MAX : ROWS_MAX)) return hipErrorInvalidValue;
+    auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * ROW_WAVES), 0, s, p, x, ldx);
+      return hipGetLastError();
+    };
+    if (x) return go(fp8_rows_kernel<T, T, 1>);
+    if (p.M <= 16) return go(fp8_rows_kernel<T, void, 1>);
+    return p.M <= 32 ? go(fp8_rows_kernel<T, void, 2>) : go(fp8_rows_kernel<T, void, 4>);
+  });
 }
 
 hipError_t launch_fp8_gemm(fqt_dtype type, const Fp8GemmParams& p, hipStream_t s) {
+  if (p.M <= ROWS_MAX) return launch_fp8_rows(type, p, nullptr, 0, s);
   return with_type(type, [&](auto e) {
     using T = decltype(e);
-    auto go = [&](auto c) {
+    constexpr bool WIDE = sizeof(T) == 4;
+    // whole lines of outputs go past the caches (8192 x 4096 x 1024, bfloat16:
+    // 46.8 us ordinary, 43.5 nontemporal; float32: 76.8, 72.0)
+    const bool nt = (p.ldc * sizeof(T)) % 128 == 0 && ((uintptr_t)p.C & 127) == 0;
+    const Plan plan = plan_of(p.M, p.N, p.K, WIDE);
+    auto tiles = [&](auto c) {
       using C = decltype(c);
-      const int64_t tiles = tiles_of<C>(p.M, p.N);
-      if (tiles > 0x3FFFFFFF) return hipErrorInvalidValue;
-      // whole lines of outputs go past the caches (8192 x 4096 x 1024, bfloat16:
-      // 46.8 us ordinary, 43.5 nontemporal; float32: 76.8, 72.0)
-      const bool nt = (p.ldc * sizeof(T)) % 128 == 0 && ((uintptr_t)p.C & 127) == 0;
-      if (nt)
-        hipLaunchKernelGGL((fp8_gemm_kernel<T, C, true>), dim3((unsigned)tiles), dim3(C::THREADS), 0, s, p);
-      else
-        hipLaunchKernelGGL((fp8_gemm_kernel<T, C, false>), dim3((unsigned)tiles), dim3(C::THREADS), 0, s, p);
+      return tiles_of(p.M, p.N, C::BM, C::BN);
+    };
+    const int64_t blocks = plan.tile == Plan::LARGE ? tiles(LargeTile{}) : plan.tile == Plan::MID ? tiles(MidTile{}) : tiles(SmallTile{});
+    if (blocks > 0x3FFFFFFF) return hipErrorInvalidValue;
+    auto go = [&](auto kernel, auto... more) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)blocks, (unsigned)plan.splits), dim3(512), 0, s, p, more...);
       return hipGetLastError();
     };
-    if (tiles_of<Fp8Large>(p.M, p.N) >= 256) return go(Fp8Large{});
-    return tiles_of<Fp8Mid>(p.M, p.N) >= 256 ? go(Fp8Mid{}) : go(Fp8Small{});
+    if (plan.tile == Plan::LARGE) return nt ? go(fp8_gemm_large_kernel<T, WIDE, true>) : go(fp8_gemm_large_kernel<T, WIDE, false>);
+    if (plan.tile == Plan::MID)
+      return nt ? go(fp8_gemm_pipe_kernel<T, MidTile, WIDE, false, true>, plan.chunk)
+                : go(fp8_gemm_pipe_kernel<T, MidTile, WIDE, false, false>, plan.chunk);
+    if (plan.splits == 1)
+      return nt ? go(fp8_gemm_pipe_kernel<T, SmallTile, WIDE, false, true>, plan.chunk)
+                : go(fp8_gemm_pipe_kernel<T, SmallTile, WIDE, false, false>, plan.chunk);
+    const hipError_t err = go(fp8_gemm_pipe_kernel<float, SmallTile, WIDE, true, false>, plan.chunk);
+    if (err != hipSuccess) return err;
+    const int64_t quads = p.M * ((p.N + 3) / 4);
+    hipLaunchKernelGGL((fp8_split_sum_kernel<T>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, s, p, plan.splits);
+    return hipGetLastError();
   });
 }
 

@@ -171,6 +171,9 @@ struct Fp8GemmParams {
   int64_t ldmask;
   float* part;        // split-K partial sums [splits][M][N]
 };
+// Raw rows X [M, K] of C's type against B (A is not read), if fp8_rows_raw(M).
+bool fp8_rows_raw(int64_t M);
+hipError_t launch_fp8_rows(fqt_dtype type, const Fp8GemmParams& p, const void* x, int64_t ldx, hipStream_t s);
 int64_t fp8_gemm_partials(int64_t M, int64_t N, int64_t K);  // floats
 hipError_t launch_fp8_gemm(fqt_dtype type, const Fp8GemmParams& p, hipStream_t s);
 

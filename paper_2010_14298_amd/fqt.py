@@ -8,6 +8,7 @@ fallback: if the library is not built or cannot load, every call raises.
 """
 import array
 import ctypes
+import operator
 import os
 
 import torch
@@ -455,44 +456,60 @@ FQT_F32, FQT_BF16, FQT_F16 = 0, 1, 2
 TYPES = {torch.float32: FQT_F32, torch.bfloat16: FQT_BF16, torch.float16: FQT_F16}
 
 
-def _here(t, name):
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+def _device():
+    """Index of the current device.  This and _raw_stream are what torch.cuda.current_device and current_stream come
+    down to, without building objects: a single token's calls are short enough to notice."""
+    return torch._C._cuda_getDevice()
+
+
+def _raw_stream(dev):
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
+def _here(t, name, dev):
+    if t.get_device() != dev:
         raise ValueError(f"{name} must be on the current CUDA device")
     return t
 
 
-def _matrix(x, name, shape=None, dtype=None):
+def _matrix(x, name, dev, shape=None, dtype=None):
     """(pointer, type, rows, cols, row pitch) of a 2-d activation tensor."""
-    if x.dim() != 2 or x.dtype not in TYPES or (dtype is not None and x.dtype != dtype):
+    dt = TYPES.get(x.dtype)
+    if dt is None or x.dim() != 2 or (dtype is not None and x.dtype != dtype):
         raise ValueError(f"{name} must be a 2-d float32, bfloat16 or float16 tensor of the call's type")
     if shape is not None and x.shape != shape:
         raise ValueError(f"{name} has shape {tuple(x.shape)}, not {tuple(shape)}")
+    if x.get_device() != dev:
+        raise ValueError(f"{name} must be on the current CUDA device")
     rows, cols = x.shape
     ld, step = x.stride()
     if step != 1 and cols != 1:
         raise ValueError(f"{name} must have unit column stride")
-    return _here(x, name).data_ptr(), TYPES[x.dtype], rows, cols, ld if rows > 1 else max(ld, cols)
+    return x.data_ptr(), dt, rows, cols, ld if rows > 1 else max(ld, cols)
 
 
-def _vector(x, name, n):
+def _vector(x, name, n, dev):
     """Pointer of a contiguous float32 [n] tensor (None: NULL)."""
     if x is None:
         return None
-    if x.dtype != torch.float32 or x.shape != (n,) or not x.is_contiguous():
+    if x.dtype != torch.float32 or x.dim() != 1 or x.shape[0] != n or not x.is_contiguous():
         raise ValueError(f"{name} must be a contiguous float32 tensor of {n} elements")
-    return _here(x, name).data_ptr()
+    if x.get_device() != dev:
+        raise ValueError(f"{name} must be on the current CUDA device")
+    return x.data_ptr()
 
 
 def fqt_layernorm_forward(X, gamma=None, beta=None, eps=1e-5, Y=None):
     """Layer norm over the columns of X [rows, cols]; returns (Y, mean, rstd)."""
-    px, dt, rows, cols, ldx = _matrix(X, "X")
+    dev = _device()
+    px, dt, rows, cols, ldx = _matrix(X, "X", dev)
     if Y is None:
-        Y = torch.empty((rows, cols), dtype=X.dtype, device=X.device)
-    py, _, _, _, ldy = _matrix(Y, "Y", X.shape, X.dtype)
-    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=X.device).unbind(0)
-    rc = load().fqt_layernorm_forward(px, dt, rows, cols, ldx, _vector(gamma, "gamma", cols),
-                                      _vector(beta, "beta", cols), eps, py, ldy, mean.data_ptr(), rstd.data_ptr(),
-                                      _stream())
+        Y = X.new_empty((rows, cols))
+    py, _, _, _, ldy = _matrix(Y, "Y", dev, X.shape, X.dtype)
+    mean, rstd = X.new_empty((2, rows), dtype=torch.float32).unbind(0)
+    rc = load().fqt_layernorm_forward(px, dt, rows, cols, ldx, _vector(gamma, "gamma", cols, dev),
+                                      _vector(beta, "beta", cols, dev), eps, py, ldy, mean.data_ptr(), rstd.data_ptr(),
+                                      _raw_stream(dev))
     _check("fqt_layernorm_forward", rc)
     return Y, mean, rstd
 
@@ -504,21 +521,22 @@ def fqt_layernorm_backward_workspace(rows, cols):
 def fqt_layernorm_backward(G, X, mean, rstd, gamma=None, grad_X=None, params=True, ws=None):
     """Gradient of fqt_layernorm_forward; returns (grad_X, grad_gamma, grad_beta, ws).  params=False forms grad_X
     only (the others are None)."""
-    pg, dt, rows, cols, ldg = _matrix(G, "G")
-    px, _, _, _, ldx = _matrix(X, "X", G.shape, G.dtype)
+    dev = _device()
+    pg, dt, rows, cols, ldg = _matrix(G, "G", dev)
+    px, _, _, _, ldx = _matrix(X, "X", dev, G.shape, G.dtype)
     if grad_X is None:
         grad_X = torch.empty((rows, cols), dtype=G.dtype, device=G.device)
-    py, _, _, _, ldgx = _matrix(grad_X, "grad_X", G.shape, G.dtype)
+    py, _, _, _, ldgx = _matrix(grad_X, "grad_X", dev, G.shape, G.dtype)
     gg = gb = None
     if params:
-        gg, gb = torch.empty((2, cols), dtype=torch.float32, device=G.device).unbind(0)
+        gg, gb = G.new_empty((2, cols), dtype=torch.float32).unbind(0)
         if ws is None:
             ws = _workspace(fqt_layernorm_backward_workspace(rows, cols), G.device)
-    rc = load().fqt_layernorm_backward(pg, ldg, px, ldx, dt, rows, cols, _vector(mean, "mean", rows),
-                                       _vector(rstd, "rstd", rows), _vector(gamma, "gamma", cols), py, ldgx,
-                                       _vector(gg, "grad_gamma", cols), _vector(gb, "grad_beta", cols),
+    rc = load().fqt_layernorm_backward(pg, ldg, px, ldx, dt, rows, cols, _vector(mean, "mean", rows, dev),
+                                       _vector(rstd, "rstd", rows, dev), _vector(gamma, "gamma", cols, dev), py, ldgx,
+                                       _vector(gg, "grad_gamma", cols, dev), _vector(gb, "grad_beta", cols, dev),
                                        ws.data_ptr() if ws is not None else None, ws.numel() if ws is not None else 0,
-                                       _stream())
+                                       _raw_stream(dev))
     _check("fqt_layernorm_backward", rc)
     return grad_X, gg, gb, ws
 
@@ -532,7 +550,7 @@ def fp8_operand(rows, K, device):
                 exp=torch.empty(((blocks + 3) // 4, rows, 4), dtype=torch.uint8, device=device), K=K)
 
 
-def _fp8(a, name, rows=None, K=None):
+def _fp8(a, name, dev, rows=None, K=None):
     """The C struct of an operand (None: NULL), checked against the rows and K that the call needs."""
     if a is None:
         return None
@@ -546,17 +564,17 @@ def _fp8(a, name, rows=None, K=None):
     k_major = not q.is_contiguous()
     if k_major and not q.t().is_contiguous():
         raise ValueError(f"{name}: codes must be contiguous by row or by column")
-    _here(e, name)
-    return Fp8(_here(q, name).data_ptr(), e.data_ptr(), int(k_major))
+    return Fp8(_here(q, name, dev).data_ptr(), _here(e, name, dev).data_ptr(), int(k_major))
 
 
 def fqt_fp8_quantize(x, tile=False, by_row=True, by_col=False, stochastic=False, seed=0):
     """Operands of x [rows, cols]: (x [rows, K = cols] or None, x^T [cols, K = rows] or None), from one read."""
-    px, dt, rows, cols, ldx = _matrix(x, "x")
+    dev = _device()
+    px, dt, rows, cols, ldx = _matrix(x, "x", dev)
     a = fp8_operand(rows, cols, x.device) if by_row else None
     b = fp8_operand(cols, rows, x.device) if by_col else None
     rc = load().fqt_fp8_quantize(px, dt, rows, cols, ldx, int(bool(tile)), int(bool(stochastic)), seed,
-                                 _fp8(a, "by_row"), _fp8(b, "by_col"), _stream())
+                                 _fp8(a, "by_row", dev), _fp8(b, "by_col", dev), _raw_stream(dev))
     _check("fqt_fp8_quantize", rc)
     return a, b
 
@@ -568,15 +586,16 @@ def fqt_fp8_gemm_workspace(M, N, K):
 def fqt_fp8_gemm(A, B, dtype=torch.float32, relu=False, mask=None, C=None, ws=None):
     """C [M, N] = A [M, K] B [N, K]^T of two operands; relu: max(C, 0); mask: zero where mask <= 0.
     Returns (C, ws)."""
+    dev = _device()
     M, N, K = A["q"].shape[0], B["q"].shape[0], A["K"]
     if C is None:
         C = torch.empty((M, N), dtype=dtype, device=A["q"].device)
-    pc, dt, _, _, ldc = _matrix(C, "C", (M, N))
-    pm, _, _, _, ldm = _matrix(mask, "mask", (M, N), C.dtype) if mask is not None else (None,) * 4 + (0,)
+    pc, dt, _, _, ldc = _matrix(C, "C", dev, (M, N))
+    pm, _, _, _, ldm = _matrix(mask, "mask", dev, (M, N), C.dtype) if mask is not None else (None,) * 4 + (0,)
     if ws is None:
         ws = _workspace(fqt_fp8_gemm_workspace(M, N, K), C.device)
-    rc = load().fqt_fp8_gemm(_fp8(A, "A"), _fp8(B, "B", N, K), M, N, K, dt, int(bool(relu)), pm, ldm, pc, ldc,
-                             ws.data_ptr(), ws.numel(), _stream())
+    rc = load().fqt_fp8_gemm(_fp8(A, "A", dev), _fp8(B, "B", dev, N, K), M, N, K, dt, int(bool(relu)), pm, ldm, pc, ldc,
+                             ws.data_ptr(), ws.numel(), _raw_stream(dev))
     _check("fqt_fp8_gemm", rc)
     return C, ws
 
@@ -588,17 +607,18 @@ def fqt_fp8_linear_forward_workspace(N, d_in, d_out):
 def fqt_fp8_linear_forward(X, W8, relu=False, save=True, Y=None, ws=None):
     """Y = Q(X) W8^T (then max(., 0) when relu), W8 the weights' by_row operand (tile=True).  save: also the operand
     of X^T that the backward reads.  Returns (Y, X8t or None, ws)."""
-    px, dt, N, d_in, ldx = _matrix(X, "X")
+    dev = _device()
+    px, dt, N, d_in, ldx = _matrix(X, "X", dev)
     d_out = W8["q"].shape[0]
-    w8 = _fp8(W8, "W8", d_out, d_in)
+    w8 = _fp8(W8, "W8", dev, d_out, d_in)
     if Y is None:
-        Y = torch.empty((N, d_out), dtype=X.dtype, device=X.device)
-    py, _, _, _, ldy = _matrix(Y, "Y", (N, d_out), X.dtype)
+        Y = X.new_empty((N, d_out))
+    py, _, _, _, ldy = _matrix(Y, "Y", dev, (N, d_out), X.dtype)
     X8t = fp8_operand(d_in, N, X.device) if save else None
     if ws is None:
         ws = _workspace(fqt_fp8_linear_forward_workspace(N, d_in, d_out), X.device)
-    rc = load().fqt_fp8_linear_forward(px, dt, N, d_in, ldx, w8, d_out, int(bool(relu)), py, ldy, _fp8(X8t, "X8t"),
-                                       ws.data_ptr(), ws.numel(), _stream())
+    rc = load().fqt_fp8_linear_forward(px, dt, N, d_in, ldx, w8, d_out, int(bool(relu)), py, ldy, _fp8(X8t, "X8t", dev),
+                                       ws.data_ptr(), ws.numel(), _raw_stream(dev))
     _check("fqt_fp8_linear_forward", rc)
     return Y, X8t, ws
 
@@ -611,10 +631,11 @@ def fqt_fp8_linear_backward(G, X8t, W8t, seed=0, stochastic=True, relu_input=Non
                             grad_X=None, ws=None):
     """grad_W = Q_b1(G)^T X8t^T (float32) and grad_X = Q_b2(G) W8t^T (G's type; zero where relu_input <= 0).
     input_grad=False forms grad_W only (grad_X is None; W8t may be None).  Returns (grad_W, grad_X, ws)."""
-    pg, dt, N, d_out, ldg = _matrix(G, "G")
+    dev = _device()
+    pg, dt, N, d_out, ldg = _matrix(G, "G", dev)
     d_in = X8t["q"].shape[0]
-    x8t = _fp8(X8t, "X8t", d_in, N)
-    w8t = _fp8(W8t, "W8t", d_in, d_out)
+    x8t = _fp8(X8t, "X8t", dev, d_in, N)
+    w8t = _fp8(W8t, "W8t", dev, d_in, d_out)
     if grad_W is None:
         grad_W = torch.empty((d_out, d_in), dtype=torch.float32, device=G.device)
     if (grad_W.dtype != torch.float32 or grad_W.shape != (d_out, d_in) or not grad_W.is_contiguous()):
@@ -625,15 +646,15 @@ def fqt_fp8_linear_backward(G, X8t, W8t, seed=0, stochastic=True, relu_input=Non
     else:
         if grad_X is None:
             grad_X = torch.empty((N, d_in), dtype=G.dtype, device=G.device)
-        px, _, _, _, ldgx = _matrix(grad_X, "grad_X", (N, d_in), G.dtype)
+        px, _, _, _, ldgx = _matrix(grad_X, "grad_X", dev, (N, d_in), G.dtype)
     pr, ldr = None, 0
     if relu_input is not None:
-        pr, _, _, _, ldr = _matrix(relu_input, "relu_input", (N, d_in), G.dtype)
+        pr, _, _, _, ldr = _matrix(relu_input, "relu_input", dev, (N, d_in), G.dtype)
     if ws is None:
         ws = _workspace(fqt_fp8_linear_backward_workspace(N, d_in, d_out), G.device)
     rc = load().fqt_fp8_linear_backward(pg, dt, N, d_out, ldg, x8t, w8t, d_in, int(bool(stochastic)), seed, pr, ldr,
-                                        _here(grad_W, "grad_W").data_ptr(), px, ldgx, ws.data_ptr(), ws.numel(),
-                                        _stream())
+                                        _here(grad_W, "grad_W", dev).data_ptr(), px, ldgx, ws.data_ptr(), ws.numel(),
+                                        _raw_stream(dev))
     _check("fqt_fp8_linear_backward", rc)
     return grad_W, grad_X, ws
 
@@ -642,27 +663,35 @@ def fqt_grad_norm_clip_workspace(count):
     return load().fqt_grad_norm_clip_workspace(count)
 
 
+def _flat_tensors(tensors, dev):
+    """(sizes, types, pointers) arrays of contiguous tensors on the device.  Mapped methods: a model has hundreds."""
+    t = torch.Tensor
+    if set(map(t.get_device, tensors)) - {dev} or not all(map(t.is_contiguous, tensors)):
+        raise ValueError("gradients must be contiguous tensors on the current CUDA device")
+    try:
+        types = array.array("i", map(TYPES.__getitem__, map(operator.attrgetter("dtype"), tensors)))
+    except KeyError:
+        raise ValueError("gradients must be float32, bfloat16 or float16") from None
+    return array.array("q", map(t.numel, tensors)), types, array.array("Q", map(t.data_ptr, tensors))
+
+
 def fqt_grad_norm_clip(grads, max_norm, outs=None, ws=None):
     """Global norm of the tensors in grads; each is scaled by max_norm / norm where norm > max_norm, in place or
     into outs.  Returns (norm, ws); norm is a float32 device scalar."""
+    dev = _device()
     count = len(grads)
-    dev = torch.cuda.current_device()
-    for t in grads if outs is None else [*grads, *outs]:
-        if t.get_device() != dev or t.dtype not in TYPES or not t.is_contiguous():
-            raise ValueError("gradients must be contiguous float32, bfloat16 or float16 tensors on the current device")
-    sizes = [t.numel() for t in grads]
-    types = [TYPES[t.dtype] for t in grads]
-    if outs is not None and ([t.numel() for t in outs] != sizes or [TYPES[t.dtype] for t in outs] != types):
-        raise ValueError("outs must match grads in number, size and type")
-    g = array.array("Q", [t.data_ptr() for t in grads])
-    o = array.array("Q", [t.data_ptr() for t in outs]) if outs is not None else None
-    n, ty = array.array("q", sizes), array.array("i", types)
-    norm = torch.empty((), dtype=torch.float32, device=dev)
+    n, ty, g = _flat_tensors(grads, dev)
+    o = None
+    if outs is not None:
+        out_n, out_ty, o = _flat_tensors(outs, dev)
+        if out_n.tobytes() != n.tobytes() or out_ty.tobytes() != ty.tobytes():
+            raise ValueError("outs must match grads in number, size and type")
+    norm = torch.empty((), dtype=torch.float32, device=torch.device("cuda", dev))
     if ws is None:
         ws = _workspace(fqt_grad_norm_clip_workspace(count), norm.device)
     rc = load().fqt_grad_norm_clip(g.buffer_info()[0], o.buffer_info()[0] if o is not None else None,
                                    n.buffer_info()[0], ty.buffer_info()[0], count, max_norm, norm.data_ptr(),
-                                   ws.data_ptr(), ws.numel(), _stream())
+                                   ws.data_ptr(), ws.numel(), _raw_stream(dev))
     _check("fqt_grad_norm_clip", rc)
     return norm, ws
 

@@ -66,19 +66,22 @@ def test_fp8_arguments(lib):
                 dict(mask=FAKE + 1), dict(C=None), dict(ldc=7)):
         assert gemm(**bad) == 1, bad
 
+    # longer contractions than a tile's offsets reach
+    assert gemm(K=(1 << 23) + 1) == 2
+
     def fwd(X=FAKE, t=0, N=4, i=8, ldx=8, W=op(), o=8, relu=0, Y=FAKE, ldy=8, Xt=None, ws=FAKE, n=WS):
         return lib.fqt_fp8_linear_forward(X, t, N, i, ldx, W, o, relu, Y, ldy, Xt, ws, n, None)
     for bad in (dict(X=None), dict(W=None), dict(N=0), dict(o=0), dict(relu=3), dict(Y=None), dict(ldy=7),
                 dict(Xt=op(None)), dict(Xt=op(FAKE, FAKE, 1)), dict(t=9)):
         assert fwd(**bad) == 1, bad
-    assert fwd(ws=None) == 4 and fwd(n=64) == 4
+    assert fwd(ws=None) == 4 and fwd(n=64) == 4 and fwd(i=(1 << 23) + 1) == 2
 
     def bwd(G=FAKE, t=0, N=4, o=8, X=op(), W=op(), i=8, sr=1, r=None, gw=FAKE, gx=FAKE, ldgx=8, ws=FAKE, n=WS):
         return lib.fqt_fp8_linear_backward(G, t, N, o, 8, X, W, i, sr, 0, r, 8, gw, gx, ldgx, ws, n, None)
     for bad in (dict(G=None), dict(gw=None, gx=None), dict(X=None), dict(W=None), dict(sr=2), dict(r=FAKE + 1),
                 dict(ldgx=7), dict(i=0)):
         assert bwd(**bad) == 1, bad
-    assert bwd(ws=None) == 4 and bwd(n=64) == 4
+    assert bwd(ws=None) == 4 and bwd(n=64) == 4 and bwd(N=(1 << 23) + 1) == 2
     # what is not formed needs no operand: the next check fails, the workspace's
     assert bwd(gw=None, X=None, n=64) == 4 and bwd(gx=None, W=None, n=64) == 4
 

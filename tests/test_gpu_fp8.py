@@ -187,6 +187,31 @@ def test_product_is_exact_on_small_integers():
         np.testing.assert_array_equal(host(f.fqt_fp8_gemm(A, B)[0]), (x @ w.T).astype(np.float64))
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M,N,K", [(8185, 1022, 200), (8200, 1000, 1500), (3900, 4000, 130), (3870, 4090, 1100),
+                                   (2048, 2048, 640), (1000, 700, 5000), (65, 129, 9000), (4000, 64, 2000)])
+def test_product_of_every_tile(M, N, K, dtype):
+    """Sizes that take the middle and large tiles, many stages, and products split along K: float64 on the device
+    from the decoded operands; a ReLU and a mask; outputs off whole lines of memory and on them."""
+    f = fqt()
+    A = f.fqt_fp8_quantize(heavy(M, M, K, spread=1.0))[0]
+    B = f.fqt_fp8_quantize(heavy(N + 1, N, K, spread=0.2), tile=True)[0]
+
+    def value(a):
+        e = a["exp"].transpose(0, 1).reshape(a["q"].shape[0], -1)[:, :a["q"].shape[1] // 128].double() - 127
+        return (a["q"].double().view(a["q"].shape[0], -1, 128) * torch.exp2(e)[:, :, None]).flatten(1)
+    a, b = value(A), value(B)
+    want, size = a @ b.t().contiguous(), a.abs() @ b.abs().t().contiguous()
+    drop = 2.0 ** -12 if dtype != torch.float32 else 0.0
+    tol = (K * 2.0 ** -24 + drop) * size + HALF[dtype] * want.abs()
+    C, _ = f.fqt_fp8_gemm(A, B, dtype=dtype)
+    assert ((C.double() - want).abs() <= tol).all()
+    wide = torch.empty((M, (N + 127) // 128 * 128), dtype=dtype, device="cuda")
+    mask = torch.randn((M, N), device="cuda").to(dtype)
+    R, _ = f.fqt_fp8_gemm(A, B, C=wide[:, :N], relu=True, mask=mask)
+    assert torch.equal(R, torch.where(mask > 0, C.clamp(min=0), torch.zeros((), dtype=dtype, device="cuda")))
+
+
 def test_nan_blocks_reach_their_outputs_only():
     f = fqt()
     for M, N, K in ((4, 40, 700), (150, 140, 700)):

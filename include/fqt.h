@@ -439,8 +439,7 @@ size_t fqt_fp8_linear_backward_workspace(int64_t N, int64_t d_in, int64_t d_out)
  * place, and nothing is written where nothing is clipped.  norm (device, may
  * be NULL) receives n.  Squares are summed in float64 in a fixed order.  A
  * norm that is not finite scales nothing.  max_norm > 0 (infinity: only the
- * norm).  Calls whose table of sizes passes 2^31 chunks of 16384 elements in 96
- * tensors return FQT_EUNSUPPORTED.                                         */
+ * norm).  168 tensors in a row of more than 2^45 bytes return FQT_EUNSUPPORTED. */
 fqt_status fqt_grad_norm_clip(const void* const* grads, void* const* outs, const int64_t* sizes, const int32_t* types,
                               int64_t count, double max_norm, float* norm, void* ws, size_t ws_bytes, fqt_stream_t s);
 size_t fqt_grad_norm_clip_workspace(int64_t count);

@@ -377,31 +377,40 @@ fqt_status fqt_grad_norm_clip(const void* const* grads, void* const* outs, const
   }
   if (!ws || !aligned(ws, 16) || ws_bytes < fqt_grad_norm_clip_workspace(count)) return FQT_EWORKSPACE;
   double* part = static_cast<double*>(ws);
-  const int64_t launches = (count + CLIP_TENSORS - 1) / CLIP_TENSORS;
-  auto table = [&](int64_t l, ClipTable& t) {
+  // tables of up to CLIP_TENSORS tensors that are not empty; next: where the following one begins
+  auto table = [&](int64_t& next, ClipTable& t) {
     t.count = 0;
     uint64_t chunks = 0;
-    for (int64_t i = l * CLIP_TENSORS; i < count && i < (l + 1) * CLIP_TENSORS; ++i) {
+    for (; next < count && t.count < CLIP_TENSORS; ++next) {
+      if (sizes[next] == 0) continue;
       const int k = t.count++;
-      t.g[k] = grads[i];
-      t.out[k] = outs ? outs[i] : const_cast<void*>(grads[i]);
-      t.n[k] = sizes[i];
-      t.type[k] = (uint8_t)types[i];
+      const uint64_t bytes = (uint64_t)sizes[next] * type_bytes((fqt_dtype)types[next]);
+      const uint64_t n = (bytes + CLIP_BYTES - 1) / CLIP_BYTES;
+      t.g[k] = grads[next];
+      t.out[k] = outs ? outs[next] : const_cast<void*>(grads[next]);
+      t.type[k] = (uint8_t)types[next];
+      t.tail[k] = (uint16_t)(bytes - (n - 1) * CLIP_BYTES);
       t.first[k] = (uint32_t)chunks;
-      chunks += (uint64_t)clip_chunks(sizes[i]);
+      chunks += n;
+      if (chunks > 0x7FFFFFFFu) return false;
     }
     t.first[t.count] = (uint32_t)chunks;
-    return chunks <= 0x7FFFFFFFu;
+    return true;
   };
   ClipTable t;
-  for (int64_t l = 0; l < launches; ++l)
-    if (!table(l, t)) return FQT_EUNSUPPORTED;
+  int64_t launches = 0, next = 0;
+  while (next < count || launches == 0) {
+    if (!table(next, t)) return FQT_EUNSUPPORTED;
+    ++launches;
+  }
+  next = 0;
   for (int64_t l = 0; l < launches; ++l) {
-    table(l, t);
+    table(next, t);
     FQT_TRY(launch_clip_norm(t, part + l * CLIP_PARTS, s));
   }
+  next = launches == 1 ? count : 0;  // one table serves both
   for (int64_t l = 0; l < launches; ++l) {
-    table(l, t);
+    if (launches > 1) table(next, t);
     FQT_TRY(launch_clip_scale(t, part, launches * CLIP_PARTS, max_norm, l == 0 ? norm : nullptr, s));
   }
   return FQT_OK;

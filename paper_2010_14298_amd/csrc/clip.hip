@@ -5,15 +5,14 @@
 // Squares and sums are float64 (a float32 squared is exact there and cannot
 // overflow), in an order that the sizes alone decide.  Two launches for up
 // to CLIP_TENSORS tensors: partial sums, then every block of the scaling
-// launch adds the partials up for itself and scales its chunks.
+// launch adds the partials up for itself and scales its chunks.  A chunk is
+// four 16-byte loads a thread; turns this small spread tensors of any size
+// evenly over the blocks.
 #include "train_kernels.h"
 
 namespace fqt {
 
 constexpr int CLIP_THREADS = 256;
-constexpr int64_t CLIP_CHUNK = 16384;  // elements of one block's turn
-int64_t clip_chunks(int64_t n) { return (n + CLIP_CHUNK - 1) / CLIP_CHUNK; }
-
 __device__ __forceinline__ double block_sum(double v, double* sh) {
 #pragma unroll
   for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
@@ -25,65 +24,139 @@ __device__ __forceinline__ double block_sum(double v, double* sh) {
   return v;
 }
 
-// The tensor that holds a chunk: the last one whose first chunk is not past it.
-__device__ __forceinline__ int tensor_of(const ClipTable& t, uint32_t chunk) {
-  int lo = 0, hi = t.count;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (t.first[mid] <= chunk)
-      lo = mid;
-    else
-      hi = mid;
-  }
-  return lo;
-}
-
-template <class T>
-__device__ __forceinline__ double chunk_squares(const T* g, int64_t n) {
-  constexpr int V = 16 / (int)sizeof(T);
-  double s = 0.0;
-  for (int64_t i = (int64_t)threadIdx.x * V; i < n; i += CLIP_THREADS * V) {
-    float v[V];
-    load_part<T, V>(g + i, n - i, v);
+// A thread's part of a chunk, as it lies in memory; zeros past the tensor.
+struct Raw {
+  typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(2)));
+  static constexpr int N = (int)CLIP_BYTES / (16 * CLIP_THREADS);
+  u32x4u v[N];
+  __device__ __forceinline__ void load(const char* p, int bytes) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) s = fma((double)v[j], (double)v[j], s);
-  }
-  return s;
-}
-
-template <class T>
-__device__ __forceinline__ void chunk_scale(const T* g, T* out, int64_t n, float c) {
-  constexpr int V = 16 / (int)sizeof(T);
-  for (int64_t i = (int64_t)threadIdx.x * V; i < n; i += CLIP_THREADS * V) {
-    float v[V];
-    load_part<T, V>(g + i, n - i, v);
+    for (int i = 0; i < N; ++i) {
+      const int at = 16 * (i * CLIP_THREADS + (int)threadIdx.x);
+      if (at + 16 <= bytes) {
+        v[i] = *reinterpret_cast<const u32x4u*>(p + at);
+      } else {
+        v[i] = u32x4u{0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int j = 0; j < V; ++j) v[j] *= c;
-    store_part<T, V>(out + i, n - i, v);
+        for (int h = 0; h < 8; ++h)  // elements have two or four bytes
+          if (at + 2 * h < bytes)
+            v[i][h / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + at + 2 * h) << (16 * (h & 1));
+      }
+    }
   }
+  __device__ __forceinline__ void store(char* p, int bytes) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int at = 16 * (i * CLIP_THREADS + (int)threadIdx.x);
+      if (at + 16 <= bytes) {
+        *reinterpret_cast<u32x4u*>(p + at) = v[i];
+      } else {
+#pragma unroll
+        for (int h = 0; h < 8; ++h)
+          if (at + 2 * h < bytes) *reinterpret_cast<uint16_t*>(p + at + 2 * h) = (uint16_t)(v[i][h / 2] >> (16 * (h & 1)));
+      }
+    }
+  }
+  template <class T>
+  __device__ __forceinline__ double squares(double s) const {
+    constexpr int V = 16 / (int)sizeof(T);
+    typedef T vec __attribute__((ext_vector_type(V)));
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const vec x = __builtin_bit_cast(vec, v[i]);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const double d = (double)(float)x[j];
+        s = fma(d, d, s);
+      }
+    }
+    return s;
+  }
+  template <class T>
+  __device__ __forceinline__ void scale(float f) {
+    constexpr int V = 16 / (int)sizeof(T);
+    typedef T vec __attribute__((ext_vector_type(V)));
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      vec x = __builtin_bit_cast(vec, v[i]);
+#pragma unroll
+      for (int j = 0; j < V; ++j) x[j] = (T)((float)x[j] * f);
+      v[i] = __builtin_bit_cast(u32x4u, x);
+    }
+  }
+};
+
+// The table in LDS, in one round of loads.
+__device__ __forceinline__ void table_to_lds(ClipTable& t) {
+  static_assert(sizeof(ClipTable) % 4 == 0, "whole words");
+  const __attribute__((address_space(4))) uint32_t* args =
+      (const __attribute__((address_space(4))) uint32_t*)__builtin_amdgcn_kernarg_segment_ptr();  // the first argument
+  uint32_t* to = reinterpret_cast<uint32_t*>(&t);
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(ClipTable) / 4 + CLIP_THREADS - 1) / CLIP_THREADS; ++i) {
+    const int w = i * CLIP_THREADS + (int)threadIdx.x;
+    if (w < (int)sizeof(ClipTable) / 4) to[w] = args[w];
+  }
+  __syncthreads();
 }
 
-__global__ __launch_bounds__(CLIP_THREADS) void clip_norm_kernel(ClipTable t, double* part) {
+// Where a chunk lies.
+struct Place {
+  const char* g;
+  char* out;
+  int bytes;
+  int type;
+};
+// Its tensor: as many first chunks as are not past it, counted over the lanes
+// (one after the other costs an LDS latency each, 161 tensors 7 us).
+__device__ __forceinline__ Place place_of(const ClipTable& t, uint32_t chunk) {
+  const int lane = threadIdx.x & 63;
+  int k = -1;
+  for (int i = 0; i < t.count; i += 64)
+    k += __popcll(__builtin_amdgcn_ballot_w64(i + lane < t.count && t.first[i + lane] <= chunk));
+  k = __builtin_amdgcn_readfirstlane(k);
+  const int64_t at = (int64_t)(chunk - t.first[k]) * CLIP_BYTES;
+  return Place{static_cast<const char*>(t.g[k]) + at, static_cast<char*>(t.out[k]) + at,
+               chunk + 1 == t.first[k + 1] ? (int)t.tail[k] : (int)CLIP_BYTES, t.type[k]};
+}
+
+__global__ __launch_bounds__(CLIP_THREADS) void clip_norm_kernel(ClipTable, double* part) {
   __shared__ double sh[CLIP_THREADS / 64];
+  __shared__ ClipTable t;
+  table_to_lds(t);
+  const uint32_t chunks = t.first[t.count];
   double s = 0.0;
-  for (uint32_t c = blockIdx.x; c < t.first[t.count]; c += gridDim.x) {
-    const int k = tensor_of(t, c);
-    const int64_t at = (int64_t)(c - t.first[k]) * CLIP_CHUNK;
-    const int64_t n = t.n[k] - at < CLIP_CHUNK ? t.n[k] - at : CLIP_CHUNK;
-    if (t.type[k] == FQT_F32)
-      s += chunk_squares(static_cast<const float*>(t.g[k]) + at, n);
-    else if (t.type[k] == FQT_BF16)
-      s += chunk_squares(static_cast<const __bf16*>(t.g[k]) + at, n);
+  int type = 0;
+  Raw now, next;  // the next turn's loads are on their way while this one's are worked on
+  auto fetch = [&](uint32_t c) __attribute__((always_inline)) {
+    if (c >= chunks) return;
+    const Place at = place_of(t, c);
+    type = at.type;
+    next.load(at.g, at.bytes);
+  };
+  fetch(blockIdx.x);
+  for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
+    now = next;
+    const int what = type;
+    fetch(c + gridDim.x);
+    if (what == FQT_F32)
+      s = now.squares<float>(s);
+    else if (what == FQT_BF16)
+      s = now.squares<__bf16>(s);
     else
-      s += chunk_squares(static_cast<const _Float16*>(t.g[k]) + at, n);
+      s = now.squares<_Float16>(s);
   }
   s = block_sum(s, sh);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
-__global__ __launch_bounds__(CLIP_THREADS) void clip_scale_kernel(ClipTable t, const double* part, int64_t parts,
+// From the last chunk to the first: what the norm read last is still in the
+// caches.
+__global__ __launch_bounds__(CLIP_THREADS) void clip_scale_kernel(ClipTable, const double* part, int64_t parts,
                                                                    double max_norm, float* norm) {
   __shared__ double sh[CLIP_THREADS / 64];
+  __shared__ ClipTable t;
+  table_to_lds(t);
   double s = 0.0;
   for (int64_t i = threadIdx.x; i < parts; i += CLIP_THREADS) s += part[i];
   const double n = sqrt(block_sum(s, sh));
@@ -91,17 +164,20 @@ __global__ __launch_bounds__(CLIP_THREADS) void clip_scale_kernel(ClipTable t, c
   // a norm that is not finite scales nothing: the caller sees it and drops the step
   const bool clip = n > max_norm && n < __builtin_huge_val();
   const float scale = clip ? (float)(max_norm / n) : 1.0f;
-  for (uint32_t c = blockIdx.x; c < t.first[t.count]; c += gridDim.x) {
-    const int k = tensor_of(t, c);
-    if (!clip && t.out[k] == t.g[k]) continue;
-    const int64_t at = (int64_t)(c - t.first[k]) * CLIP_CHUNK;
-    const int64_t len = t.n[k] - at < CLIP_CHUNK ? t.n[k] - at : CLIP_CHUNK;
-    if (t.type[k] == FQT_F32)
-      chunk_scale(static_cast<const float*>(t.g[k]) + at, static_cast<float*>(t.out[k]) + at, len, scale);
-    else if (t.type[k] == FQT_BF16)
-      chunk_scale(static_cast<const __bf16*>(t.g[k]) + at, static_cast<__bf16*>(t.out[k]) + at, len, scale);
+  const uint32_t chunks = t.first[t.count];
+  for (uint32_t i = blockIdx.x; i < chunks; i += gridDim.x) {
+    const uint32_t c = chunks - 1 - i;
+    const Place at = place_of(t, c);
+    if (!clip && at.out == at.g) continue;
+    Raw v;
+    v.load(at.g, at.bytes);
+    if (at.type == FQT_F32)
+      v.scale<float>(scale);
+    else if (at.type == FQT_BF16)
+      v.scale<__bf16>(scale);
     else
-      chunk_scale(static_cast<const _Float16*>(t.g[k]) + at, static_cast<_Float16*>(t.out[k]) + at, len, scale);
+      v.scale<_Float16>(scale);
+    v.store(at.out, at.bytes);
   }
 }
 

@@ -14,22 +14,23 @@ namespace fqt {
 
 // Elements of a row that each thread of a team of TPR threads holds: NV
 // vectors of VEC, vector v at column (v TPR + t) VEC.
-template <int TPR_, int VEC_, int NV_>
+template <int TPR_, int VEC_, int NV_, int THREADS_ = TPR_ < 256 ? 256 : TPR_>
 struct Team {
-  static constexpr int TPR = TPR_, VEC = VEC_, NV = NV_;
-  static constexpr int THREADS = TPR < 256 ? 256 : TPR;
+  static constexpr int TPR = TPR_, VEC = VEC_, NV = NV_, THREADS = THREADS_;
   static constexpr int PER_BLOCK = THREADS / TPR;  // rows at a time
   static constexpr int WAVES = TPR / 64;
   static constexpr int64_t COLS = (int64_t)TPR * VEC * NV;
 };
 
-// Sums of N values over the team, in every thread.
+// Sums of N values over the team, in every thread.  sh: the team's [WAVES][N];
+// teams of several waves meet at block barriers, which every team of the block
+// has to reach.
 template <class C, int N>
 __device__ __forceinline__ void team_sum(float (&v)[N], float (*sh)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
   if constexpr (C::WAVES > 1) {
-    const int wave = threadIdx.x >> 6;
+    const int wave = threadIdx.x % C::TPR >> 6;
     __syncthreads();  // the last sums have been read
     if ((threadIdx.x & 63) == 0) {
 #pragma unroll
@@ -144,53 +145,61 @@ __global__ __launch_bounds__(C::THREADS) void norm_forward_long_kernel(NormParam
   }
 }
 
-// Backward: each team takes every (teams)-th row and keeps its columns' sums
-// of g xh and g in registers; at the end the block adds its teams' sums in
-// order and writes one partial row of each.
+// Backward: one block of 1024 threads a unit, so that there are few partial
+// sums (8192 x 1024 bfloat16: 1024 blocks of four teams left 8 MB of them, 6.9
+// us to add up).  Each team takes every (teams)-th row and keeps its columns'
+// sums of g xh and g in registers; at the end the block's teams meet in LDS
+// pairwise and one writes the block's partial row (an only block writes the
+// parameter gradients themselves).
 template <class T, class C>
 __global__ __launch_bounds__(C::THREADS) void norm_backward_kernel(NormParams p) {
-  __shared__ float sh[C::WAVES][2];
-  __shared__ float col_sum[C::PER_BLOCK > 1 ? 2 * C::COLS : 1];
+  __shared__ float sh[C::PER_BLOCK][C::WAVES][2];
+  __shared__ __attribute__((aligned(16))) float col_sum[C::PER_BLOCK > 1 ? C::PER_BLOCK / 2 : 1][2][C::PER_BLOCK > 1 ? C::COLS : 4];
   const int t = threadIdx.x % C::TPR, team = threadIdx.x / C::TPR;
   const float inv = 1.0f / (float)p.cols;
-  float ga[C::NV][C::VEC], sg[C::NV][C::VEC], sb[C::NV][C::VEC];
+  float sg[C::NV][C::VEC], sb[C::NV][C::VEC];
 #pragma unroll
-  for (int k = 0; k < C::NV; ++k) {
-    const int64_t col = (int64_t)(k * C::TPR + t) * C::VEC;
+  for (int k = 0; k < C::NV; ++k)
 #pragma unroll
-    for (int i = 0; i < C::VEC; ++i) {
-      ga[k][i] = 1.0f;
-      sg[k][i] = sb[k][i] = 0.0f;
-    }
-    if (p.gamma) load_part<float, C::VEC>(p.gamma + col, p.cols - col, ga[k]);
-  }
-  // PER_BLOCK == 1: every thread of the block has the same trip count, so the
-  // barriers inside team_sum meet
-  for (int64_t row = (int64_t)blockIdx.x * C::PER_BLOCK + team; row < p.rows; row += (int64_t)gridDim.x * C::PER_BLOCK) {
+    for (int i = 0; i < C::VEC; ++i) sg[k][i] = sb[k][i] = 0.0f;
+  // every team of the block makes the same number of turns (the barriers
+  // inside team_sum meet); a team without a row reads and writes nothing
+  for (int64_t base = (int64_t)blockIdx.x * C::PER_BLOCK; base < p.rows; base += (int64_t)gridDim.x * C::PER_BLOCK) {
+    const bool any = base + team < p.rows;
+    const int64_t row = any ? base + team : 0;
+    const int cols = any ? (int)p.cols : 0;
     const T* x = static_cast<const T*>(p.x) + row * p.ldx;
     const T* g = static_cast<const T*>(p.g) + row * p.ldg;
-    const float mean = p.mean[row], rstd = p.rstd[row];
     float xh[C::NV][C::VEC], gv[C::NV][C::VEC];
+#pragma unroll
+    for (int k = 0; k < C::NV; ++k) {
+      const int col = (k * C::TPR + t) * C::VEC;
+      load_part<T, C::VEC>(x + col, cols - col, xh[k]);
+      load_part<T, C::VEC>(g + col, cols - col, gv[k]);
+    }
+    const float mean = p.mean[row], rstd = p.rstd[row];
     float s[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int k = 0; k < C::NV; ++k) {
-      const int64_t col = (int64_t)(k * C::TPR + t) * C::VEC;
-      load_part<T, C::VEC>(x + col, p.cols - col, xh[k]);
-      load_part<T, C::VEC>(g + col, p.cols - col, gv[k]);
-    }
+      const int col = (k * C::TPR + t) * C::VEC;
+      float ga[C::VEC];
 #pragma unroll
-    for (int k = 0; k < C::NV; ++k)
+      for (int i = 0; i < C::VEC; ++i) ga[i] = 1.0f;
+      // read again for every row: from the nearest cache, and the registers
+      // hold more waves instead
+      if (p.gamma) load_part<float, C::VEC>(p.gamma + col, (int)p.cols - col, ga);
 #pragma unroll
       for (int i = 0; i < C::VEC; ++i) {
         // columns past the end have g = 0, so whatever xh is there adds nothing
         xh[k][i] = (xh[k][i] - mean) * rstd;
         sg[k][i] = fmaf(gv[k][i], xh[k][i], sg[k][i]);
         sb[k][i] += gv[k][i];
-        gv[k][i] *= ga[k][i];
+        gv[k][i] *= ga[i];
         s[0] += gv[k][i];
         s[1] = fmaf(gv[k][i], xh[k][i], s[1]);
       }
-    team_sum<C, 2>(s, sh);
+    }
+    team_sum<C, 2>(s, sh[team]);
     const float a = s[0] * inv, b = s[1] * inv;
     T* y = static_cast<T*>(p.y) + row * p.ldy;
 #pragma unroll
@@ -199,38 +208,46 @@ __global__ __launch_bounds__(C::THREADS) void norm_backward_kernel(NormParams p)
       float o[C::VEC];
 #pragma unroll
       for (int i = 0; i < C::VEC; ++i) o[i] = rstd * ((gv[k][i] - a) - xh[k][i] * b);
-      store_part<T, C::VEC>(y + col, p.cols - col, o);
+      store_part<T, C::VEC>(y + col, cols - col, o);
     }
   }
   if (!p.grad_gamma && !p.grad_beta) return;
-  float* part = p.part + (int64_t)blockIdx.x * 2 * p.cols;
-  if constexpr (C::PER_BLOCK > 1) {
-    for (int w = 0; w < C::PER_BLOCK; ++w) {
-      if (team == w) {
 #pragma unroll
-        for (int k = 0; k < C::NV; ++k)
+  for (int w = C::PER_BLOCK / 2; w > 0; w /= 2) {  // teams w .. 2 w - 1 hand over to 0 .. w - 1
+    if (team >= w && team < 2 * w) {
 #pragma unroll
-          for (int i = 0; i < C::VEC; ++i) {
-            const int col = (k * C::TPR + t) * C::VEC + i;
-            if (w > 0) {
-              sg[k][i] += col_sum[col];
-              sb[k][i] += col_sum[C::COLS + col];
-            }
-            if (w + 1 < C::PER_BLOCK) {
-              col_sum[col] = sg[k][i];
-              col_sum[C::COLS + col] = sb[k][i];
-            }
-          }
+      for (int k = 0; k < C::NV; ++k) {
+        const int col = (k * C::TPR + t) * C::VEC;
+        store_vec<float, C::VEC>(&col_sum[team - w][0][col], sg[k]);
+        store_vec<float, C::VEC>(&col_sum[team - w][1][col], sb[k]);
       }
-      __syncthreads();
     }
-    if (team != C::PER_BLOCK - 1) return;
+    __syncthreads();
+    if (team < w) {
+#pragma unroll
+      for (int k = 0; k < C::NV; ++k) {
+        const int col = (k * C::TPR + t) * C::VEC;
+        float a[C::VEC], b[C::VEC];
+        load_vec<float, C::VEC>(&col_sum[team][0][col], a);
+        load_vec<float, C::VEC>(&col_sum[team][1][col], b);
+#pragma unroll
+        for (int i = 0; i < C::VEC; ++i) {
+          sg[k][i] += a[i];
+          sb[k][i] += b[i];
+        }
+      }
+    }
+    __syncthreads();
   }
+  if (team != 0) return;
+  float* part = p.part + (int64_t)blockIdx.x * 2 * p.cols;
+  float* const to_gamma = gridDim.x == 1 ? p.grad_gamma : part;
+  float* const to_beta = gridDim.x == 1 ? p.grad_beta : part + p.cols;
 #pragma unroll
   for (int k = 0; k < C::NV; ++k) {
     const int64_t col = (int64_t)(k * C::TPR + t) * C::VEC;
-    store_part<float, C::VEC>(part + col, p.cols - col, sg[k]);
-    store_part<float, C::VEC>(part + p.cols + col, p.cols - col, sb[k]);
+    if (to_gamma) store_part<float, C::VEC>(to_gamma + col, p.cols - col, sg[k]);
+    if (to_beta) store_part<float, C::VEC>(to_beta + col, p.cols - col, sb[k]);
   }
 }
 
@@ -346,11 +363,25 @@ hipError_t launch_norm_forward(fqt_dtype type, const NormParams& p, hipStream_t 
   });
 }
 
-constexpr int64_t BACKWARD_BLOCKS = 1024;
+// Backward: blocks of 1024 threads.
+template <class T, class F>
+static hipError_t with_block(int64_t cols, F f) {
+  constexpr int V = 16 / (int)sizeof(T);
+  constexpr int H = V / 2;
+  if (cols <= 64 * 4) return f(Team<64, H, 4 / H, 1024>{});
+  if (cols <= 64 * 8) return f(Team<64, V, 8 / V, 1024>{});
+  if (cols <= 64 * 16) return f(Team<64, V, 16 / V, 1024>{});
+  if (cols <= 256 * 8) return f(Team<256, V, 8 / V, 1024>{});
+  if (cols <= 256 * 16) return f(Team<256, V, 16 / V, 1024>{});
+  if (cols <= 512 * 16) return f(Team<512, V, 16 / V, 1024>{});
+  return f(Team<1024, V, 16 / V>{});
+}
+constexpr int64_t BACKWARD_BLOCKS = 256;
 static int64_t backward_blocks(int64_t rows, int64_t cols) {
   if (cols > TEAM_COLS) return rows < LONG_RUNS ? rows : LONG_RUNS;
-  const int64_t teams = cols <= 64 * 16 ? (rows + 3) / 4 : rows;
-  return teams < BACKWARD_BLOCKS ? teams : BACKWARD_BLOCKS;
+  const int64_t per = cols <= 64 * 16 ? 16 : cols <= 256 * 16 ? 4 : cols <= 512 * 16 ? 2 : 1;
+  const int64_t blocks = (rows + per - 1) / per;
+  return blocks < BACKWARD_BLOCKS ? blocks : BACKWARD_BLOCKS;
 }
 int64_t norm_backward_partials(int64_t rows, int64_t cols) { return backward_blocks(rows, cols) * 2 * cols; }
 
@@ -360,7 +391,7 @@ hipError_t launch_norm_backward(fqt_dtype type, const NormParams& p, hipStream_t
   if (p.rows > 0x7FFFFFFF) return hipErrorInvalidValue;
   const hipError_t e = with_type(type, [&](auto el) {
     using T = decltype(el);
-    return with_team<T>(p.cols, [&](auto c) {
+    return with_block<T>(p.cols, [&](auto c) {
       using C = decltype(c);
       if (p.cols <= TEAM_COLS) {
         hipLaunchKernelGGL((norm_backward_kernel<T, C>), dim3((unsigned)blocks), dim3(C::THREADS), 0, s, p);
@@ -373,7 +404,7 @@ hipError_t launch_norm_backward(fqt_dtype type, const NormParams& p, hipStream_t
       return hipGetLastError();
     });
   });
-  if (e != hipSuccess || !sums) return e;
+  if (e != hipSuccess || !sums || (blocks == 1 && p.cols <= TEAM_COLS)) return e;
   hipLaunchKernelGGL(norm_reduce_kernel, dim3((unsigned)((2 * p.cols + 63) / 64)), dim3(64 * REDUCE_WAVES), 0, s,
                      p.part, blocks, p.cols, p.grad_gamma, p.grad_beta);
   return hipGetLastError();

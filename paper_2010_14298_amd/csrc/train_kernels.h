@@ -180,17 +180,20 @@ hipError_t launch_fp8_gemm(fqt_dtype type, const Fp8GemmParams& p, hipStream_t s
 // ---------------------------------------------------------------------------
 // gradient norm and clipping
 // ---------------------------------------------------------------------------
-constexpr int CLIP_TENSORS = 96;  // tensors of one launch: their table travels in the kernel's arguments
-constexpr int CLIP_PARTS = 1024;  // partial sums of one launch
+// Tensors of one launch: their table travels in the kernel's arguments (4 KB),
+// so nothing is copied to the device beforehand.
+constexpr int CLIP_TENSORS = 168;
+constexpr int CLIP_PARTS = 1024;        // partial sums of one launch
+constexpr int64_t CLIP_BYTES = 16384;   // a chunk: one block's turn
 struct ClipTable {
-  const void* g[CLIP_TENSORS];
+  const void* g[CLIP_TENSORS];  // none of them empty
   void* out[CLIP_TENSORS];
-  int64_t n[CLIP_TENSORS];
   uint32_t first[CLIP_TENSORS + 1];  // first chunk of each tensor
+  uint16_t tail[CLIP_TENSORS];       // bytes of its last chunk
   uint8_t type[CLIP_TENSORS];
   int count;
 };
-int64_t clip_chunks(int64_t n);
+static_assert(sizeof(ClipTable) <= 4000, "kernel arguments");
 hipError_t launch_clip_norm(const ClipTable& t, double* part, hipStream_t s);
 hipError_t launch_clip_scale(const ClipTable& t, const double* part, int64_t parts, double max_norm, float* norm,
                              hipStream_t s);

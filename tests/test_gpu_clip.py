@@ -41,7 +41,7 @@ def check(grads, outs, norm, max_norm):
 
 
 SETS = [[1], [0, 1, 0], [5, 3, 0, 16384, 16385, 16383], [100003], [7] * 96, [13] * 97, [1, 1000, 0, 31] * 75,
-        [3000000, 17, 1 << 20]]
+        [3000000, 17, 1 << 20], [7] * 168, [13] * 169, [1, 1000, 0, 31] * 175, [0, 0]]
 
 
 @pytest.mark.parametrize("max_norm", [0.125, 1e9])

@@ -59,6 +59,12 @@ struct Quad<float> {
   }
   static __device__ __forceinline__ uint32_t bf_keys(uint32_t w) { return w; }
   __device__ __forceinline__ float at(int j) const { return v[j]; }
+  // the elements' sign bits, a byte each
+  __device__ __forceinline__ uint32_t signs() const {
+    const uint32_t a = __builtin_amdgcn_perm(__float_as_uint(v[1]), __float_as_uint(v[0]), 0x0c0c0703u);
+    const uint32_t b = __builtin_amdgcn_perm(__float_as_uint(v[3]), __float_as_uint(v[2]), 0x07030c0cu);
+    return (a | b) & 0x80808080u;
+  }
   // nearest codes of this row's quad, and of column j over four rows
   __device__ __forceinline__ uint32_t row_codes(float scale) const {
     s16x2 w = {0, 0};
@@ -102,6 +108,7 @@ struct Quad16 {
     k[0] = c.m[0];
     k[1] = c.m[1];
   }
+  __device__ __forceinline__ uint32_t signs() const { return __builtin_amdgcn_perm(w[1], w[0], 0x07050301u) & 0x80808080u; }
   // the words of rows a and b: element j of each
   static __device__ __forceinline__ uint32_t pair(uint32_t a, uint32_t b, int j) {
     return __builtin_amdgcn_perm(b, a, (j & 1) ? 0x07060302u : 0x05040100u);

@@ -26,32 +26,40 @@ constexpr int GROUP = TILE / (QT / 32);  // rows of one thread: 16
 // Stochastic codes of four elements v 2^-E, |v 2^-E| <= 448, from the low 24
 // bits u of a word each.  With m the bits of |v 2^-E|: from 2^-6 on, the part
 // below the format's three mantissa bits is m's low 20 bits, so u < frac 2^24
-// says that u >> 4 is below them: adding the complement of u >> 4 carries into
-// the code, bits 20 and up, exactly then (less the exponents' difference of
-// 120; an element that is zero stays below and saturates to code 0).  Below
-// 2^-6 the step is 2^-9: ceil(|v 2^-E| 2^9 2^24) plus the complement of u
-// carries into bit 24.  Codes are formed in the top byte, with the sign.
-__device__ __forceinline__ uint32_t quad_codes(const float (&v)[4], const float (&down)[4], const u32x4& u) {
+// says that u >> 4 is below them: m + 2^20 - 1 - (u >> 4) has carried into the
+// code, bits 20 and up, exactly then (less the exponents' difference of 120;
+// an element that is zero stays below and saturates to code 0).  Below 2^-6
+// the step is 2^-9: ceil(|v 2^-E| 2^9 2^24) plus the complement of u carries
+// into bit 24.  sign: the elements' sign bits, a byte each.
+__device__ __forceinline__ uint32_t quad_codes(const float (&v)[4], const float (&down)[4], const u32x4& u,
+                                               uint32_t sign) {
   const uint32_t word[4] = {u.x, u.y, u.z, u.w};
-  uint32_t m[4], c[4], least = ~0u;
+  uint32_t m[4], c[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     m[j] = __float_as_uint(__builtin_fabsf(v[j]) * down[j]);
-    least = least < m[j] - 1u ? least : m[j] - 1u;
-    c[j] = __builtin_elementwise_sub_sat(m[j] + (~word[j] >> 4 & 0xfffffu), 120u << 23) << 4;
+    const uint32_t f = word[j] >> 4 & 0xfffffu;
+    c[j] = __builtin_elementwise_sub_sat(__builtin_elementwise_sub_sat(m[j], f), (120u << 23) - 0xfffffu);
   }
-  // rare: one element in thousands lies that far below its block's largest
-  if (__builtin_amdgcn_ballot_w64(least < 0x3c7fffffu) != 0) {  // 0 < |v 2^-E| < 2^-6
+  // zeros are right as they are; anything else below 2^-6 is rare, one element
+  // in thousands lies that far below its block's largest
+  const uint32_t a = m[0] < m[1] ? m[0] : m[1], b = m[2] < m[3] ? m[2] : m[3];
+  if (__builtin_amdgcn_ballot_w64((a < b ? a : b) < 0x3c800000u) != 0) {
+    uint32_t least = ~0u;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t t = (uint32_t)ceilf(__uint_as_float(m[j]) * 8589934592.0f) + (~word[j] & 0xffffffu);
-      c[j] = m[j] < 0x3c800000u ? t : c[j];
+    for (int j = 0; j < 4; ++j) least = least < m[j] - 1u ? least : m[j] - 1u;
+    if (__builtin_amdgcn_ballot_w64(least < 0x3c7fffffu) != 0) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t t = (uint32_t)ceilf(__uint_as_float(m[j]) * 8589934592.0f) + (~word[j] & 0xffffffu);
+        c[j] = m[j] < 0x3c800000u ? t >> 4 : c[j];
+      }
     }
   }
-#pragma unroll
-  for (int j = 0; j < 4; ++j) c[j] = (c[j] & 0x7fffffffu) | (__float_as_uint(v[j]) & 0x80000000u);
-  const uint32_t lo = __builtin_amdgcn_perm(c[1], c[0], 0x0c0c0703u);
-  uint32_t w = lo | __builtin_amdgcn_perm(c[3], c[2], 0x07030c0cu);
+  // bits 20 .. 26 of each, side by side
+  const u16x2 lo = as<u16x2>(__builtin_amdgcn_perm(c[1], c[0], 0x07060302u)) >> (unsigned short)4;
+  const u16x2 hi = as<u16x2>(__builtin_amdgcn_perm(c[3], c[2], 0x07060302u)) >> (unsigned short)4;
+  uint32_t w = __builtin_amdgcn_perm(as<uint32_t>(hi), as<uint32_t>(lo), 0x06040200u) | sign;
   asm volatile("" : "+v"(w));  // packed here: the compiler would keep all rows' codes apart to the end
   return w;
 }
@@ -168,17 +176,18 @@ __global__ __launch_bounds__(QT) void fp8_tile_kernel(Fp8QuantParams p) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const float f[4] = {v[i + k].at(0), v[i + k].at(1), v[i + k].at(2), v[i + k].at(3)};
+        const uint32_t sign = v[i + k].signs();
         const uint64_t e = (uint64_t)(row + i + k) * (uint64_t)p.cols + (uint64_t)col;
         if constexpr (ROW) {
           const int sh = 16 * (k & 1);
           const uint32_t rkey = rk[(i + k) / 2] >> sh & 0xffffu, rbyte = scale_bytes(rk[(i + k) / 2]) >> sh & 0xffffu;
           const float s = scale_down(rbyte);
           const float down[4] = {s, s, s, s};
-          store_row(i + k, rkey, quad_codes(f, down, quad_words(e, p.seed, 1u, whole)));
+          store_row(i + k, rkey, quad_codes(f, down, quad_words(e, p.seed, 1u, whole), sign));
         }
         if constexpr (COL) {
           const float down[4] = {scale_down(byte[0]), scale_down(byte[1]), scale_down(byte[2]), scale_down(byte[3])};
-          r[k] = quad_codes(f, down, quad_words(e, p.seed, 0u, whole));
+          r[k] = quad_codes(f, down, quad_words(e, p.seed, 0u, whole), sign);
         }
         __builtin_amdgcn_sched_barrier(0);  // one row at a time: fewer registers, more waves
       }

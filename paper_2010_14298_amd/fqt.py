@@ -525,7 +525,7 @@ def fqt_layernorm_backward(G, X, mean, rstd, gamma=None, grad_X=None, params=Tru
     pg, dt, rows, cols, ldg = _matrix(G, "G", dev)
     px, _, _, _, ldx = _matrix(X, "X", dev, G.shape, G.dtype)
     if grad_X is None:
-        grad_X = torch.empty((rows, cols), dtype=G.dtype, device=G.device)
+        grad_X = G.new_empty((rows, cols))
     py, _, _, _, ldgx = _matrix(grad_X, "grad_X", dev, G.shape, G.dtype)
     gg = gb = None
     if params:
@@ -550,6 +550,14 @@ def fp8_operand(rows, K, device):
                 exp=torch.empty(((blocks + 3) // 4, rows, 4), dtype=torch.uint8, device=device), K=K)
 
 
+def _new_fp8(like, rows, K):
+    """fp8_operand on the device of `like`, and its C struct."""
+    blocks = (K + 127) // 128
+    q = like.new_empty((rows, blocks * 128), dtype=torch.float8_e4m3fn)
+    e = like.new_empty(((blocks + 3) // 4, rows, 4), dtype=torch.uint8)
+    return dict(q=q, exp=e, K=K), Fp8(q.data_ptr(), e.data_ptr(), 0)
+
+
 def _fp8(a, name, dev, rows=None, K=None):
     """The C struct of an operand (None: NULL), checked against the rows and K that the call needs."""
     if a is None:
@@ -571,10 +579,10 @@ def fqt_fp8_quantize(x, tile=False, by_row=True, by_col=False, stochastic=False,
     """Operands of x [rows, cols]: (x [rows, K = cols] or None, x^T [cols, K = rows] or None), from one read."""
     dev = _device()
     px, dt, rows, cols, ldx = _matrix(x, "x", dev)
-    a = fp8_operand(rows, cols, x.device) if by_row else None
-    b = fp8_operand(cols, rows, x.device) if by_col else None
-    rc = load().fqt_fp8_quantize(px, dt, rows, cols, ldx, int(bool(tile)), int(bool(stochastic)), seed,
-                                 _fp8(a, "by_row", dev), _fp8(b, "by_col", dev), _raw_stream(dev))
+    a, ca = _new_fp8(x, rows, cols) if by_row else (None, None)
+    b, cb = _new_fp8(x, cols, rows) if by_col else (None, None)
+    rc = load().fqt_fp8_quantize(px, dt, rows, cols, ldx, int(bool(tile)), int(bool(stochastic)), seed, ca, cb,
+                                 _raw_stream(dev))
     _check("fqt_fp8_quantize", rc)
     return a, b
 
@@ -614,11 +622,12 @@ def fqt_fp8_linear_forward(X, W8, relu=False, save=True, Y=None, ws=None):
     if Y is None:
         Y = X.new_empty((N, d_out))
     py, _, _, _, ldy = _matrix(Y, "Y", dev, (N, d_out), X.dtype)
-    X8t = fp8_operand(d_in, N, X.device) if save else None
+    X8t, x8t = _new_fp8(X, d_in, N) if save else (None, None)
+    lib = load()
     if ws is None:
-        ws = _workspace(fqt_fp8_linear_forward_workspace(N, d_in, d_out), X.device)
-    rc = load().fqt_fp8_linear_forward(px, dt, N, d_in, ldx, w8, d_out, int(bool(relu)), py, ldy, _fp8(X8t, "X8t", dev),
-                                       ws.data_ptr(), ws.numel(), _raw_stream(dev))
+        ws = X.new_empty(lib.fqt_fp8_linear_forward_workspace(N, d_in, d_out), dtype=torch.uint8)
+    rc = lib.fqt_fp8_linear_forward(px, dt, N, d_in, ldx, w8, d_out, int(bool(relu)), py, ldy, x8t, ws.data_ptr(),
+                                    ws.numel(), _raw_stream(dev))
     _check("fqt_fp8_linear_forward", rc)
     return Y, X8t, ws
 
@@ -637,24 +646,25 @@ def fqt_fp8_linear_backward(G, X8t, W8t, seed=0, stochastic=True, relu_input=Non
     x8t = _fp8(X8t, "X8t", dev, d_in, N)
     w8t = _fp8(W8t, "W8t", dev, d_in, d_out)
     if grad_W is None:
-        grad_W = torch.empty((d_out, d_in), dtype=torch.float32, device=G.device)
-    if (grad_W.dtype != torch.float32 or grad_W.shape != (d_out, d_in) or not grad_W.is_contiguous()):
+        grad_W = G.new_empty((d_out, d_in), dtype=torch.float32)
+    elif (grad_W.dtype != torch.float32 or grad_W.shape != (d_out, d_in) or not grad_W.is_contiguous()):
         raise ValueError("grad_W must be a contiguous float32 tensor [d_out, d_in]")
     px, ldgx = None, 0
     if not input_grad:
         grad_X = None
     else:
         if grad_X is None:
-            grad_X = torch.empty((N, d_in), dtype=G.dtype, device=G.device)
+            grad_X = G.new_empty((N, d_in))
         px, _, _, _, ldgx = _matrix(grad_X, "grad_X", dev, (N, d_in), G.dtype)
     pr, ldr = None, 0
     if relu_input is not None:
         pr, _, _, _, ldr = _matrix(relu_input, "relu_input", dev, (N, d_in), G.dtype)
+    lib = load()
     if ws is None:
-        ws = _workspace(fqt_fp8_linear_backward_workspace(N, d_in, d_out), G.device)
-    rc = load().fqt_fp8_linear_backward(pg, dt, N, d_out, ldg, x8t, w8t, d_in, int(bool(stochastic)), seed, pr, ldr,
-                                        _here(grad_W, "grad_W", dev).data_ptr(), px, ldgx, ws.data_ptr(), ws.numel(),
-                                        _raw_stream(dev))
+        ws = G.new_empty(lib.fqt_fp8_linear_backward_workspace(N, d_in, d_out), dtype=torch.uint8)
+    rc = lib.fqt_fp8_linear_backward(pg, dt, N, d_out, ldg, x8t, w8t, d_in, int(bool(stochastic)), seed, pr, ldr,
+                                     _here(grad_W, "grad_W", dev).data_ptr(), px, ldgx, ws.data_ptr(), ws.numel(),
+                                     _raw_stream(dev))
     _check("fqt_fp8_linear_backward", rc)
     return grad_W, grad_X, ws
 

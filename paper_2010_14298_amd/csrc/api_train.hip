@@ -56,10 +56,11 @@ Fp8Buffers take_operand(Carver& c, int64_t rows, int64_t K) {
   return b;
 }
 
-// An operand's codes row by row: its own, or laid out in `room`.
-hipError_t rows_of(const fqt_fp8* a, int64_t rows, int64_t K, uint8_t* room, const uint8_t** q, hipStream_t s) {
-  *q = a->k_major ? room : a->q;
-  return a->k_major ? launch_fp8_turn(a->q, rows, K, room, s) : hipSuccess;
+// An operand's codes row by row: its own, or laid out in `room` by `turn`.
+const uint8_t* rows_of(const fqt_fp8* a, int64_t rows, int64_t K, uint8_t* room, Fp8Turn* turn) {
+  if (!a->k_major) return a->q;
+  *turn = Fp8Turn{a->q, rows, K, room};
+  return room;
 }
 
 struct GemmWs {
@@ -221,10 +222,13 @@ fqt_status fqt_fp8_gemm(const fqt_fp8* A, const fqt_fp8* B, int64_t M, int64_t N
   Carver c(ws);
   const GemmWs w = carve_gemm(c, M, N, K);
   Fp8GemmParams p{};
-  FQT_TRY(rows_of(A, M, K, w.a, &p.A, s));
+  Fp8Turn a{}, b{};
+  p.A = rows_of(A, M, K, w.a, &a);
   p.eA = A->exp;
-  FQT_TRY(rows_of(B, N, K, w.b, &p.B, s));
+  p.B = rows_of(B, N, K, w.b, &b);
   p.eB = B->exp;
+  FQT_TRY(launch_fp8_turn(a, s));
+  FQT_TRY(launch_fp8_turn(b, s));
   p.M = M;
   p.N = N;
   p.K = K;
@@ -270,12 +274,13 @@ fqt_status fqt_fp8_linear_forward(const void* X, fqt_dtype type, int64_t N, int6
     q.q_col = X8t->q;
     q.e_col = X8t->exp;
   }
-  if (q.q_row || q.q_col) FQT_TRY(launch_fp8_quantize(type, q, s));
   Fp8GemmParams p{};
+  Fp8Turn turn{};
   p.A = w.x.q;
   p.eA = w.x.e;
-  FQT_TRY(rows_of(W8, d_out, d_in, w.w, &p.B, s));
+  p.B = rows_of(W8, d_out, d_in, w.w, &turn);
   p.eB = W8->exp;
+  FQT_TRY(launch_fp8_quantize_turn(type, q, turn, Fp8Turn{}, s));
   p.M = N;
   p.N = d_out;
   p.K = d_in;
@@ -325,14 +330,17 @@ fqt_status fqt_fp8_linear_backward(const void* G, fqt_dtype type, int64_t N, int
     q.q_col = w.gt.q;
     q.e_col = w.gt.e;
   }
-  FQT_TRY(launch_fp8_quantize(type, q, s));
+  Fp8Turn turn_x{}, turn_w{};
+  const uint8_t* const x8 = grad_W ? rows_of(X8t, d_in, N, w.x, &turn_x) : nullptr;
+  const uint8_t* const w8 = grad_X ? rows_of(W8t, d_in, d_out, w.w, &turn_w) : nullptr;
+  FQT_TRY(launch_fp8_quantize_turn(type, q, turn_x, turn_w, s));
   Fp8GemmParams p{};
   p.part = w.part;
   p.N = d_in;
   if (grad_W) {
     p.A = w.gt.q;
     p.eA = w.gt.e;
-    FQT_TRY(rows_of(X8t, d_in, N, w.x, &p.B, s));
+    p.B = x8;
     p.eB = X8t->exp;
     p.M = d_out;
     p.K = N;
@@ -343,7 +351,7 @@ fqt_status fqt_fp8_linear_backward(const void* G, fqt_dtype type, int64_t N, int
   if (grad_X) {
     p.A = w.g.q;
     p.eA = w.g.e;
-    FQT_TRY(rows_of(W8t, d_in, d_out, w.w, &p.B, s));
+    p.B = w8;
     p.eB = W8t->exp;
     p.M = N;
     p.K = d_out;

@@ -89,14 +89,14 @@ __device__ __forceinline__ u32x4 quad_words(uint64_t e, uint64_t seed, uint32_t 
   return u;
 }
 
+// One tile of 128 x 128, by a block of threads; `turned`: LDS, 16 KB where COL.
 template <class T, bool ROW, bool COL, bool SQUARE, bool SR>
-__global__ __launch_bounds__(QT) void fp8_tile_kernel(Fp8QuantParams p) {
+__device__ __forceinline__ void quantize_tile(const Fp8QuantParams& p, uint32_t block, uint8_t* turned) {
   __shared__ uint32_t col_top[QT / 32][TILE / 2];
   __shared__ __attribute__((aligned(8))) uint16_t keys[2][TILE];  // of the rows, of the columns
-  __shared__ __attribute__((aligned(16))) uint8_t turned[COL ? TILE * TILE : 16];
   const int tid = threadIdx.x, quad = tid & 31, grp = tid >> 5;
   const uint32_t row_blocks = (uint32_t)fp8_blocks(p.rows);
-  const uint32_t cb = blockIdx.x / row_blocks, rb = blockIdx.x - cb * row_blocks;
+  const uint32_t cb = block / row_blocks, rb = block - cb * row_blocks;
   const int64_t r0 = (int64_t)rb * TILE, c0 = (int64_t)cb * TILE;
   const int64_t row = r0 + grp * GROUP, col = c0 + 4 * quad;
   const T* x = static_cast<const T*>(p.x) + row * p.ldx + col;
@@ -243,10 +243,11 @@ __global__ __launch_bounds__(QT) void fp8_tile_kernel(Fp8QuantParams p) {
 // Codes laid out column by column, [pitch][rows], into rows [rows][pitch]:
 // 128 x 128 bytes a block; a thread turns 4 x 4 bytes over in registers, LDS
 // gathers rows of 128.
-__global__ __launch_bounds__(QT) void fp8_turn_kernel(const uint8_t* src, int64_t rows, int64_t pitch, uint8_t* dst) {
-  __shared__ uint32_t sh[TILE][TILE / 4 + 1];
-  const int64_t kblocks = pitch / TILE;
-  const int64_t k0 = (int64_t)blockIdx.x % kblocks * TILE, r0 = (int64_t)blockIdx.x / kblocks * TILE;
+typedef uint32_t TurnLds[TILE][TILE / 4 + 1];
+__device__ __forceinline__ void turn_tile(const uint8_t* src, int64_t rows, int64_t pitch, uint8_t* dst, uint32_t block,
+                                          TurnLds& sh) {
+  const uint32_t kblocks = (uint32_t)(pitch / TILE);
+  const int64_t k0 = (int64_t)(block % kblocks) * TILE, r0 = (int64_t)(block / kblocks) * TILE;
   const int quad = threadIdx.x & 31, grp = threadIdx.x >> 5;
   const int64_t row = r0 + 4 * quad, left = rows - row;
   uint32_t in[GROUP];
@@ -276,11 +277,59 @@ __global__ __launch_bounds__(QT) void fp8_turn_kernel(const uint8_t* src, int64_
   }
 }
 
-hipError_t launch_fp8_turn(const uint8_t* src, int64_t rows, int64_t K, uint8_t* dst, hipStream_t s) {
-  const int64_t blocks = fp8_blocks(rows) * fp8_blocks(K);
+template <class T, bool ROW, bool COL, bool SQUARE, bool SR>
+__global__ __launch_bounds__(QT) void fp8_tile_kernel(Fp8QuantParams p) {
+  __shared__ __attribute__((aligned(16))) uint8_t turned[COL ? TILE * TILE : 16];
+  quantize_tile<T, ROW, COL, SQUARE, SR>(p, blockIdx.x, turned);
+}
+__global__ __launch_bounds__(QT) void fp8_turn_kernel(Fp8Turn t) {
+  __shared__ TurnLds sh;
+  turn_tile(t.src, t.rows, fp8_pitch(t.K), t.dst, blockIdx.x, sh);
+}
+// Both in one launch: of every `step` blocks the last lays codes out, until there
+// are `turns` of them.  They wait for memory while the others compute.
+template <class T, bool SR>
+__global__ __launch_bounds__(QT) void fp8_tile_turn_kernel(Fp8QuantParams p, Fp8Turn a, Fp8Turn b, uint32_t turns_a,
+                                                           uint32_t turns, uint32_t step) {
+  __shared__ __attribute__((aligned(16))) uint8_t room[sizeof(TurnLds) > TILE * TILE ? sizeof(TurnLds) : TILE * TILE];
+  const uint32_t before = blockIdx.x / step;  // of those that lay out, up to `turns`
+  if (before >= turns || blockIdx.x - before * step != step - 1) {
+    quantize_tile<T, true, true, false, SR>(p, blockIdx.x - (before < turns ? before : turns), room);
+  } else {
+    const bool first = before < turns_a;
+    const Fp8Turn t = first ? a : b;
+    turn_tile(t.src, t.rows, fp8_pitch(t.K), t.dst, first ? before : before - turns_a, *reinterpret_cast<TurnLds*>(room));
+  }
+}
+
+static int64_t turn_blocks(const Fp8Turn& t) { return t.src ? fp8_blocks(t.rows) * fp8_blocks(t.K) : 0; }
+
+hipError_t launch_fp8_turn(const Fp8Turn& t, hipStream_t s) {
+  const int64_t blocks = turn_blocks(t);
+  if (blocks == 0) return hipSuccess;
   if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(fp8_turn_kernel, dim3((unsigned)blocks), dim3(QT), 0, s, src, rows, fp8_pitch(K), dst);
+  hipLaunchKernelGGL(fp8_turn_kernel, dim3((unsigned)blocks), dim3(QT), 0, s, t);
   return hipGetLastError();
+}
+
+hipError_t launch_fp8_quantize_turn(fqt_dtype type, const Fp8QuantParams& p, const Fp8Turn& a, const Fp8Turn& b,
+                                    hipStream_t s) {
+  const int64_t na = turn_blocks(a), nb = turn_blocks(b), blocks = fp8_blocks(p.rows) * fp8_blocks(p.cols) + na + nb;
+  if (na + nb > 0 && p.q_row && p.q_col && !p.tile && blocks <= 0x7FFFFFFF) {
+    return with_type(type, [&](auto e) {
+      using T = decltype(e);
+      auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(QT), 0, s, p, a, b, (uint32_t)na, (uint32_t)(na + nb),
+                           (uint32_t)(blocks / (na + nb)));
+        return hipGetLastError();
+      };
+      return p.stochastic ? go(fp8_tile_turn_kernel<T, true>) : go(fp8_tile_turn_kernel<T, false>);
+    });
+  }
+  hipError_t e = launch_fp8_turn(a, s);
+  if (e == hipSuccess) e = launch_fp8_turn(b, s);
+  if (e == hipSuccess && (p.q_row || p.q_col)) e = launch_fp8_quantize(type, p, s);
+  return e;
 }
 
 hipError_t launch_fp8_quantize(fqt_dtype type, const Fp8QuantParams& p, hipStream_t s) {

@@ -155,8 +155,18 @@ struct Fp8QuantParams {
 };
 hipError_t launch_fp8_quantize(fqt_dtype type, const Fp8QuantParams& p, hipStream_t s);
 
-// Codes that lie column by column (element (r, k) at k rows + r) into rows.
-hipError_t launch_fp8_turn(const uint8_t* src, int64_t rows, int64_t K, uint8_t* dst, hipStream_t s);
+// Codes that lie column by column (element (r, k) at k rows + r) into rows; src
+// null: nothing to do.
+struct Fp8Turn {
+  const uint8_t* src;
+  int64_t rows, K;
+  uint8_t* dst;
+};
+hipError_t launch_fp8_turn(const Fp8Turn& t, hipStream_t s);
+// The quantizer (or nothing, if neither operand is wanted) and two of those, in
+// one launch where both of the quantizer's operands are wanted.
+hipError_t launch_fp8_quantize_turn(fqt_dtype type, const Fp8QuantParams& p, const Fp8Turn& a, const Fp8Turn& b,
+                                    hipStream_t s);
 
 struct Fp8GemmParams {
   const uint8_t* A;   // [M, pitch(K)]

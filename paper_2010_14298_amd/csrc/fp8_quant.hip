@@ -287,7 +287,9 @@ __global__ __launch_bounds__(QT) void fp8_turn_kernel(Fp8Turn t) {
   turn_tile(t.src, t.rows, fp8_pitch(t.K), t.dst, blockIdx.x, sh);
 }
 // Both in one launch: of every `step` blocks the last lays codes out, until there
-// are `turns` of them.  They wait for memory while the others compute.
+// are `turns` of them.  They wait for memory while the others compute: a
+// backward of 8192, 1024 -> 4096 bfloat16 with both kept operands to lay out takes
+// 148.5 us, in three launches 151.5; of 1000, 512 -> 512 30.3 us, 35.4.
 template <class T, bool SR>
 __global__ __launch_bounds__(QT) void fp8_tile_turn_kernel(Fp8QuantParams p, Fp8Turn a, Fp8Turn b, uint32_t turns_a,
                                                            uint32_t turns, uint32_t step) {

@@ -505,7 +505,9 @@ def fqt_layernorm_forward(X, gamma=None, beta=None, eps=1e-5, Y=None):
     px, dt, rows, cols, ldx = _matrix(X, "X", dev)
     if Y is None:
         Y = X.new_empty((rows, cols))
-    py, _, _, _, ldy = _matrix(Y, "Y", dev, X.shape, X.dtype)
+        py, ldy = Y.data_ptr(), cols
+    else:
+        py, _, _, _, ldy = _matrix(Y, "Y", dev, X.shape, X.dtype)
     mean, rstd = X.new_empty((2, rows), dtype=torch.float32).unbind(0)
     rc = load().fqt_layernorm_forward(px, dt, rows, cols, ldx, _vector(gamma, "gamma", cols, dev),
                                       _vector(beta, "beta", cols, dev), eps, py, ldy, mean.data_ptr(), rstd.data_ptr(),
@@ -526,17 +528,20 @@ def fqt_layernorm_backward(G, X, mean, rstd, gamma=None, grad_X=None, params=Tru
     px, _, _, _, ldx = _matrix(X, "X", dev, G.shape, G.dtype)
     if grad_X is None:
         grad_X = G.new_empty((rows, cols))
-    py, _, _, _, ldgx = _matrix(grad_X, "grad_X", dev, G.shape, G.dtype)
-    gg = gb = None
+        py, ldgx = grad_X.data_ptr(), cols
+    else:
+        py, _, _, _, ldgx = _matrix(grad_X, "grad_X", dev, G.shape, G.dtype)
+    lib = load()
+    gg = gb = pgg = pgb = None
     if params:
         gg, gb = G.new_empty((2, cols), dtype=torch.float32).unbind(0)
+        pgg, pgb = gg.data_ptr(), gb.data_ptr()
         if ws is None:
-            ws = _workspace(fqt_layernorm_backward_workspace(rows, cols), G.device)
-    rc = load().fqt_layernorm_backward(pg, ldg, px, ldx, dt, rows, cols, _vector(mean, "mean", rows, dev),
-                                       _vector(rstd, "rstd", rows, dev), _vector(gamma, "gamma", cols, dev), py, ldgx,
-                                       _vector(gg, "grad_gamma", cols, dev), _vector(gb, "grad_beta", cols, dev),
-                                       ws.data_ptr() if ws is not None else None, ws.numel() if ws is not None else 0,
-                                       _raw_stream(dev))
+            ws = G.new_empty(max(lib.fqt_layernorm_backward_workspace(rows, cols), 16), dtype=torch.uint8)
+    rc = lib.fqt_layernorm_backward(pg, ldg, px, ldx, dt, rows, cols, _vector(mean, "mean", rows, dev),
+                                    _vector(rstd, "rstd", rows, dev), _vector(gamma, "gamma", cols, dev), py, ldgx,
+                                    pgg, pgb, ws.data_ptr() if ws is not None else None,
+                                    ws.numel() if ws is not None else 0, _raw_stream(dev))
     _check("fqt_layernorm_backward", rc)
     return grad_X, gg, gb, ws
 
@@ -621,7 +626,9 @@ def fqt_fp8_linear_forward(X, W8, relu=False, save=True, Y=None, ws=None):
     w8 = _fp8(W8, "W8", dev, d_out, d_in)
     if Y is None:
         Y = X.new_empty((N, d_out))
-    py, _, _, _, ldy = _matrix(Y, "Y", dev, (N, d_out), X.dtype)
+        py, ldy = Y.data_ptr(), d_out
+    else:
+        py, _, _, _, ldy = _matrix(Y, "Y", dev, (N, d_out), X.dtype)
     X8t, x8t = _new_fp8(X, d_in, N) if save else (None, None)
     lib = load()
     if ws is None:
@@ -655,7 +662,9 @@ def fqt_fp8_linear_backward(G, X8t, W8t, seed=0, stochastic=True, relu_input=Non
     else:
         if grad_X is None:
             grad_X = G.new_empty((N, d_in))
-        px, _, _, _, ldgx = _matrix(grad_X, "grad_X", dev, (N, d_in), G.dtype)
+            px, ldgx = grad_X.data_ptr(), d_in
+        else:
+            px, _, _, _, ldgx = _matrix(grad_X, "grad_X", dev, (N, d_in), G.dtype)
     pr, ldr = None, 0
     if relu_input is not None:
         pr, _, _, _, ldr = _matrix(relu_input, "relu_input", dev, (N, d_in), G.dtype)

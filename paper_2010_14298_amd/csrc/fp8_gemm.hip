@@ -177,13 +177,13 @@ __device__ __forceinline__ void interleave() {
 // have to be complete before the waves in front read them, so every wave
 // waits for the half stage after next at the end of its read segment.
 //
-// RUN: blocks stay for several tiles (16-bit outputs without a mask, whole tiles,
-// an even number of stages, at least four).  The next tile's first two stages
+// RUN: blocks stay for several tiles (16-bit outputs without a mask, whole tiles
+// of columns, an even number of stages, at least four).  The next tile's first two stages
 // are on their way before this one's outputs are stored, and loads behind the
 // stores are first waited for four segments later.  The load counter counts
 // stores as well, so until then the waits allow for STORES of them.  With one
-// block a tile / several, us: 8192 x 4096 x 1024 46.6 / 41.4, 8192 x 8192 x 1024
-// 91.0 / 76.5, 8192 x 4096 x 512 32.8 / 30.6, 8192 x 8192 x 8192 448 / 438, 6144 x
+// block a tile / several, us: 8192 x 4096 x 1024 46.6 / 41.4, 8000 x 4096 x 1024
+// 45.5 / 42.0, 16000 x 4096 x 512 63.5 / 52.2, 8192 x 8192 x 1024 91.0 / 76.5, 8192 x 4096 x 512 32.8 / 30.6, 8192 x 8192 x 8192 448 / 438, 6144 x
 // 4096 x 1024 (one and a half tiles a unit) 42.0 / 42.5.
 template <class T, bool WIDE, bool NT, bool RUN>
 __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(Fp8GemmParams p) {
@@ -364,7 +364,9 @@ __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(Fp8G
       T* const strip = out[wave];
       const float least = p.relu ? 0.0f : -__builtin_huge_valf();
       const int lr = lane >> 3, lc = (lane & 7) * 8;
-      T* const to = static_cast<T*>(p.C) + (row0 + wm * C::WM + lr) * p.ldc + col0 + wn * C::WN + lc;
+      // rows past the edge hold what the last row does and store it there again
+      T* const to = static_cast<T*>(p.C) + row0 * p.ldc + col0 + wn * C::WN + lc;
+      const int last = p.M - 1 - row0 < C::BM - 1 ? (int)(p.M - 1 - row0) : C::BM - 1;
 #pragma unroll
       for (int i = 0; i < 2 * C::IT; ++i) {
 #pragma unroll
@@ -379,7 +381,8 @@ __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(Fp8G
         for (int h = 0; h < 2; ++h) {
           typedef T vec __attribute__((ext_vector_type(8)));
           const vec v = *reinterpret_cast<const vec*>(strip + (8 * h + lr) * C::OUT16_LD + lc);
-          __builtin_nontemporal_store(v, reinterpret_cast<vec*>(to + (int64_t)(16 * i + 8 * h) * p.ldc));
+          const int r = wm * C::WM + 16 * i + 8 * h + lr;
+          __builtin_nontemporal_store(v, reinterpret_cast<vec*>(to + (r < last ? r : last) * p.ldc));
         }
         __builtin_amdgcn_wave_barrier();
       }
@@ -438,7 +441,7 @@ __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(Fp8G
     };
     rest_of_start();
     begin(none);
-    const int64_t tiles = (p.M / C::BM) * (p.N / C::BN);
+    const int64_t tiles = ((p.M + C::BM - 1) / C::BM) * (p.N / C::BN);
     for (;;) {
       stages_from(2);
       const int64_t row0 = m0, col0 = n0;
@@ -980,7 +983,7 @@ hipError_t launch_fp8_gemm(fqt_dtype type, const Fp8GemmParams& p, hipStream_t s
     };
     if (plan.tile == Plan::LARGE) {
       if constexpr (!WIDE) {
-        if (nt && blocks > 256 && p.M % LargeTile::BM == 0 && p.N % LargeTile::BN == 0 && !p.mask && plan.chunk % 2 == 0 &&
+        if (nt && blocks > 256 && p.N % LargeTile::BN == 0 && !p.mask && plan.chunk % 2 == 0 &&
             plan.chunk >= 4) {
           grid = 256;  // one block a unit
           return go(fp8_gemm_large_kernel<T, false, true, true>);

@@ -79,3 +79,15 @@ def test_nan_rows_reach_their_outputs_only():
     keep = torch.ones(M, dtype=torch.bool, device="cuda")
     keep[bad] = False
     assert torch.equal(C1[keep], C0[keep])
+
+
+@pytest.mark.parametrize("M", [4097, 8000, 8447])
+def test_rows_that_end_inside_a_tile(M):
+    """The same bits as the product of whole tiles, and nothing stored past the last row."""
+    N, K = 4096, 768
+    A, B = operand(7, 8448, K), operand(8, N, K, tile=True)
+    C, _ = fqt.fqt_fp8_gemm(A, B, dtype=torch.bfloat16)
+    wide = torch.full((M + 260, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    fqt.fqt_fp8_gemm(rows_of(A, 0, M), B, C=wide[:M])
+    assert torch.equal(wide[:M], C[:M])
+    assert (wide[M:] == 7.0).all()

@@ -50,7 +50,6 @@ struct LargeTile {
   static constexpr int E_SEGS = (BM + BN) / 64;             // 64-row runs of a stage's scale words
   static constexpr int E_INS = (E_SEGS + WAVES - 1) / WAVES;
   static constexpr int OUT_LD = WN + 8;                     // float row of the output staging
-  static constexpr int OUT16_LD = WN + 8;                   // 16-bit row of the same
   static_assert(WAVES == 8 && A_INS * 16 * WAVES == BM && B_INS * 16 * WAVES == BN, "whole 1 KB blocks per wave");
   static_assert(32 * OUT_LD * 4 <= HALF / 2, "two waves' output strips in a half stage's LDS");
 };
@@ -177,21 +176,24 @@ __device__ __forceinline__ void interleave() {
 // have to be complete before the waves in front read them, so every wave
 // waits for the half stage after next at the end of its read segment.
 //
-// RUN: blocks stay for several tiles (16-bit outputs without a mask, whole tiles
-// of columns, an even number of stages, at least four).  The next tile's first two stages
+// RUN: blocks stay for several tiles (no mask, whole tiles of columns, an even
+// number of stages, at least four).  The next tile's first two stages
 // are on their way before this one's outputs are stored, and loads behind the
 // stores are first waited for four segments later.  The load counter counts
 // stores as well, so until then the waits allow for STORES of them.  With one
 // block a tile / several, us: 8192 x 4096 x 1024 46.6 / 41.4, 8000 x 4096 x 1024
 // 45.5 / 42.0, 16000 x 4096 x 512 63.5 / 52.2, 8192 x 8192 x 1024 91.0 / 76.5, 8192 x 4096 x 512 32.8 / 30.6, 8192 x 8192 x 8192 448 / 438, 6144 x
-// 4096 x 1024 (one and a half tiles a unit) 42.0 / 42.5.
+// 4096 x 1024 (one and a half tiles a unit) 42.0 / 42.5; float32 8192 x 4096 x
+// 1024 70.4 / 70.8, 4096 x 8192 x 1024 79.0 / 71.5, 8192^3 780 / 774.
 template <class T, bool WIDE, bool NT, bool RUN>
 __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(Fp8GemmParams p) {
   using C = LargeTile;
   // separate arrays, so that a pending load into one does not hold up reads of another
   __shared__ __attribute__((aligned(16))) uint8_t h00[C::HALF], h01[C::HALF], h10[C::HALF], h11[C::HALF];
   __shared__ int e0[C::BM + C::BN], e1[C::BM + C::BN];
-  __shared__ __attribute__((aligned(16))) T out[RUN ? C::WAVES : 1][RUN ? 16 * C::OUT16_LD : 1];
+  // RUN: strips of outputs, 2 KB and padding a wave
+  constexpr int V = 16 / (int)sizeof(T), STRIP = 2 * V, STRIP_LD = C::WN + V;
+  __shared__ __attribute__((aligned(16))) T out[RUN ? C::WAVES : 1][RUN ? STRIP * STRIP_LD : 1];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / C::WAVES_N, wn = wave % C::WAVES_N;
@@ -360,28 +362,28 @@ __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(Fp8G
   };
   auto store_all = [&](int64_t row0, int64_t col0) __attribute__((always_inline)) {
     if constexpr (RUN) {
-      // 16 rows at a time through LDS of their own, whole lines out of it
+      // STRIP rows at a time through LDS of their own, whole lines out of it;
+      // rows past the edge hold what the last row does and store it there again
       T* const strip = out[wave];
       const float least = p.relu ? 0.0f : -__builtin_huge_valf();
-      const int lr = lane >> 3, lc = (lane & 7) * 8;
-      // rows past the edge hold what the last row does and store it there again
+      const int lr = lane / (C::WN / V), lc = lane % (C::WN / V) * V;
       T* const to = static_cast<T*>(p.C) + row0 * p.ldc + col0 + wn * C::WN + lc;
       const int last = p.M - 1 - row0 < C::BM - 1 ? (int)(p.M - 1 - row0) : C::BM - 1;
 #pragma unroll
-      for (int i = 0; i < 2 * C::IT; ++i) {
+      for (int i = 0; i < C::WM / STRIP; ++i) {
 #pragma unroll
         for (int j = 0; j < C::JT; ++j)
 #pragma unroll
-          for (int r = 0; r < 8; ++r) {
-            const float o = acc[i / 2][j][8 * (i & 1) + r];
-            strip[(8 * (r >> 2) + 4 * half + (r & 3)) * C::OUT16_LD + j * 32 + lrow] = (T)(o < least ? least : o);
+          for (int r = 0; r < STRIP / 2; ++r) {
+            const float o = acc[i * STRIP / 32][j][i * STRIP % 32 / 2 + r];
+            strip[(8 * (r >> 2) + 4 * half + (r & 3)) * STRIP_LD + j * 32 + lrow] = (T)(o < least ? least : o);
           }
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          typedef T vec __attribute__((ext_vector_type(8)));
-          const vec v = *reinterpret_cast<const vec*>(strip + (8 * h + lr) * C::OUT16_LD + lc);
-          const int r = wm * C::WM + 16 * i + 8 * h + lr;
+          typedef T vec __attribute__((ext_vector_type(V)));
+          const vec v = *reinterpret_cast<const vec*>(strip + (V * h + lr) * STRIP_LD + lc);
+          const int r = wm * C::WM + STRIP * i + V * h + lr;
           __builtin_nontemporal_store(v, reinterpret_cast<vec*>(to + (r < last ? r : last) * p.ldc));
         }
         __builtin_amdgcn_wave_barrier();
@@ -424,8 +426,7 @@ __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(Fp8G
     stages_from(0);
     store_all(m0, n0);
   } else {
-    static_assert(!WIDE && NT, "strips of 16-bit outputs");
-    constexpr std::integral_constant<int, 2 * C::IT * 2> STORES{};
+    constexpr std::integral_constant<int, C::WM / STRIP * 2> STORES{};
     // the first two stages, behind `more` stores
     auto begin = [&](auto more) __attribute__((always_inline)) {
       wait_loads<N1 + N0 + N1 + more>();  // (0, 0) is there
@@ -982,12 +983,9 @@ hipError_t launch_fp8_gemm(fqt_dtype type, const Fp8GemmParams& p, hipStream_t s
       return hipGetLastError();
     };
     if (plan.tile == Plan::LARGE) {
-      if constexpr (!WIDE) {
-        if (nt && blocks > 256 && p.N % LargeTile::BN == 0 && !p.mask && plan.chunk % 2 == 0 &&
-            plan.chunk >= 4) {
-          grid = 256;  // one block a unit
-          return go(fp8_gemm_large_kernel<T, false, true, true>);
-        }
+      if (nt && blocks > 256 && p.N % LargeTile::BN == 0 && !p.mask && plan.chunk % 2 == 0 && plan.chunk >= 4) {
+        grid = 256;  // one block a unit
+        return go(fp8_gemm_large_kernel<T, WIDE, true, true>);
       }
       return nt ? go(fp8_gemm_large_kernel<T, WIDE, true, false>) : go(fp8_gemm_large_kernel<T, WIDE, false, false>);
     }

@@ -91,3 +91,21 @@ def test_rows_that_end_inside_a_tile(M):
     fqt.fqt_fp8_gemm(rows_of(A, 0, M), B, C=wide[:M])
     assert torch.equal(wide[:M], C[:M])
     assert (wide[M:] == 7.0).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(4352, 4096, 512), (8000, 4096, 1000), (16640, 1024, 1250)])
+def test_float32_against_float64(M, N, K):
+    """float32 outputs: codes converted exactly, float32 accumulation in any order, no dropped terms."""
+    A, B = operand(M + 1, M, K), operand(N + 1, N, K, tile=True)
+    wide = torch.full((M + 260, N), 7.0, device="cuda")
+    fqt.fqt_fp8_gemm(A, B, C=wide[:M])
+    C = wide[:M]
+    R, _ = fqt.fqt_fp8_gemm(A, B, relu=True)
+    assert torch.equal(R, C.clamp(min=0)) and (wide[M:] == 7.0).all()
+    b = value(B)
+    bt, bat = b.t().contiguous(), b.abs().t().contiguous()
+    for r in range(0, M, 2048):
+        a = value(rows_of(A, r, min(r + 2048, M)))
+        want, size = a @ bt, a.abs() @ bat
+        tol = (K * 2.0 ** -24) * size + 2.0 ** -24 * want.abs()
+        assert ((C[r:r + 2048].double() - want).abs() <= tol).all(), r

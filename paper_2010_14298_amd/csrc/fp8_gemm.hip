@@ -15,8 +15,8 @@
 //
 // Back to back on changing operands, us (PFLOP/s), M x N x K:
 //                         bfloat16 outputs   float32 outputs
-//   8192 x 8192 x 8192       438 (2.51)         777 (1.42)
-//   8192 x 4096 x 1024       41.4 (1.66)        76.6 (0.90)
+//   8192 x 8192 x 8192       438 (2.51)         774 (1.42)
+//   8192 x 4096 x 1024       41.4 (1.66)        70.8 (0.97)
 //   8192 x 1024 x 4096       38.3 (1.79)        60.8 (1.13)
 //   4096 x 1024 x 8192       35.9 (1.91)        63.0 (1.09)
 // A library product on this card: 8192^3 3.2 PFLOP/s in 8-bit floating point,

@@ -13,19 +13,18 @@
 //     v_mfma_f32_32x32x16_bf16 at half the rate, which sums to 1.5e-7.
 // The output is rounded once.
 //
-// Back to back on changing operands, us (PFLOP/s), M x N x K:
-//                         bfloat16 outputs   float32 outputs
-//   8192 x 8192 x 8192       438 (2.51)         774 (1.42)
-//   8192 x 4096 x 1024       41.4 (1.66)        70.8 (0.97)
-//   8192 x 1024 x 4096       38.3 (1.79)        60.8 (1.13)
-//   4096 x 1024 x 8192       35.9 (1.91)        63.0 (1.09)
-// A library product on this card: 8192^3 3.2 PFLOP/s in 8-bit floating point,
-// 1.64 in bfloat16; 1.7 and 1.0 - 1.06 on the other three shapes.  8192 x 4096 x
-// 1024 spends the rest on the stores of the last tiles, which all units issue
+// Back to back on changing operands, us (PFLOP/s), M x N x K, and a library
+// product of the same sizes in the same run, without block scales and with
+// bfloat16 outputs:
+//                        bfloat16 outputs   8-bit library   float32 outputs   bfloat16 library
+//   8192 x 8192 x 8192      439 (2.50)          348            772 (1.42)          691
+//   8192 x 4096 x 1024       42 (1.64)           38             74 (0.93)           60
+//   8192 x 1024 x 4096       35 (1.95)           38             60 (1.15)           61
+//   4096 x 1024 x 8192       35 (1.98)           40             62 (1.12)           66
+// 8192 x 4096 x 1024 waits for the stores of its last tiles, which all units issue
 // at the same time.  In the longer products matrix instructions fill 50 % of the
 // cycles (bfloat16 outputs, 8192 x 1024 x 4096) and 57 % (float32, 4096 x 1024 x
-// 8192), at a clock of 1.8 GHz; without the conversions the latter is no faster
-// (64 us).
+// 8192), at a clock of 1.8 GHz; without the conversions the latter is no faster.
 #include "fp8_codes.h"
 
 namespace fqt {

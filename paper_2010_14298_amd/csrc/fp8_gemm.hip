@@ -203,11 +203,13 @@ __device__ __forceinline__ void interleave() {
 // number of stages, at least four).  The next tile's first two stages
 // are on their way before this one's outputs are stored, and loads behind the
 // stores are first waited for four segments later.  The load counter counts
-// stores as well, so until then the waits allow for STORES of them.  With one
-// block a tile / several, us: 8192 x 4096 x 1024 46.6 / 41.4, 8000 x 4096 x 1024
-// 45.5 / 42.0, 16000 x 4096 x 512 63.5 / 52.2, 8192 x 8192 x 1024 91.0 / 76.5, 8192 x 4096 x 512 32.8 / 30.6, 8192 x 8192 x 8192 448 / 438, 6144 x
-// 4096 x 1024 (one and a half tiles a unit) 42.0 / 42.5; float32 8192 x 4096 x
-// 1024 70.4 / 70.8, 4096 x 8192 x 1024 79.0 / 71.5, 8192^3 780 / 774.
+// stores as well, so until then the waits allow for STORES of them.  One block a
+// tile / several, with the pass that reads the outputs next, us: bfloat16 8192 x
+// 4096 x 1024 76.2 / 68.4, 8000 x 4096 x 1024 72.2 / 63.5, 16384 x 4096 x 512 118 /
+// 102, 5120 x 5120 x 1024 62.3 / 51.9, 8192 x 8192 x 8192 492 / 493, 6144 x 4096 x
+// 1024 (one and a half tiles a unit) 60.5 / 60.8; float32 8192 x 4096 x 1024 103.5 /
+// 99.6, 4096 x 8192 x 1024 114.3 / 99.2.  The product alone 44.7 / 39.5, 42.7 / 36.5,
+// 59.5 / 54.2, 39.0 / 32.3, 435 / 437, 39.7 / 39.2; 69.9 / 73.8, 77.2 / 75.0.
 template <class T, bool WIDE, bool NT, bool RUN>
 __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(Fp8GemmParams p) {
   using C = LargeTile;
@@ -386,7 +388,11 @@ __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(Fp8G
   auto store_all = [&](int64_t row0, int64_t col0) __attribute__((always_inline)) {
     if constexpr (RUN) {
       // STRIP rows at a time through LDS of their own, whole lines out of it;
-      // rows past the edge hold what the last row does and store it there again
+      // rows past the edge hold what the last row does and store it there again.
+      // Ordinary stores: nontemporal / ordinary with the pass that reads the
+      // outputs next, us: bfloat16 8192 x 4096 x 1024 70.1 / 68.8, 16384 x 4096 x
+      // 512 113.5 / 100.8, float32 8192 x 4096 x 1024 109 / 103, 8192 x 8192 x 1024
+      // 200 / 182; the product alone 40.4 / 39.2, 51.5 / 53.6, 70.4 / 73.6, 129 / 144.
       T* const strip = out[wave];
       const float least = p.relu ? 0.0f : -__builtin_huge_valf();
       const int lr = lane / (C::WN / V), lc = lane % (C::WN / V) * V;
@@ -407,7 +413,7 @@ __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(Fp8G
           typedef T vec __attribute__((ext_vector_type(V)));
           const vec v = *reinterpret_cast<const vec*>(strip + (V * h + lr) * STRIP_LD + lc);
           const int r = wm * C::WM + STRIP * i + V * h + lr;
-          __builtin_nontemporal_store(v, reinterpret_cast<vec*>(to + (r < last ? r : last) * p.ldc));
+          *reinterpret_cast<vec*>(to + (r < last ? r : last) * p.ldc) = v;
         }
         __builtin_amdgcn_wave_barrier();
       }
@@ -987,11 +993,11 @@ hipError_t launch_fp8_gemm(fqt_dtype type, const Fp8GemmParams& p, hipStream_t s
   return with_type(type, [&](auto e) {
     using T = decltype(e);
     constexpr bool WIDE = sizeof(T) == 4;
-    // Whole lines of outputs go past the caches.  Ordinary / nontemporal, with
-    // the pass that reads them next, us: bfloat16 and a quantizer 8192 x 4096 x 1024
-    // 76.3 / 75.6, 8192 x 6144 x 1024 115 / 105, 8192 x 1024 x 4096 44.8 / 43.4;
-    // float32 and a norm 4096 x 1024 x 8192 70.7 / 70.4, 3001 x 4096 x 4096 116 /
-    // 111, but 8192 x 4096 x 1024 104.8 / 110.  The product alone gains up to 18 %.
+    // Whole lines of outputs of one tile a block go past the caches.  Ordinary /
+    // nontemporal, with the pass that reads them next, us: bfloat16 and a quantizer
+    // 8192 x 1024 x 4096 44.8 / 43.4, 2048 x 4096 x 1024 26.5 / 25.1; float32 and a norm
+    // 4096 x 1024 x 8192 70.7 / 70.4, 3001 x 4096 x 4096 116 / 111, but 3001 x 4096 x
+    // 1024 47.1 / 48.2.
     const bool nt = (p.ldc * sizeof(T)) % 128 == 0 && ((uintptr_t)p.C & 127) == 0;
     const Plan plan = plan_of(p.M, p.N, p.K, WIDE);
     auto tiles = [&](auto c) {

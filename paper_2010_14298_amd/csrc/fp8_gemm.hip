@@ -17,10 +17,10 @@
 // product of the same sizes in the same run, without block scales and with
 // bfloat16 outputs:
 //                        bfloat16 outputs   8-bit library   float32 outputs   bfloat16 library
-//   8192 x 8192 x 8192      439 (2.50)          348            772 (1.42)          691
-//   8192 x 4096 x 1024       42 (1.64)           38             74 (0.93)           60
-//   8192 x 1024 x 4096       35 (1.95)           38             60 (1.15)           61
-//   4096 x 1024 x 8192       35 (1.98)           40             62 (1.12)           66
+//   8192 x 8192 x 8192      436 (2.52)          344            763 (1.44)          680
+//   8192 x 4096 x 1024       40 (1.74)           39             76 (0.91)           60
+//   8192 x 1024 x 4096       35 (1.96)           37             57 (1.20)           58
+//   4096 x 1024 x 8192       34 (2.05)           38             58 (1.18)           64
 // 8192 x 4096 x 1024 waits for the stores of its last tiles, which all units issue
 // at the same time.  In the longer products matrix instructions fill 50 % of the
 // cycles (bfloat16 outputs, 8192 x 1024 x 4096) and 57 % (float32, 4096 x 1024 x

@@ -203,7 +203,8 @@ __device__ __forceinline__ void interleave() {
 // number of stages, at least four).  The next tile's first two stages
 // are on their way before this one's outputs are stored, and loads behind the
 // stores are first waited for four segments later.  The load counter counts
-// stores as well, so until then the waits allow for STORES of them.  One block a
+// stores as well, in the order of issue, so until then the waits allow for
+// STORES of them (another access in between only makes them stricter).  One block a
 // tile / several, with the pass that reads the outputs next, us: bfloat16 8192 x
 // 4096 x 1024 76.2 / 68.4, 8000 x 4096 x 1024 72.2 / 63.5, 16384 x 4096 x 512 118 /
 // 102, 5120 x 5120 x 1024 62.3 / 51.9, 8192 x 8192 x 8192 492 / 493, 6144 x 4096 x

@@ -3,28 +3,27 @@
 //
 //   C[m, n] = sum over blocks b, k in b of A[m, k] 2^EA[m, b] B[n, k] 2^EB[n, b]
 //
-// Two ways through the matrix cores, by the output's type:
-//   16-bit outputs  v_mfma_scale_f32_32x32x64_f8f6f4 on the codes as they are;
-//     it applies both scales itself.  It drops the part of a product that lies
-//     more than 13 bits below the largest product summed with it: 1.5e-5 to
-//     7e-5 of the result (2-norm) against the output's own rounding of 1.7e-3.
-//   float32 outputs  the codes are converted to bfloat16 with their scale
-//     (v_cvt_scalef32_pk_bf16_fp8, exact) and go through
-//     v_mfma_f32_32x32x16_bf16 at half the rate, which sums to 1.5e-7.
-// The output is rounded once.
+// The codes are converted to bfloat16 with their scale
+// (v_cvt_scalef32_pk_bf16_fp8, exact) and go through v_mfma_f32_32x32x16_bf16,
+// whose sums are float32: 2e-8 to 1.5e-7 of the result (2-norm).  The output is
+// rounded once.  The matrix instructions that take the codes as they are
+// (v_mfma_scale_f32_32x32x64_f8f6f4 and the plain ones) run at twice the rate,
+// but they drop the part of a product that lies more than 13 bits below the
+// largest product summed with it: 65536 - 65536 + 4 gives 0.  That loses 1.5e-5
+// (normal data) to 7e-5 (one large element a block) of the result, and all of
+// one that is left over from large products that cancel, so no output takes
+// them: 8192 x 4096 x 1024 with bfloat16 outputs was 43 us with them, 66 without.
 //
 // Back to back on changing operands, us (PFLOP/s), M x N x K, and a library
-// product of the same sizes in the same run, without block scales and with
-// bfloat16 outputs:
-//                        bfloat16 outputs   8-bit library   float32 outputs   bfloat16 library
-//   8192 x 8192 x 8192      436 (2.52)          344            763 (1.44)          680
-//   8192 x 4096 x 1024       40 (1.74)           39             76 (0.91)           60
-//   8192 x 1024 x 4096       35 (1.96)           37             57 (1.20)           58
-//   4096 x 1024 x 8192       34 (2.05)           38             58 (1.18)           64
+// product of bfloat16 operands and outputs (no scales) in the same run:
+//                        bfloat16 outputs   float32 outputs   library
+//   8192 x 8192 x 8192      758 (1.45)         782 (1.41)        695
+//   8192 x 4096 x 1024       64 (1.07)          78 (0.88)         64
+//   8192 x 1024 x 4096       63 (1.08)          61 (1.14)         61
+//   4096 x 1024 x 8192       68 (1.00)          62 (1.11)         67
 // 8192 x 4096 x 1024 waits for the stores of its last tiles, which all units issue
-// at the same time.  In the longer products matrix instructions fill 50 % of the
-// cycles (bfloat16 outputs, 8192 x 1024 x 4096) and 57 % (float32, 4096 x 1024 x
-// 8192), at a clock of 1.8 GHz; without the conversions the latter is no faster.
+// at the same time.  In 4096 x 1024 x 8192 (float32) matrix instructions fill 57 %
+// of the cycles at a clock of 1.8 GHz; without the conversions it is no faster.
 #include "fp8_codes.h"
 
 namespace fqt {
@@ -124,8 +123,9 @@ __device__ __forceinline__ void store_strip(const Fp8GemmParams& p, const float*
   }
 }
 
-// Eight codes (two words) as bfloat16 times `scale`, a power of two: exact
-// where the result is at least 2^-126, the smallest normal number.
+// Eight codes (two words) as bfloat16 times `scale`, a power of two: exact for
+// scales from 2^-124 on; below, codes become multiples of 2^-133, bfloat16's
+// smallest step.
 __device__ __forceinline__ v8b widen(int w0, int w1, float scale) {
   const v2b a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, false);
   const v2b b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, true);
@@ -133,9 +133,9 @@ __device__ __forceinline__ v8b widen(int w0, int w1, float scale) {
   const v2b d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, true);
   return v8b{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
-// 2^E of the scale byte `sh` bits up in w (byte 0: 2^-127, a subnormal).
-__device__ __forceinline__ float scale_of(int w, int sh) {
-  const uint32_t b = ((uint32_t)w >> sh) & 255u;
+// 2^E of the scale byte in w's low bits (byte 0: 2^-127, a subnormal).
+__device__ __forceinline__ float scale_of(int w) {
+  const uint32_t b = (uint32_t)w & 255u;
   return __uint_as_float(b ? b << 23 : 0x400000u);
 }
 
@@ -206,12 +206,12 @@ __device__ __forceinline__ void interleave() {
 // stores as well, in the order of issue, so until then the waits allow for
 // STORES of them (another access in between only makes them stricter).  One block a
 // tile / several, with the pass that reads the outputs next, us: bfloat16 8192 x
-// 4096 x 1024 76.2 / 68.4, 8000 x 4096 x 1024 72.2 / 63.5, 16384 x 4096 x 512 118 /
-// 102, 5120 x 5120 x 1024 62.3 / 51.9, 8192 x 8192 x 8192 492 / 493, 6144 x 4096 x
-// 1024 (one and a half tiles a unit) 60.5 / 60.8; float32 8192 x 4096 x 1024 103.5 /
-// 99.6, 4096 x 8192 x 1024 114.3 / 99.2.  The product alone 44.7 / 39.5, 42.7 / 36.5,
-// 59.5 / 54.2, 39.0 / 32.3, 435 / 437, 39.7 / 39.2; 69.9 / 73.8, 77.2 / 75.0.
-template <class T, bool WIDE, bool NT, bool RUN>
+// 4096 x 1024 98 / 88, 8000 x 4096 x 1024 97 / 87, 16384 x 4096 x 512 144 / 123,
+// 5120 x 5120 x 1024 86 / 74, 8192 x 8192 x 8192 840 / 813, 6144 x 4096 x 1024
+// (one and a half tiles a unit) 84 / 83; float32 8192 x 4096 x 1024 108 / 104, 4096 x
+// 8192 x 1024 120 / 104.  The product alone 70 / 64, 67 / 61, 86 / 78, 62 / 54, 781 /
+// 762, 61 / 61; 74 / 78 (slower: its ordinary stores), 82 / 78.
+template <class T, bool NT, bool RUN>
 __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(Fp8GemmParams p) {
   using C = LargeTile;
   // separate arrays, so that a pending load into one does not hold up reads of another
@@ -302,33 +302,25 @@ __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(Fp8G
   };
   auto multiply = [&]() __attribute__((always_inline)) {
     __builtin_amdgcn_s_setprio(1);
-    if constexpr (!WIDE) {
+    float fa[C::IT], fb[C::JT];
+#pragma unroll
+    for (int i = 0; i < C::IT; ++i) fa[i] = scale_of(sa[i]);
+#pragma unroll
+    for (int j = 0; j < C::JT; ++j) fb[j] = scale_of(sb[j]);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      v8b wa[C::IT], wb[C::JT];
+#pragma unroll
+      for (int j = 0; j < C::JT; ++j) wb[j] = widen(b[j][2 * q], b[j][2 * q + 1], fb[j]);
+#pragma unroll
+      for (int i = 0; i < C::IT; ++i) wa[i] = widen(a[i][2 * q], a[i][2 * q + 1], fa[i]);
 #pragma unroll
       for (int i = 0; i < C::IT; ++i)
 #pragma unroll
         for (int j = 0; j < C::JT; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a[i], b[j], acc[i][j], 0, 0, 0, sa[i], 0, sb[j]);
-    } else {
-      float fa[C::IT], fb[C::JT];
-#pragma unroll
-      for (int i = 0; i < C::IT; ++i) fa[i] = scale_of(sa[i], 0);
-#pragma unroll
-      for (int j = 0; j < C::JT; ++j) fb[j] = scale_of(sb[j], 0);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        v8b wa[C::IT], wb[C::JT];
-#pragma unroll
-        for (int j = 0; j < C::JT; ++j) wb[j] = widen(b[j][2 * q], b[j][2 * q + 1], fb[j]);
-#pragma unroll
-        for (int i = 0; i < C::IT; ++i) wa[i] = widen(a[i][2 * q], a[i][2 * q + 1], fa[i]);
-#pragma unroll
-        for (int i = 0; i < C::IT; ++i)
-#pragma unroll
-          for (int j = 0; j < C::JT; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wa[i], wb[j], acc[i][j], 0, 0, 0);
-      }
-      interleave<4, C::IT * C::JT, 4 * (C::IT + C::JT)>();
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wa[i], wb[j], acc[i][j], 0, 0, 0);
     }
+    interleave<4, C::IT * C::JT, 4 * (C::IT + C::JT)>();
     __builtin_amdgcn_s_setprio(0);
     // the products belong to this segment: keep the compiler from moving them past the barrier
 #pragma unroll
@@ -391,9 +383,10 @@ __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(Fp8G
       // STRIP rows at a time through LDS of their own, whole lines out of it;
       // rows past the edge hold what the last row does and store it there again.
       // Ordinary stores: nontemporal / ordinary with the pass that reads the
-      // outputs next, us: bfloat16 8192 x 4096 x 1024 70.1 / 68.8, 16384 x 4096 x
-      // 512 113.5 / 100.8, float32 8192 x 4096 x 1024 109 / 103, 8192 x 8192 x 1024
-      // 200 / 182; the product alone 40.4 / 39.2, 51.5 / 53.6, 70.4 / 73.6, 129 / 144.
+      // outputs next, us: bfloat16 8192 x 4096 x 1024 93 / 88, 16384 x 4096 x 512
+      // 134 / 124, float32 8192 x 4096 x 1024 110 / 104, 8192 x 8192 x 1024 208 / 190;
+      // the product alone 63 / 63, 74 / 78, 75 / 77, 134 / 149.  An output that is
+      // read only much later, as a weight gradient may be, loses by them.
       T* const strip = out[wave];
       const float least = p.relu ? 0.0f : -__builtin_huge_valf();
       const int lr = lane / (C::WN / V), lc = lane % (C::WN / V) * V;
@@ -521,8 +514,8 @@ struct PipeTile {
   static_assert(PLANE * KG == 8 && E_SEGS <= 8 && NS >= 2 && NS <= 4, "eight waves");
 };
 
-// WIDE: through bfloat16.  T: the stored type (SPLIT: float).
-template <class T, class C, bool WIDE, bool SPLIT, bool NT>
+// T: the stored type (SPLIT: float).
+template <class T, class C, bool SPLIT, bool NT>
 __global__ __launch_bounds__(512) void fp8_gemm_pipe_kernel(Fp8GemmParams p, int chunk) {
   __shared__ __attribute__((aligned(16))) uint8_t q0[C::CODES], q1[C::CODES], q2[C::NS > 2 ? C::CODES : 16],
       q3[C::NS > 3 ? C::CODES : 16];
@@ -596,32 +589,23 @@ __global__ __launch_bounds__(512) void fp8_gemm_pipe_kernel(Fp8GemmParams p, int
     }
   };
   auto multiply = [&](const Operands& o) __attribute__((always_inline)) {
-    if constexpr (!WIDE) {
+    float fa[C::IT], fb[C::JT];
+#pragma unroll
+    for (int i = 0; i < C::IT; ++i) fa[i] = scale_of(o.sa[i]);
+#pragma unroll
+    for (int j = 0; j < C::JT; ++j) fb[j] = scale_of(o.sb[j]);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      v8b wa[C::IT], wb[C::JT];
+#pragma unroll
+      for (int j = 0; j < C::JT; ++j) wb[j] = widen(o.b[j][2 * q], o.b[j][2 * q + 1], fb[j]);
+#pragma unroll
+      for (int i = 0; i < C::IT; ++i) wa[i] = widen(o.a[i][2 * q], o.a[i][2 * q + 1], fa[i]);
 #pragma unroll
       for (int i = 0; i < C::IT; ++i)
 #pragma unroll
         for (int j = 0; j < C::JT; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(o.a[i], o.b[j], acc[i][j], 0, 0, 0, o.sa[i], 0,
-                                                                      o.sb[j]);
-    } else {
-      float fa[C::IT], fb[C::JT];
-#pragma unroll
-      for (int i = 0; i < C::IT; ++i) fa[i] = scale_of(o.sa[i], 0);
-#pragma unroll
-      for (int j = 0; j < C::JT; ++j) fb[j] = scale_of(o.sb[j], 0);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        v8b wa[C::IT], wb[C::JT];
-#pragma unroll
-        for (int j = 0; j < C::JT; ++j) wb[j] = widen(o.b[j][2 * q], o.b[j][2 * q + 1], fb[j]);
-#pragma unroll
-        for (int i = 0; i < C::IT; ++i) wa[i] = widen(o.a[i][2 * q], o.a[i][2 * q + 1], fa[i]);
-#pragma unroll
-        for (int i = 0; i < C::IT; ++i)
-#pragma unroll
-          for (int j = 0; j < C::JT; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wa[i], wb[j], acc[i][j], 0, 0, 0);
-      }
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wa[i], wb[j], acc[i][j], 0, 0, 0);
     }
 #pragma unroll
     for (int i = 0; i < C::IT; ++i)
@@ -794,9 +778,9 @@ __global__ __launch_bounds__(256) void fp8_split_sum_kernel(Fp8GemmParams p, int
 // registers once, 16 outputs a block, its waves take every eighth block of K
 // and add up in LDS.  A from raw rows (X is quantized here, in registers: every
 // block of threads needs all of it, but it is small) or from codes.
-// v_mfma_scale_f32_16x16x128_f8f6f4: lane l holds row l % 16, codes
-// 32 (l / 16) .. + 31 of a block.  Latency bounds it: one bfloat16 row through
-// 4096 x 1024 weights (4.2 MB) takes 3.9 us.
+// Lane l holds row l % 16, codes 32 (l / 16) .. + 31 of a block, eight of them a
+// v_mfma_f32_16x16x32_bf16.  Latency bounds it: one bfloat16 row through 4096 x
+// 1024 weights (4.2 MB) takes 4.0 us.
 // ---------------------------------------------------------------------------
 constexpr int ROW_WAVES = 8;
 
@@ -875,15 +859,11 @@ __global__ __launch_bounds__(64 * ROW_WAVES) void fp8_rows_kernel(Fp8GemmParams 
         const int64_t at = (int64_t)k * FP8_BLOCK + 32 * g;
         a = row_block(static_cast<const X*>(x) + (row < p.M ? row : 0) * ldx + at, row < p.M ? p.K - at : 0, sa);
       }
-      if constexpr (sizeof(T) == 2) {
-        acc[m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, acc[m], 0, 0, 0, sb, 0, sa);
-      } else {
-        const float fa = scale_of(sa, 0), fb = scale_of(sb, 0);
+      const float fa = scale_of(sa), fb = scale_of(sb);
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(b[2 * q], b[2 * q + 1], fb),
-                                                           widen(a[2 * q], a[2 * q + 1], fa), acc[m], 0, 0, 0);
-      }
+      for (int q = 0; q < 4; ++q)
+        acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(b[2 * q], b[2 * q + 1], fb),
+                                                         widen(a[2 * q], a[2 * q + 1], fa), acc[m], 0, 0, 0);
     }
   }
   // lane: output columns n0 + 4 g .., row r
@@ -909,6 +889,11 @@ __global__ __launch_bounds__(64 * ROW_WAVES) void fp8_rows_kernel(Fp8GemmParams 
 // ---------------------------------------------------------------------------
 using MidTile = PipeTile<256, 128, 64, 64, 1, 3>;
 using SmallTile = PipeTile<128, 128, 64, 64, 2, 4>;
+// For 16-bit outputs: sums in the order of the larger tiles, so that a row of an
+// activation has the same bits whichever tile the number of rows leads to.
+// Halves of K / one order, us: 2048 x 4096 x 1024 24.2 / 24.1, 300 x 1024 x 512
+// 9.0 / 8.7, 1024 x 1024 x 4096 21.0 / 21.0, 4096 x 1024 x 8192 67 / 72.
+using SmallTile16 = PipeTile<128, 128, 64, 32, 1, 4>;
 
 static int64_t tiles_of(int64_t M, int64_t N, int64_t bm, int64_t bn) {
   return ((M + bm - 1) / bm) * ((N + bn - 1) / bn);
@@ -917,23 +902,23 @@ static int64_t tiles_of(int64_t M, int64_t N, int64_t bm, int64_t bn) {
 // Which tile, and for small tiles into how many parts along K the product is
 // split: the least estimated time of turns x (stages x c + t0), turns the
 // tiles (times parts) over 256 units of one block each, plus the pass that adds
-// the parts.  Measured on one product a turn (us a stage of 128, 16-bit /
-// float32 outputs): small 0.53 / 0.94 (4096 x 1024 x 8192), mid 1.05 / 1.77
-// (8192 x 1024 x 4096), large 1.85 / 3.3 (4096 x 4096 x 4096).
+// the parts.  Measured on one product a turn (us a stage of 128): small 0.94
+// (4096 x 1024 x 8192), mid 1.77 (8192 x 1024 x 4096), large 3.3 (4096 x 4096 x
+// 4096).
 // Every product with each tile, us, large / mid / small, the choice first:
-//   8192 x 4096 x 1024 bfloat16  large 41.4   (41.4 / 57.7 / 73.8)
-//   8192 x 1024 x 4096 bfloat16  mid   38.3   (44.7 / 37.1 / 43.9)
-//   4096 x 1024 x 8192 float32   small 63.0   (142 / 84.9 / 61.8)
-//   3001 x 1024 x 4096 float32   small 30.3   (75.8 / 46.8 / 30.3)
-//   250 x 1001 x 2048 float32    split 13.3   (41.9 / 25.7 / 16.4)
-//   130 x 260 x 8192 float32     split 15.5   (139 / 82.2 / 48.6)
+//   8192 x 4096 x 1024 bfloat16  large 64     (67 / 83 / 101)
+//   8192 x 1024 x 4096 bfloat16  mid   63     (83 / 63 / 76)
+//   4096 x 1024 x 8192 float32   small 65     (145 / 87 / 64)
+//   3001 x 1024 x 4096 float32   small 32     (78 / 46 / 32)
+//   250 x 1001 x 2048 float32    split 13.4   (45.6 / 25.8 / 16.6)
+//   130 x 260 x 8192 float32     split 15.6   (142 / 82 / 48.7)
 struct Plan {
   enum Tile { SMALL, MID, LARGE } tile;
   int splits, chunk;  // parts along K, stages of each
 };
-static Plan plan_of(int64_t M, int64_t N, int64_t K, bool wide) {
+static Plan plan_of(int64_t M, int64_t N, int64_t K) {
   const int64_t nk = fp8_blocks(K);
-  const double c[3] = {wide ? 0.94 : 0.53, wide ? 1.77 : 1.05, wide ? 3.3 : 1.85}, t0[3] = {4.0, 5.0, 8.0};
+  const double c[3] = {0.94, 1.77, 3.3}, t0[3] = {4.0, 5.0, 8.0};
   auto turns = [](int64_t blocks) { return (double)((blocks + 255) / 256); };
   const int64_t small = tiles_of(M, N, SmallTile::BM, SmallTile::BN);
   Plan best{Plan::LARGE, 1, (int)nk};
@@ -957,21 +942,17 @@ static Plan plan_of(int64_t M, int64_t N, int64_t K, bool wide) {
 }
 
 // Up to 64 rows stream the weights (fp8_rows_kernel): 17 x 4096 x 1024 bfloat16
-// 3.4 us, in small tiles 7.7; 64 x 4096 x 1024 5.0, 8.2; 64 x 1024 x 4096 float32 12.2,
-// 14.2.  Up to 16 rows are quantized there as well: 1024 -> 4096 bfloat16, one row
-// 3.9 us, 7.1 with a quantizer's launch before it, 16 rows 4.6, 8.4; 16 rows
-// of 4096 -> 1024 11.0, 11.3.
+// 3.6 us, in small tiles 10.5; 64 x 4096 x 1024 5.1, 11.1; 64 x 1024 x 4096 float32
+// 12.2, 14.1.  Up to 16 rows are quantized there as well: 1024 -> 4096 bfloat16, one
+// row 4.0 us, 7.1 with a quantizer's launch before it, 16 rows 4.7, 8.5; 16 rows
+// of 4096 -> 1024 11.2, 11.4.
 constexpr int64_t ROWS_MAX = 64, ROWS_RAW_MAX = 16;
 bool fp8_rows_raw(int64_t M) { return M <= ROWS_RAW_MAX; }
 
 int64_t fp8_gemm_partials(int64_t M, int64_t N, int64_t K) {
   if (M <= ROWS_MAX) return 0;
-  int64_t s = 0;
-  for (bool wide : {false, true}) {
-    const Plan p = plan_of(M, N, K, wide);
-    if (p.splits > 1 && p.splits > s) s = p.splits;
-  }
-  return s * M * N;
+  const int64_t s = plan_of(M, N, K).splits;
+  return s > 1 ? s * M * N : 0;
 }
 
 hipError_t launch_fp8_rows(fqt_dtype type, const Fp8GemmParams& p, const void* x, int64_t ldx, hipStream_t s) {
@@ -993,14 +974,13 @@ hipError_t launch_fp8_gemm(fqt_dtype type, const Fp8GemmParams& p, hipStream_t s
   if (p.M <= ROWS_MAX) return launch_fp8_rows(type, p, nullptr, 0, s);
   return with_type(type, [&](auto e) {
     using T = decltype(e);
-    constexpr bool WIDE = sizeof(T) == 4;
     // Whole lines of outputs of one tile a block go past the caches.  Ordinary /
     // nontemporal, with the pass that reads them next, us: bfloat16 and a quantizer
-    // 8192 x 1024 x 4096 44.8 / 43.4, 2048 x 4096 x 1024 26.5 / 25.1; float32 and a norm
-    // 4096 x 1024 x 8192 70.7 / 70.4, 3001 x 4096 x 4096 116 / 111, but 3001 x 4096 x
-    // 1024 47.1 / 48.2.
+    // 8192 x 1024 x 4096 74.4 / 74.4, 2048 x 4096 x 1024 33.0 / 31.7; float32 and a norm
+    // 4096 x 1024 x 8192 76.8 / 74.8, 3001 x 4096 x 4096 119 / 115, 3001 x 4096 x 1024
+    // 51.1 / 47.9.
     const bool nt = (p.ldc * sizeof(T)) % 128 == 0 && ((uintptr_t)p.C & 127) == 0;
-    const Plan plan = plan_of(p.M, p.N, p.K, WIDE);
+    const Plan plan = plan_of(p.M, p.N, p.K);
     auto tiles = [&](auto c) {
       using C = decltype(c);
       return tiles_of(p.M, p.N, C::BM, C::BN);
@@ -1015,17 +995,18 @@ hipError_t launch_fp8_gemm(fqt_dtype type, const Fp8GemmParams& p, hipStream_t s
     if (plan.tile == Plan::LARGE) {
       if (nt && blocks > 256 && p.N % LargeTile::BN == 0 && !p.mask && plan.chunk % 2 == 0 && plan.chunk >= 4) {
         grid = 256;  // one block a unit
-        return go(fp8_gemm_large_kernel<T, WIDE, true, true>);
+        return go(fp8_gemm_large_kernel<T, true, true>);
       }
-      return nt ? go(fp8_gemm_large_kernel<T, WIDE, true, false>) : go(fp8_gemm_large_kernel<T, WIDE, false, false>);
+      return nt ? go(fp8_gemm_large_kernel<T, true, false>) : go(fp8_gemm_large_kernel<T, false, false>);
     }
     if (plan.tile == Plan::MID)
-      return nt ? go(fp8_gemm_pipe_kernel<T, MidTile, WIDE, false, true>, plan.chunk)
-                : go(fp8_gemm_pipe_kernel<T, MidTile, WIDE, false, false>, plan.chunk);
+      return nt ? go(fp8_gemm_pipe_kernel<T, MidTile, false, true>, plan.chunk)
+                : go(fp8_gemm_pipe_kernel<T, MidTile, false, false>, plan.chunk);
+    using Small = std::conditional_t<sizeof(T) == 2, SmallTile16, SmallTile>;
     if (plan.splits == 1)
-      return nt ? go(fp8_gemm_pipe_kernel<T, SmallTile, WIDE, false, true>, plan.chunk)
-                : go(fp8_gemm_pipe_kernel<T, SmallTile, WIDE, false, false>, plan.chunk);
-    const hipError_t err = go(fp8_gemm_pipe_kernel<float, SmallTile, WIDE, true, false>, plan.chunk);
+      return nt ? go(fp8_gemm_pipe_kernel<T, Small, false, true>, plan.chunk)
+                : go(fp8_gemm_pipe_kernel<T, Small, false, false>, plan.chunk);
+    const hipError_t err = go(fp8_gemm_pipe_kernel<float, SmallTile, true, false>, plan.chunk);
     if (err != hipSuccess) return err;
     const int64_t quads = p.M * ((p.N + 3) / 4);
     hipLaunchKernelGGL((fp8_split_sum_kernel<T>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, s, p, plan.splits);

@@ -1,7 +1,6 @@
 // Block quantizer to 8-bit floating point (4 exponent bits, 3 mantissa bits,
 // largest value 448): codes with one power-of-two scale for each block of
-// 128 along the contraction, as the matrix cores' scaled instruction reads
-// them.
+// 128 along the contraction, as the products read them.
 //
 //   E = the least integer >= -127 with max|block| <= 448 2^E (0: empty block)
 //   y = x 2^-E (exact),  code = the format's value nearest to y, ties to even,

@@ -196,8 +196,8 @@ __global__ __launch_bounds__(C::THREADS) void norm_backward_kernel(NormParams p)
       if (p.gamma) load_part<float, C::VEC>(p.gamma + col, (int)p.cols - col, ga);
 #pragma unroll
       for (int i = 0; i < C::VEC; ++i) {
-        // columns past the end have g = 0, so whatever xh is there adds nothing
-        xh[k][i] = (xh[k][i] - mean) * rstd;
+        // no column (or no row): xh is 0 like g, since (0 - mean) rstd may be infinite
+        xh[k][i] = col + i < cols ? (xh[k][i] - mean) * rstd : 0.0f;
         sg[k][i] = fmaf(gv[k][i], xh[k][i], sg[k][i]);
         sb[k][i] += gv[k][i];
         gv[k][i] *= ga[i];
@@ -274,9 +274,10 @@ __global__ __launch_bounds__(C::THREADS) void norm_backward_long_kernel(NormPara
     load_part<T, C::VEC>(g + col, p.cols - col, gv);
 #pragma unroll
     for (int i = 0; i < C::VEC; ++i) {
-      const float c = gv[i] * (p.gamma && col + i < p.cols ? p.gamma[col + i] : 1.0f);
+      const bool in = col + i < p.cols;
+      const float c = gv[i] * (p.gamma && in ? p.gamma[col + i] : 1.0f);
       s[0] += c;
-      s[1] = fmaf(c, (xv[i] - mean) * rstd, s[1]);
+      s[1] = fmaf(c, in ? (xv[i] - mean) * rstd : 0.0f, s[1]);  // (0 - mean) rstd may be infinite
     }
   }
   team_sum<C, 2>(s, sh);

@@ -441,7 +441,7 @@ size_t fqt_fp8_linear_backward_workspace(int64_t N, int64_t d_in, int64_t d_out)
  * arrays, read before the call returns; outs NULL or outs[i] = grads[i]: in
  * place, and nothing is written where nothing is clipped.  norm (device, may
  * be NULL) receives n.  Squares are summed in float64 in a fixed order.  A
- * norm that is not finite scales nothing.  max_norm > 0 (infinity: only the
+ * norm that is not finite in float32 scales nothing.  max_norm > 0 (infinity: only the
  * norm).  168 tensors in a row of more than 2^45 bytes return FQT_EUNSUPPORTED. */
 fqt_status fqt_grad_norm_clip(const void* const* grads, void* const* outs, const int64_t* sizes, const int32_t* types,
                               int64_t count, double max_norm, float* norm, void* ws, size_t ws_bytes, fqt_stream_t s);

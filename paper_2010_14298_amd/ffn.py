@@ -55,16 +55,21 @@ class FeedForward:
         return [dW1, dW2, dgamma, dbeta], dX + dY
 
     def step(self, X, target, lr, max_norm, seed):
-        """One training step on 1/2 mean |Y - target|^2; returns (loss, gradient norm), device scalars."""
+        """One training step on 1/2 mean |Y - target|^2; returns (loss, gradient norm), device scalars.
+
+        The backward runs on the loss times the power of two next to its number of elements: float16 would lose
+        diff / numel below its smallest step.  The float32 gradients of the parameters are larger by as much, exactly,
+        which the bound, the update and the norm take out again."""
         Y, kept = self.forward(X)
         diff = Y.float() - target.float()
         loss = 0.5 * diff.square().mean()
-        grads, _ = self.backward((diff / diff.numel()).to(self.dtype), kept, seed)
-        norm, _ = fqt.fqt_grad_norm_clip(grads, max_norm)
+        scale = 2.0 ** (diff.numel() - 1).bit_length()
+        grads, _ = self.backward((diff / diff.numel() * scale).to(self.dtype), kept, seed)
+        norm, _ = fqt.fqt_grad_norm_clip(grads, max_norm * scale)
         for p, g in zip(self.parameters(), grads):
-            p.add_(g, alpha=-lr)
+            p.add_(g, alpha=-lr / scale)
         self.quantize()
-        return loss, norm
+        return loss, norm / scale
 
 
 def main(argv=None):

@@ -488,6 +488,13 @@ def _matrix(x, name, dev, shape=None, dtype=None):
     return x.data_ptr(), dt, rows, cols, ld if rows > 1 else max(ld, cols)
 
 
+def _room(ws, dev):
+    """A caller's workspace, checked: kernels write to as many bytes as it has elements."""
+    if ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.get_device() != dev:
+        raise ValueError("ws must be a contiguous uint8 tensor on the current CUDA device")
+    return ws
+
+
 def _vector(x, name, n, dev):
     """Pointer of a contiguous float32 [n] tensor (None: NULL)."""
     if x is None:
@@ -533,6 +540,8 @@ def fqt_layernorm_backward(G, X, mean, rstd, gamma=None, grad_X=None, params=Tru
         py, _, _, _, ldgx = _matrix(grad_X, "grad_X", dev, G.shape, G.dtype)
     lib = load()
     gg = gb = pgg = pgb = None
+    if ws is not None:
+        _room(ws, dev)
     if params:
         gg, gb = G.new_empty((2, cols), dtype=torch.float32).unbind(0)
         pgg, pgb = gg.data_ptr(), gb.data_ptr()
@@ -607,6 +616,8 @@ def fqt_fp8_gemm(A, B, dtype=torch.float32, relu=False, mask=None, C=None, ws=No
     pm, _, _, _, ldm = _matrix(mask, "mask", dev, (M, N), C.dtype) if mask is not None else (None,) * 4 + (0,)
     if ws is None:
         ws = _workspace(fqt_fp8_gemm_workspace(M, N, K), C.device)
+    else:
+        _room(ws, dev)
     rc = load().fqt_fp8_gemm(_fp8(A, "A", dev), _fp8(B, "B", dev, N, K), M, N, K, dt, int(bool(relu)), pm, ldm, pc, ldc,
                              ws.data_ptr(), ws.numel(), _raw_stream(dev))
     _check("fqt_fp8_gemm", rc)
@@ -633,6 +644,8 @@ def fqt_fp8_linear_forward(X, W8, relu=False, save=True, Y=None, ws=None):
     lib = load()
     if ws is None:
         ws = X.new_empty(lib.fqt_fp8_linear_forward_workspace(N, d_in, d_out), dtype=torch.uint8)
+    else:
+        _room(ws, dev)
     rc = lib.fqt_fp8_linear_forward(px, dt, N, d_in, ldx, w8, d_out, int(bool(relu)), py, ldy, x8t, ws.data_ptr(),
                                     ws.numel(), _raw_stream(dev))
     _check("fqt_fp8_linear_forward", rc)
@@ -671,6 +684,8 @@ def fqt_fp8_linear_backward(G, X8t, W8t, seed=0, stochastic=True, relu_input=Non
     lib = load()
     if ws is None:
         ws = G.new_empty(lib.fqt_fp8_linear_backward_workspace(N, d_in, d_out), dtype=torch.uint8)
+    else:
+        _room(ws, dev)
     rc = lib.fqt_fp8_linear_backward(pg, dt, N, d_out, ldg, x8t, w8t, d_in, int(bool(stochastic)), seed, pr, ldr,
                                      _here(grad_W, "grad_W", dev).data_ptr(), px, ldgx, ws.data_ptr(), ws.numel(),
                                      _raw_stream(dev))
@@ -708,6 +723,8 @@ def fqt_grad_norm_clip(grads, max_norm, outs=None, ws=None):
     norm = torch.empty((), dtype=torch.float32, device=torch.device("cuda", dev))
     if ws is None:
         ws = _workspace(fqt_grad_norm_clip_workspace(count), norm.device)
+    else:
+        _room(ws, dev)
     rc = load().fqt_grad_norm_clip(g.buffer_info()[0], o.buffer_info()[0] if o is not None else None,
                                    n.buffer_info()[0], ty.buffer_info()[0], count, max_norm, norm.data_ptr(),
                                    ws.data_ptr(), ws.numel(), _raw_stream(dev))

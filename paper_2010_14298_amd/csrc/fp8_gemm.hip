@@ -511,15 +511,15 @@ struct PipeTile {
   static constexpr int INS = (BM + BN) / 64;                            // 1 KB loads of a wave and stage, eight rows each
   static constexpr int E_SEGS = (BM + BN) / 64;
   static constexpr int OUT_LD = WN + 8;
-  static_assert(PLANE * KG == 8 && E_SEGS <= 8 && NS >= 2 && NS <= 4, "eight waves");
+  static_assert(PLANE * KG == 8 && E_SEGS <= 8, "eight waves");
+  static_assert(NS == 4 || (NS == 3 && KG == 1), "an even number of steps a turn");
 };
 
 // T: the stored type (SPLIT: float).
 template <class T, class C, bool SPLIT, bool NT>
 __global__ __launch_bounds__(512) void fp8_gemm_pipe_kernel(Fp8GemmParams p, int chunk) {
-  __shared__ __attribute__((aligned(16))) uint8_t q0[C::CODES], q1[C::CODES], q2[C::NS > 2 ? C::CODES : 16],
-      q3[C::NS > 3 ? C::CODES : 16];
-  __shared__ int x0[C::BM + C::BN], x1[C::BM + C::BN], x2[C::NS > 2 ? C::BM + C::BN : 4], x3[C::NS > 3 ? C::BM + C::BN : 4];
+  __shared__ __attribute__((aligned(16))) uint8_t q0[C::CODES], q1[C::CODES], q2[C::CODES], q3[C::NS > 3 ? C::CODES : 16];
+  __shared__ int x0[C::BM + C::BN], x1[C::BM + C::BN], x2[C::BM + C::BN], x3[C::NS > 3 ? C::BM + C::BN : 4];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kg = wave / C::PLANE, wm = wave % C::PLANE / C::WAVES_N, wn = wave % C::WAVES_N;
@@ -627,7 +627,7 @@ __global__ __launch_bounds__(512) void fp8_gemm_pipe_kernel(Fp8GemmParams p, int
       const int later = nk - t - 2;  // stages behind t + 1 that are under way
       if (C::NS > 3 && later >= 2)
         wait_loads<2 * PER>();
-      else if (C::NS > 2 && later >= 1)
+      else if (later >= 1)
         wait_loads<PER>();
       else
         wait_loads<0>();
@@ -640,7 +640,7 @@ __global__ __launch_bounds__(512) void fp8_gemm_pipe_kernel(Fp8GemmParams p, int
   };
   load(q0, x0, 0);
   if (nk > 1) load(q1, x1, 1);
-  if (C::NS > 2 && nk > 2) load(q2, x2, 2);
+  if (nk > 2) load(q2, x2, 2);
   if (C::NS > 3 && nk > 3) load(q3, x3, 3);
   if (nk >= C::NS)
     wait_loads<(C::NS - 1) * PER>();
@@ -659,28 +659,17 @@ __global__ __launch_bounds__(512) void fp8_gemm_pipe_kernel(Fp8GemmParams p, int
                   __attribute__((always_inline)) {
       if (in || t + k < nk) stage(in, t + k, c, n, q, e, qn, en);
     };
-    if constexpr (C::NS == 2) {
-      go(0, set0, set1, q0, x0, q1, x1);
-      go(1, odd, even, q1, x1, q0, x0);
-    } else if constexpr (C::NS == 3) {
-      go(0, set0, set1, q0, x0, q1, x1);
-      go(1, odd, even, q1, x1, q2, x2);
+    go(0, set0, set1, q0, x0, q1, x1);
+    go(1, odd, even, q1, x1, q2, x2);
+    if constexpr (C::NS == 3) {
       go(2, set0, set1, q2, x2, q0, x0);
-      if constexpr (C::STEPS == 1) {
-        go(3, odd, even, q0, x0, q1, x1);
-        go(4, set0, set1, q1, x1, q2, x2);
-        go(5, odd, even, q2, x2, q0, x0);
-      }
     } else {
-      go(0, set0, set1, q0, x0, q1, x1);
-      go(1, odd, even, q1, x1, q2, x2);
       go(2, set0, set1, q2, x2, q3, x3);
       go(3, odd, even, q3, x3, q0, x0);
     }
   };
-  constexpr int TURN = C::NS == 3 && C::STEPS == 1 ? 6 : C::NS;  // stages of a turn
-  for (; t + TURN - 1 + C::NS < nk; t += TURN) turn(inner);
-  for (; t < nk; t += TURN) turn(last);
+  for (; t + 2 * C::NS - 1 < nk; t += C::NS) turn(inner);
+  for (; t < nk; t += C::NS) turn(last);
   __syncthreads();
   if constexpr (C::KG == 2) {
     // the two halves of K: each wave hands half of its rows to its partner

@@ -103,9 +103,6 @@ struct AddF {
     return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
   }
 };
-struct MaxU {
-  __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return a > b ? a : b; }
-};
 __device__ __forceinline__ float wave_sum(float v) { return __uint_as_float(wave_reduce(__float_as_uint(v), AddF{})); }
 
 // ---------------------------------------------------------------------------

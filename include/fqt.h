@@ -411,6 +411,21 @@ fqt_status fqt_fp8_gemm(const fqt_fp8* A, const fqt_fp8* B, int64_t M, int64_t N
                         fqt_stream_t s);
 size_t fqt_fp8_gemm_workspace(int64_t M, int64_t N, int64_t K);
 
+/* Which of its forms a product takes (the layers' products too): few rows of A
+ * against streamed weights; tiles of 128 x 128, also in parts along K; tiles of
+ * 256 x 128; tiles of 256 x 256, also several of them a block.  masked: there
+ * is a mask; lines: C and its pitch are multiples of 128 bytes.  -1 for sizes
+ * that the product refuses.  A host-side query: nothing is launched.         */
+typedef enum {
+  FQT_FP8_ROWS = 0,
+  FQT_FP8_SMALL = 1,
+  FQT_FP8_PARTS = 2,
+  FQT_FP8_MIDDLE = 3,
+  FQT_FP8_LARGE = 4,
+  FQT_FP8_SEVERAL = 5
+} fqt_fp8_form;
+int32_t fqt_fp8_gemm_form(int64_t M, int64_t N, int64_t K, int masked, int lines);
+
 /* Linear layer forward in 8-bit floating point: Y [N, d_out] = Q(X) W8^T with
  * X [N, d_in] quantized here to nearest in blocks of 1 x 128 and W8 [d_out,
  * K = d_in] the weights' codes (fqt_fp8_quantize with tile, by_row);

@@ -242,6 +242,11 @@ fqt_status fqt_fp8_gemm(const fqt_fp8* A, const fqt_fp8* B, int64_t M, int64_t N
   return FQT_OK;
 }
 
+int32_t fqt_fp8_gemm_form(int64_t M, int64_t N, int64_t K, int masked, int lines) {
+  if (!side(M) || !side(N) || !side(K) || K > MAX_CONTRACTION) return -1;
+  return fp8_gemm_form(M, N, K, masked != 0, lines != 0);
+}
+
 size_t fqt_fp8_linear_forward_workspace(int64_t N, int64_t d_in, int64_t d_out) {
   if (!side(N) || !side(d_in) || !side(d_out)) return 0;
   Carver c(nullptr);

@@ -938,6 +938,24 @@ static Plan plan_of(int64_t M, int64_t N, int64_t K) {
 constexpr int64_t ROWS_MAX = 64, ROWS_RAW_MAX = 16;
 bool fp8_rows_raw(int64_t M) { return M <= ROWS_RAW_MAX; }
 
+// Blocks of the large tile that stay for several: more whole tiles of columns
+// than units, an even number of stages, no mask, outputs in whole lines.
+static bool several_tiles(const Plan& plan, int64_t M, int64_t N, bool masked, bool lines) {
+  return plan.tile == Plan::LARGE && lines && !masked && tiles_of(M, N, LargeTile::BM, LargeTile::BN) > 256 &&
+         N % LargeTile::BN == 0 && plan.chunk % 2 == 0 && plan.chunk >= 4;
+}
+
+fqt_fp8_form fp8_gemm_form(int64_t M, int64_t N, int64_t K, bool masked, bool lines) {
+  if (M <= ROWS_MAX) return FQT_FP8_ROWS;
+  const Plan plan = plan_of(M, N, K);
+  switch (plan.tile) {
+    case Plan::SMALL: return plan.splits > 1 ? FQT_FP8_PARTS : FQT_FP8_SMALL;
+    case Plan::MID: return FQT_FP8_MIDDLE;
+    case Plan::LARGE: break;
+  }
+  return several_tiles(plan, M, N, masked, lines) ? FQT_FP8_SEVERAL : FQT_FP8_LARGE;
+}
+
 int64_t fp8_gemm_partials(int64_t M, int64_t N, int64_t K) {
   if (M <= ROWS_MAX) return 0;
   const int64_t s = plan_of(M, N, K).splits;
@@ -982,7 +1000,7 @@ hipError_t launch_fp8_gemm(fqt_dtype type, const Fp8GemmParams& p, hipStream_t s
       return hipGetLastError();
     };
     if (plan.tile == Plan::LARGE) {
-      if (nt && blocks > 256 && p.N % LargeTile::BN == 0 && !p.mask && plan.chunk % 2 == 0 && plan.chunk >= 4) {
+      if (several_tiles(plan, p.M, p.N, p.mask != nullptr, nt)) {
         grid = 256;  // one block a unit
         return go(fp8_gemm_large_kernel<T, true, true>);
       }

@@ -182,6 +182,7 @@ struct Fp8GemmParams {
 bool fp8_rows_raw(int64_t M);
 hipError_t launch_fp8_rows(fqt_dtype type, const Fp8GemmParams& p, const void* x, int64_t ldx, hipStream_t s);
 int64_t fp8_gemm_partials(int64_t M, int64_t N, int64_t K);  // floats
+fqt_fp8_form fp8_gemm_form(int64_t M, int64_t N, int64_t K, bool masked, bool lines);
 hipError_t launch_fp8_gemm(fqt_dtype type, const Fp8GemmParams& p, hipStream_t s);
 
 // ---------------------------------------------------------------------------

@@ -72,6 +72,7 @@ EXPORTS = [
     "fqt_gemm_s8s8_s64", "fqt_gemm_workspace", "fqt_gemm_s4s4_bf6", "fqt_gemm_s4s4_bf6_workspace",
     "fqt_layernorm_forward", "fqt_layernorm_backward", "fqt_layernorm_backward_workspace",
     "fqt_fp8_pitch", "fqt_fp8_exp_bytes", "fqt_fp8_quantize", "fqt_fp8_gemm", "fqt_fp8_gemm_workspace",
+    "fqt_fp8_gemm_form",
     "fqt_fp8_linear_forward", "fqt_fp8_linear_forward_workspace",
     "fqt_fp8_linear_backward", "fqt_fp8_linear_backward_workspace",
     "fqt_grad_norm_clip", "fqt_grad_norm_clip_workspace",
@@ -125,6 +126,7 @@ def load(path=LIB_PATH):
         "fqt_fp8_quantize": ([vp, i32, i64, i64, i64, i32, i32, u64, f8p, f8p, vp], i32),
         "fqt_fp8_gemm": ([f8p, f8p, i64, i64, i64, i32, i32, vp, i64, vp, i64, vp, sz, vp], i32),
         "fqt_fp8_gemm_workspace": ([i64, i64, i64], sz),
+        "fqt_fp8_gemm_form": ([i64, i64, i64, i32, i32], i32),
         "fqt_fp8_linear_forward": ([vp, i32, i64, i64, i64, f8p, i64, i32, vp, i64, f8p, vp, sz, vp], i32),
         "fqt_fp8_linear_forward_workspace": ([i64, i64, i64], sz),
         "fqt_fp8_linear_backward": ([vp, i32, i64, i64, i64, f8p, f8p, i64, i32, u64, vp, i64, vp, vp, i64, vp, sz,
@@ -603,6 +605,17 @@ def fqt_fp8_quantize(x, tile=False, by_row=True, by_col=False, stochastic=False,
 
 def fqt_fp8_gemm_workspace(M, N, K):
     return load().fqt_fp8_gemm_workspace(M, N, K)
+
+
+FP8_FORMS = ("rows", "small", "parts", "middle", "large", "several")
+
+
+def fqt_fp8_gemm_form(M, N, K, masked=False, lines=True):
+    """The form (of FP8_FORMS) that a product takes; lines: C's rows are whole lines of 128 bytes."""
+    form = load().fqt_fp8_gemm_form(M, N, K, int(bool(masked)), int(bool(lines)))
+    if form < 0:
+        raise ValueError(f"no product of {M} x {N} x {K}")
+    return FP8_FORMS[form]
 
 
 def fqt_fp8_gemm(A, B, dtype=torch.float32, relu=False, mask=None, C=None, ws=None):

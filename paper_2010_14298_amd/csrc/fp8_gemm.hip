@@ -810,7 +810,8 @@ __global__ __launch_bounds__(64 * ROW_WAVES) void fp8_rows_kernel(Fp8GemmParams 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
-  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const int64_t n0 = block_id() * 16;
+  if (n0 >= p.N) return;
   const int64_t n = n0 + r < p.N ? n0 + r : p.N - 1;
   const int64_t pitch = fp8_pitch(p.K);
   const int nk = (int)fp8_blocks(p.K);
@@ -966,9 +967,9 @@ hipError_t launch_fp8_rows(fqt_dtype type, const Fp8GemmParams& p, const void* x
   return with_type(type, [&](auto e) {
     using T = decltype(e);
     const int64_t blocks = (p.N + 15) / 16;
-    if (blocks > 0x7FFFFFFF || p.M > (x ? ROWS_RAW_MAX : ROWS_MAX)) return hipErrorInvalidValue;
+    if (p.M > (x ? ROWS_RAW_MAX : ROWS_MAX)) return hipErrorInvalidValue;
     auto go = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * ROW_WAVES), 0, s, p, x, ldx);
+      hipLaunchKernelGGL(kernel, grid_of(blocks, 64 * ROW_WAVES), dim3(64 * ROW_WAVES), 0, s, p, x, ldx);
       return hipGetLastError();
     };
     if (x) return go(fp8_rows_kernel<T, T, 1>);
@@ -993,7 +994,7 @@ hipError_t launch_fp8_gemm(fqt_dtype type, const Fp8GemmParams& p, hipStream_t s
       return tiles_of(p.M, p.N, C::BM, C::BN);
     };
     const int64_t blocks = plan.tile == Plan::LARGE ? tiles(LargeTile{}) : plan.tile == Plan::MID ? tiles(MidTile{}) : tiles(SmallTile{});
-    if (blocks > 0x3FFFFFFF) return hipErrorInvalidValue;
+    if (blocks > 0x7FFFFF) return hipErrorInvalidValue;  // 2^32 threads, 2^37 outputs
     int64_t grid = blocks;
     auto go = [&](auto kernel, auto... more) {
       hipLaunchKernelGGL(kernel, dim3((unsigned)grid, (unsigned)plan.splits), dim3(512), 0, s, p, more...);

@@ -279,7 +279,9 @@ __device__ __forceinline__ void turn_tile(const uint8_t* src, int64_t rows, int6
 template <class T, bool ROW, bool COL, bool SQUARE, bool SR>
 __global__ __launch_bounds__(QT) void fp8_tile_kernel(Fp8QuantParams p) {
   __shared__ __attribute__((aligned(16))) uint8_t turned[COL ? TILE * TILE : 16];
-  quantize_tile<T, ROW, COL, SQUARE, SR>(p, blockIdx.x, turned);
+  const int64_t block = block_id();
+  if (block >= fp8_blocks(p.rows) * fp8_blocks(p.cols)) return;
+  quantize_tile<T, ROW, COL, SQUARE, SR>(p, (uint32_t)block, turned);
 }
 __global__ __launch_bounds__(QT) void fp8_turn_kernel(Fp8Turn t) {
   __shared__ TurnLds sh;
@@ -303,12 +305,13 @@ __global__ __launch_bounds__(QT) void fp8_tile_turn_kernel(Fp8QuantParams p, Fp8
   }
 }
 
+constexpr int64_t MOST_BLOCKS = (((int64_t)1 << 32) - 1) / QT;  // of one dimension: operands of 2^38 bytes
 static int64_t turn_blocks(const Fp8Turn& t) { return t.src ? fp8_blocks(t.rows) * fp8_blocks(t.K) : 0; }
 
 hipError_t launch_fp8_turn(const Fp8Turn& t, hipStream_t s) {
   const int64_t blocks = turn_blocks(t);
   if (blocks == 0) return hipSuccess;
-  if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+  if (blocks > MOST_BLOCKS) return hipErrorInvalidValue;
   hipLaunchKernelGGL(fp8_turn_kernel, dim3((unsigned)blocks), dim3(QT), 0, s, t);
   return hipGetLastError();
 }
@@ -316,7 +319,7 @@ hipError_t launch_fp8_turn(const Fp8Turn& t, hipStream_t s) {
 hipError_t launch_fp8_quantize_turn(fqt_dtype type, const Fp8QuantParams& p, const Fp8Turn& a, const Fp8Turn& b,
                                     hipStream_t s) {
   const int64_t na = turn_blocks(a), nb = turn_blocks(b), blocks = fp8_blocks(p.rows) * fp8_blocks(p.cols) + na + nb;
-  if (na + nb > 0 && p.q_row && p.q_col && !p.tile && blocks <= 0x7FFFFFFF) {
+  if (na + nb > 0 && p.q_row && p.q_col && !p.tile && blocks <= MOST_BLOCKS) {
     return with_type(type, [&](auto e) {
       using T = decltype(e);
       auto go = [&](auto kernel) {
@@ -340,7 +343,7 @@ hipError_t launch_fp8_quantize(fqt_dtype type, const Fp8QuantParams& p, hipStrea
     using T = decltype(e);
     const bool row = p.q_row, col = p.q_col;
     auto go = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(QT), 0, s, p);
+      hipLaunchKernelGGL(kernel, grid_of(blocks, QT), dim3(QT), 0, s, p);
       return hipGetLastError();
     };
     auto pick = [&](auto square, auto sr) {

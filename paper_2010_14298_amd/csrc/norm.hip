@@ -56,8 +56,8 @@ template <class T, class C>
 __global__ __launch_bounds__(C::THREADS) void norm_forward_kernel(NormParams p) {
   __shared__ float sh[C::WAVES][1];
   const int t = threadIdx.x % C::TPR;
-  const int64_t row = (int64_t)blockIdx.x * C::PER_BLOCK + threadIdx.x / C::TPR;
-  if (C::PER_BLOCK > 1 && row >= p.rows) return;  // whole waves, and no barrier below
+  const int64_t row = block_id() * C::PER_BLOCK + threadIdx.x / C::TPR;
+  if (row >= p.rows) return;  // whole waves and no barrier below, or whole blocks
   const T* x = static_cast<const T*>(p.x) + row * p.ldx;
   float v[C::NV][C::VEC];
   float s[1] = {0.0f};
@@ -112,7 +112,8 @@ __global__ __launch_bounds__(C::THREADS) void norm_forward_kernel(NormParams p) 
 template <class T, class C>
 __global__ __launch_bounds__(C::THREADS) void norm_forward_long_kernel(NormParams p) {
   __shared__ float sh[C::WAVES][1];
-  const int64_t row = blockIdx.x;
+  const int64_t row = block_id();
+  if (row >= p.rows) return;
   const T* x = static_cast<const T*>(p.x) + row * p.ldx;
   const int64_t step = (int64_t)C::TPR * C::VEC, first = (int64_t)threadIdx.x * C::VEC;
   float v[C::VEC];
@@ -261,7 +262,8 @@ __global__ __launch_bounds__(C::THREADS) void norm_backward_kernel(NormParams p)
 template <class T, class C>
 __global__ __launch_bounds__(C::THREADS) void norm_backward_long_kernel(NormParams p) {
   __shared__ float sh[C::WAVES][2];
-  const int64_t row = blockIdx.x;
+  const int64_t row = block_id();
+  if (row >= p.rows) return;
   const T* x = static_cast<const T*>(p.x) + row * p.ldx;
   const T* g = static_cast<const T*>(p.g) + row * p.ldg;
   T* y = static_cast<T*>(p.y) + row * p.ldy;
@@ -318,7 +320,7 @@ __global__ __launch_bounds__(64 * REDUCE_WAVES) void norm_reduce_kernel(const fl
                                                                          float* grad_gamma, float* grad_beta) {
   __shared__ float sh[REDUCE_WAVES][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t col = (int64_t)blockIdx.x * 64 + lane;  // of 2 * cols: gamma's, then beta's
+  const int64_t col = block_id() * 64 + lane;  // of 2 * cols: gamma's, then beta's
   float s = 0.0f;
   if (col < 2 * cols) {
 #pragma unroll 4
@@ -365,11 +367,11 @@ hipError_t launch_norm_forward(fqt_dtype type, const NormParams& p, hipStream_t 
     return with_team<T>(p.cols, [&](auto c) {
       using C = decltype(c);
       const int64_t blocks = (p.rows + C::PER_BLOCK - 1) / C::PER_BLOCK;
-      if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+      const dim3 grid = grid_of(blocks, C::THREADS);
       if (p.cols <= TEAM_COLS)
-        hipLaunchKernelGGL((norm_forward_kernel<T, C>), dim3((unsigned)blocks), dim3(C::THREADS), 0, s, p);
+        hipLaunchKernelGGL((norm_forward_kernel<T, C>), grid, dim3(C::THREADS), 0, s, p);
       else if constexpr (C::TPR == 1024)
-        hipLaunchKernelGGL((norm_forward_long_kernel<T, C>), dim3((unsigned)blocks), dim3(C::THREADS), 0, s, p);
+        hipLaunchKernelGGL((norm_forward_long_kernel<T, C>), grid, dim3(C::THREADS), 0, s, p);
       return hipGetLastError();
     });
   });
@@ -400,7 +402,6 @@ int64_t norm_backward_partials(int64_t rows, int64_t cols) { return backward_blo
 hipError_t launch_norm_backward(fqt_dtype type, const NormParams& p, hipStream_t s) {
   const bool sums = p.grad_gamma || p.grad_beta;
   const int64_t blocks = backward_blocks(p.rows, p.cols);
-  if (p.rows > 0x7FFFFFFF) return hipErrorInvalidValue;
   const hipError_t e = with_type(type, [&](auto el) {
     using T = decltype(el);
     return with_block<T>(p.cols, [&](auto c) {
@@ -408,7 +409,7 @@ hipError_t launch_norm_backward(fqt_dtype type, const NormParams& p, hipStream_t
       if (p.cols <= TEAM_COLS) {
         hipLaunchKernelGGL((norm_backward_kernel<T, C>), dim3((unsigned)blocks), dim3(C::THREADS), 0, s, p);
       } else if constexpr (C::TPR == 1024) {
-        hipLaunchKernelGGL((norm_backward_long_kernel<T, C>), dim3((unsigned)p.rows), dim3(C::THREADS), 0, s, p);
+        hipLaunchKernelGGL((norm_backward_long_kernel<T, C>), grid_of(p.rows, C::THREADS), dim3(C::THREADS), 0, s, p);
         if (sums)
           hipLaunchKernelGGL((norm_columns_kernel<T>), dim3((unsigned)((p.cols + 255) / 256), (unsigned)blocks),
                              dim3(256), 0, s, p);
@@ -417,8 +418,8 @@ hipError_t launch_norm_backward(fqt_dtype type, const NormParams& p, hipStream_t
     });
   });
   if (e != hipSuccess || !sums || (blocks == 1 && p.cols <= TEAM_COLS)) return e;
-  hipLaunchKernelGGL(norm_reduce_kernel, dim3((unsigned)((2 * p.cols + 63) / 64)), dim3(64 * REDUCE_WAVES), 0, s,
-                     p.part, blocks, p.cols, p.grad_gamma, p.grad_beta);
+  hipLaunchKernelGGL(norm_reduce_kernel, grid_of((2 * p.cols + 63) / 64, 64 * REDUCE_WAVES), dim3(64 * REDUCE_WAVES),
+                     0, s, p.part, blocks, p.cols, p.grad_gamma, p.grad_beta);
   return hipGetLastError();
 }
 

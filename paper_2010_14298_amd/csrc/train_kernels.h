@@ -70,6 +70,17 @@ inline hipError_t with_type(fqt_dtype type, F f) {
 inline bool valid_type(fqt_dtype t) { return t == FQT_F32 || t == FQT_BF16 || t == FQT_F16; }
 
 // ---------------------------------------------------------------------------
+// one-dimensional launches of any length: a dimension of a grid holds fewer
+// than 2^32 threads (more are cut off without an error), so long launches get a
+// second one.  Blocks from `blocks` on find nothing to do.
+// ---------------------------------------------------------------------------
+inline dim3 grid_of(int64_t blocks, int threads) {
+  const int64_t most = ((int64_t)1 << 31) / threads, y = (blocks + most - 1) / most;
+  return dim3((unsigned)(y > 1 ? most : blocks), (unsigned)y);
+}
+__device__ __forceinline__ int64_t block_id() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
+// ---------------------------------------------------------------------------
 // reductions over a wave: every lane gets the result, in a fixed order.
 // Rotations inside rows of 16 lanes, then row and half-wave swaps.
 // ---------------------------------------------------------------------------

@@ -401,11 +401,11 @@ fqt_status fqt_fp8_quantize(const void* x, fqt_dtype type, int64_t rows, int64_t
 /* C [M, N] = A [M, K] B [N, K]^T of two operands, accumulated in float32 on
  * the matrix cores; optionally C = max(C, 0) (relu != 0) and C = 0 where mask
  * [M, N] (of C's type) is not positive.  Codes and scales are read exactly
- * (codes of a block with E < -124 to the nearest multiple of 2^-133), the sums
- * are float32 whatever C's type.  Their order depends on M, N, K and the type
- * alone: the same call gives the same bits, but a row's last bits may differ
- * with the number of rows.  K up to 2^23 (FQT_EUNSUPPORTED beyond; also in the
- * layers below).                                                           */
+ * (codes of a block with E < -124 to the nearest multiple of 2^-133, elements
+ * that stand for 2^128 as infinity), the sums are float32 whatever C's type.
+ * Their order depends on M, N, K and the type alone: the same call gives the
+ * same bits, but a row's last bits may differ with the number of rows.  K up to
+ * 2^23 (FQT_EUNSUPPORTED beyond; also in the layers below).                */
 fqt_status fqt_fp8_gemm(const fqt_fp8* A, const fqt_fp8* B, int64_t M, int64_t N, int64_t K, fqt_dtype type, int relu,
                         const void* mask, int64_t ldmask, void* C, int64_t ldc, void* ws, size_t ws_bytes,
                         fqt_stream_t s);

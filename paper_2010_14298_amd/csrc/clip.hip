@@ -11,7 +11,7 @@
 //
 // Memory bounds it: 25.2 M float32 gradients take 25.5 us for the norm (101 MB,
 // 4.0 TB/s) and 34.3 us for the scaling (201 MB, 5.9 TB/s: part of the second
-// read comes from the last cache).  161 bfloat16 tensors, 51 MB: 13.2 + 19.4 us.
+// read comes from the last cache).  161 bfloat16 tensors, 51 MB: 13.4 + 19.7 us.
 #include "train_kernels.h"
 
 namespace fqt {

@@ -16,8 +16,10 @@
 //
 // To nearest, 8192 x 1024 bfloat16 to both operands (34 MB): 9.9 us, 3.4 TB/s.
 // Two tiles a unit, each a chain of load, maxima and store; vector issue is 40 %
-// busy.  Stochastic, 8192 x 4096 bfloat16 (134 MB): 53 us, 2.6 TB/s, vector
-// issue 93 % busy: two random blocks for four elements are 28 wide multiplies.
+// busy.  Stochastic, 8192 x 4096 bfloat16 (134 MB): 44.5 us, 3.0 TB/s, vector issue
+// 90 % busy: two random blocks for four elements are 28 wide multiplies.  Where
+// many elements lie far below their block's largest (1 % of rows a thousand times
+// the rest) 51 us against 46.5 in the same run.
 #include "fp8_codes.h"
 #include "fqt_device.h"
 
@@ -45,8 +47,8 @@ __device__ __forceinline__ uint32_t quad_codes(const float (&v)[4], const float 
     const uint32_t f = word[j] >> 4 & 0xfffffu;
     c[j] = __builtin_elementwise_sub_sat(__builtin_elementwise_sub_sat(m[j], f), (120u << 23) - 0xfffffu);
   }
-  // zeros are right as they are; anything else below 2^-6 is rare, one element
-  // in thousands lies that far below its block's largest
+  // zeros are right as they are; anything else below 2^-6 is rare where a block's
+  // elements are alike: one in thousands lies that far below the largest
   const uint32_t a = m[0] < m[1] ? m[0] : m[1], b = m[2] < m[3] ? m[2] : m[3];
   if (__builtin_amdgcn_ballot_w64((a < b ? a : b) < 0x3c800000u) != 0) {
     uint32_t least = ~0u;
@@ -290,7 +292,7 @@ __global__ __launch_bounds__(QT) void fp8_turn_kernel(Fp8Turn t) {
 // Both in one launch: of every `step` blocks the last lays codes out, until there
 // are `turns` of them.  They wait for memory while the others compute: a
 // backward of 8192, 1024 -> 4096 bfloat16 with both kept operands to lay out takes
-// 148.5 us, in three launches 151.5; of 1000, 512 -> 512 30.3 us, 35.4.
+// 170 us, in three launches 174.5; of 1000, 512 -> 512 31.6 us, 36.6.
 template <class T, bool SR>
 __global__ __launch_bounds__(QT) void fp8_tile_turn_kernel(Fp8QuantParams p, Fp8Turn a, Fp8Turn b, uint32_t turns_a,
                                                            uint32_t turns, uint32_t step) {

@@ -10,10 +10,11 @@
 // parameter gradients are float32; the outputs are rounded once.
 //
 // Forward, 8192 x 4096 float32 (268 MB): 51 us, 5.3 TB/s, a large copy's rate;
-// memory bounds it.  Backward, 8192 x 1024 bfloat16 (50 MB): 15.5 us, 3.2 TB/s,
+// memory bounds it.  Backward, 8192 x 1024 bfloat16 (50 MB): 15.4 us, 3.3 TB/s,
 // and 3.8 us for the partial sums; two rows a wave, whose waves wait three
-// quarters of the time for their loads.  One row of 4096 bfloat16 forward: 3.1
-// us, a launch and a chain of latencies.
+// quarters of the time for their loads.  float32 (101 MB): 24.0 us, 4.2 TB/s, waits
+// half of the time.  One row of 4096 bfloat16 forward: 3.0 us, a launch and a chain
+// of latencies.
 #include "train_kernels.h"
 
 namespace fqt {
@@ -153,8 +154,8 @@ __global__ __launch_bounds__(C::THREADS) void norm_forward_long_kernel(NormParam
 }
 
 // Backward: one block of 1024 threads a unit, so that there are few partial
-// sums (8192 x 1024 bfloat16: 1024 blocks of four teams left 8 MB of them, 6.9
-// us to add up).  Each team takes every (teams)-th row and keeps its columns'
+// sums (8192 x 1024 bfloat16: 1024 blocks of four teams leave 8 MB of them, 21.1
+// us in all instead of 17.8; float32 29.5, 27.3).  Each team takes every (teams)-th row and keeps its columns'
 // sums of g xh and g in registers; at the end the block's teams meet in LDS
 // pairwise and one writes the block's partial row (an only block writes the
 // parameter gradients themselves).
@@ -342,11 +343,12 @@ __global__ __launch_bounds__(64 * REDUCE_WAVES) void norm_reduce_kernel(const fl
 // launches
 // ---------------------------------------------------------------------------
 // Teams by row length; 16 elements a thread.  A wave up to 1024 columns needs no
-// barrier (8192 x 1024: bfloat16 9.5 us, with four waves a row 12.2; float32
-// 12.5, 15.4; backward 17.5, 20.0 and 27.3, 29.0); at 2048 columns 32 elements
-// a thread gain nothing (15.6 us with four waves, 16.1 with one; float32 27.8,
-// 29.5).  A call of one row of 1024 is the other way round, 2.9 us against 2.6
-// and 6.1 against 3.3 in the backward, whose block adds up idle teams too.
+// barrier (8192 x 1024: bfloat16 9.6 us, with four waves a row 13.1; float32
+// 13.0, 15.9; backward 17.8, 22.1 and 27.3, 29.5); at 2048 columns 32 elements
+// a thread gain nothing (15.5 us with four waves, 16.1 with one; float32 27.6,
+// 29.9; backward 30.7, 30.5 and 44.5, 44.2).  A call of one row of 1024 is the other
+// way round, 2.9 us against 2.6 and 6.2 against 4.1 in the backward, whose block
+// adds up idle teams too.
 template <class T, class F>
 static hipError_t with_team(int64_t cols, F f) {
   constexpr int V = 16 / (int)sizeof(T);  // elements of 16 bytes

@@ -3,10 +3,10 @@
   Y = X + W2 relu(W1 layernorm(X))
 
 Weights are float32; their codes (128 x 128 tiles, by row for the forward, by column for the input gradient) are
-formed once a step and kept between steps that do not change them, as while serving.  Every product runs in 8-bit
-floating point with a scale for each block of 128; gradients are quantized stochastically, so that they stay
-unbiased (Sec. 2.2), with independent draws for grad_W and grad_X (App. E).  Gradients are clipped by their global
-norm before the update.
+formed once a step and kept between steps that do not change them, as while serving.  Every product reads 8-bit
+floating point operands with a scale for each block of 128 and sums in float32; gradients are quantized
+stochastically, so that they stay unbiased (Sec. 2.2), with independent draws for grad_W and grad_X (App. E).
+Gradients are clipped by their global norm before the update.
 
   python -m paper_2010_14298_amd.ffn [--tokens N] [--width D] [--hidden H] [--steps K]
 

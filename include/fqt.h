@@ -333,7 +333,8 @@ size_t fqt_gemm_s4s4_bf6_workspace(int64_t M, int64_t N, int64_t K);
 
 /* ---------------------------------------------------------------------------
  * Floating-point operators around the layers of a feed-forward training step:
- * layer norm, layers in 8-bit floating point, gradient norm and clipping.
+ * layer norm, layers in 8-bit floating point (plain and gated), checkpoints in
+ * 8 bits, gradient norm and clipping.
  *
  * Matrices are row-major with unit column stride and any row pitch (ld*, in
  * elements; an input's rows may overlap, pitch 0 repeats one row), at any
@@ -449,6 +450,74 @@ fqt_status fqt_fp8_linear_backward(const void* G, fqt_dtype type, int64_t N, int
                                    const void* relu_input, int64_t ldr, float* grad_W, void* grad_X, int64_t ldgx,
                                    void* ws, size_t ws_bytes, fqt_stream_t s);
 size_t fqt_fp8_linear_backward_workspace(int64_t N, int64_t d_in, int64_t d_out);
+
+/* A checkpoint: activations [rows, cols] kept in 8 bits between a training
+ * step's forward and its backward, one byte an element and one for each 32
+ * consecutive elements of a row.
+ *   q    [rows, fqt_fp8_kept_pitch(cols)], 16-byte aligned: codes as above,
+ *        whole blocks of 32, zero codes past cols.
+ *   exp  [rows, pitch / 32]: E + 127 of each block; 255 is NaN.
+ * An element stands for q 2^E, E the least integer >= -127 with max|block| <=
+ * 448 2^E (0 for an empty block); codes are rounded to nearest, ties to even.  A
+ * block that holds a NaN or an infinity becomes NaN as a whole.              */
+typedef struct {
+  uint8_t* q;
+  uint8_t* exp;
+} fqt_kept;
+size_t fqt_fp8_kept_pitch(int64_t cols);
+
+/* Layer norm with a checkpoint for its backward: Y as fqt_layernorm_forward's,
+ * xh8 the checkpoint of xh = (x - mean) rstd [rows, cols], rstd [rows].      */
+fqt_status fqt_layernorm_forward8(const void* X, fqt_dtype type, int64_t rows, int64_t cols, int64_t ldx,
+                                  const float* gamma, const float* beta, float eps, void* Y, int64_t ldy,
+                                  const fqt_kept* xh8, float* rstd, fqt_stream_t s);
+
+/* fqt_layernorm_backward with xh as the checkpoint has it.  The workspace is
+ * fqt_layernorm_backward_workspace's.                                        */
+fqt_status fqt_layernorm_backward8(const void* G, int64_t ldg, const fqt_kept* xh8, fqt_dtype type, int64_t rows,
+                                   int64_t cols, const float* rstd, const float* gamma, void* grad_X, int64_t ldgx,
+                                   float* grad_gamma, float* grad_beta, void* ws, size_t ws_bytes, fqt_stream_t s);
+
+/* Activations of a gated layer, with s(z) = 1 / (1 + exp(-z)):
+ *   silu        a s(a)
+ *   gelu_tanh   a s(2 u), u = sqrt(2 / pi) (a + 0.044715 a^3)  (= a (1 + tanh u) / 2)
+ *   relu        max(a, 0), whose derivative at 0 is 0                        */
+typedef enum { FQT_SILU = 0, FQT_GELU_TANH = 1, FQT_RELU = 2 } fqt_act;
+
+/* Gated layer forward in 8-bit floating point: with W8 [2 hidden, K = d_in]
+ * the codes of [W_gate; W_up] (fqt_fp8_quantize with tile, by_row) and X
+ * quantized as in fqt_fp8_linear_forward,
+ *   a = Q(X) W_gate^T,  b = Q(X) W_up^T,  H [N, hidden] = act(a) b
+ * with a and b in float32 and H rounded once.  What the backward reads (each
+ * may be NULL, as while serving):
+ *   X8t     operand of X^T [d_in, K = N]
+ *   d_gate  checkpoint [N, hidden] of dH/da = b act'(a)
+ *   d_up    checkpoint [N, hidden] of dH/db = act(a)
+ * Two bytes a hidden unit: the derivatives themselves are kept, not a and b, so
+ * that the backward is linear in what was rounded.  2 hidden < 2^31, d_in up to
+ * 2^23 (FQT_EUNSUPPORTED beyond).                                            */
+fqt_status fqt_fp8_gated_forward(const void* X, fqt_dtype type, int64_t N, int64_t d_in, int64_t ldx,
+                                 const fqt_fp8* W8, int64_t hidden, fqt_act act, void* H, int64_t ldh,
+                                 const fqt_fp8* X8t, const fqt_kept* d_gate, const fqt_kept* d_up, void* ws,
+                                 size_t ws_bytes, fqt_stream_t s);
+size_t fqt_fp8_gated_forward_workspace(int64_t N, int64_t d_in, int64_t hidden);
+
+/* Its backward.  With G = dL/dH [N, hidden], the float32 products
+ *   D [N, 2 hidden] = [G d_gate | G d_up]
+ * (exact for 16-bit G) are quantized twice and never stored otherwise:
+ *   grad_W [2 hidden, d_in] = Q1(D)^T X8t^T   (D^T in blocks of 128 along N)
+ *   grad_X [N, d_in]        = Q2(D) W8t^T     (D in blocks of 128 along 2 hidden)
+ * to nearest or (stochastic != 0) unbiased with one random word an element of D
+ * (stream 2), as in the other quantizers with u = 2^8 times the word's low 16
+ * bits for Q1 and its high 16 bits for Q2.  X8t [d_in, K = N], d_gate and d_up
+ * from the forward, W8t [d_in, K = 2 hidden] the weights' by_col operand.
+ * grad_W or grad_X may be NULL (not formed; its operand may then be NULL too).
+ * N and 2 hidden up to 2^23 where they are contracted (FQT_EUNSUPPORTED).     */
+fqt_status fqt_fp8_gated_backward(const void* G, fqt_dtype type, int64_t N, int64_t hidden, int64_t ldg,
+                                  const fqt_kept* d_gate, const fqt_kept* d_up, const fqt_fp8* X8t,
+                                  const fqt_fp8* W8t, int64_t d_in, int stochastic, uint64_t seed, float* grad_W,
+                                  void* grad_X, int64_t ldgx, void* ws, size_t ws_bytes, fqt_stream_t s);
+size_t fqt_fp8_gated_backward_workspace(int64_t N, int64_t d_in, int64_t hidden);
 
 /* Global gradient norm and clipping over `count` contiguous tensors:
  *   n = sqrt(sum over all tensors of g^2),  out = g max_norm / n if n > max_norm, else g

@@ -24,6 +24,7 @@ struct Carver {
 
 constexpr int64_t MAX_SIDE = (int64_t)1 << 31;   // rows or columns of a matrix
 bool side(int64_t n) { return n >= 1 && n < MAX_SIDE; }
+bool half_side(int64_t n) { return n >= 1 && n < MAX_SIDE / 2; }
 // the products address a tile of 256 rows of codes with 31-bit offsets
 constexpr int64_t MAX_CONTRACTION = (int64_t)1 << 23;
 size_t type_bytes(fqt_dtype t) { return t == FQT_F32 ? 4 : 2; }
@@ -39,6 +40,9 @@ bool operand(const fqt_fp8* a) {
 }
 // one that a call writes: row by row only
 bool written(const fqt_fp8* a) { return operand(a) && a->k_major == 0; }
+
+bool checkpoint(const fqt_kept* k) { return k && k->q && k->exp && aligned(k->q, 16); }
+Kept kept_of(const fqt_kept* k) { return k ? Kept{k->q, k->exp} : Kept{}; }
 
 #define FQT_TRY(expr)                              \
   do {                                             \
@@ -100,6 +104,56 @@ BackwardWs carve_backward(Carver& c, int64_t N, int64_t d_in, int64_t d_out) {
   w.w = c.take<uint8_t>(d_in * fp8_pitch(d_out));
   const int64_t a = fp8_gemm_partials(N, d_in, d_out), b = fp8_gemm_partials(d_out, d_in, N);
   w.part = c.take<float>(a > b ? a : b);
+  return w;
+}
+
+// Both products of a layer's backward, from the operands in w and the codes x8, w8
+// of the kept ones.  grad_W or grad_X null: not formed.
+hipError_t gradients_of(fqt_dtype type, const BackwardWs& w, int64_t N, int64_t d_in, int64_t d_out, const uint8_t* x8,
+                        const fqt_fp8* X8t, const uint8_t* w8, const fqt_fp8* W8t, const void* relu_input, int64_t ldr,
+                        float* grad_W, void* grad_X, int64_t ldgx, hipStream_t s) {
+  Fp8GemmParams p{};
+  p.part = w.part;
+  p.N = d_in;
+  if (grad_W) {
+    p.A = w.gt.q;
+    p.eA = w.gt.e;
+    p.B = x8;
+    p.eB = X8t->exp;
+    p.M = d_out;
+    p.K = N;
+    p.C = grad_W;
+    p.ldc = d_in;
+    const hipError_t e = launch_fp8_gemm(FQT_F32, p, s);
+    if (e != hipSuccess) return e;
+  }
+  if (grad_X) {
+    p.A = w.g.q;
+    p.eA = w.g.e;
+    p.B = w8;
+    p.eB = W8t->exp;
+    p.M = N;
+    p.K = d_out;
+    p.C = grad_X;
+    p.ldc = ldgx;
+    p.mask = relu_input;
+    p.ldmask = ldr;
+    return launch_fp8_gemm(type, p, s);
+  }
+  return hipSuccess;
+}
+
+struct GatedForwardWs {
+  Fp8Buffers x;
+  uint8_t* w;
+  float *both, *part;  // a and b; their partial sums
+};
+GatedForwardWs carve_gated_forward(Carver& c, int64_t N, int64_t d_in, int64_t hidden) {
+  GatedForwardWs w;
+  w.w = c.take<uint8_t>(2 * hidden * fp8_pitch(d_in));
+  w.x = take_operand(c, N, d_in);
+  w.both = c.take<float>(N * 2 * hidden);
+  w.part = c.take<float>(fp8_gemm_partials(N, 2 * hidden, d_in));
   return w;
 }
 
@@ -172,9 +226,60 @@ fqt_status fqt_layernorm_backward(const void* G, int64_t ldg, const void* X, int
   return FQT_OK;
 }
 
+fqt_status fqt_layernorm_forward8(const void* X, fqt_dtype type, int64_t rows, int64_t cols, int64_t ldx,
+                                  const float* gamma, const float* beta, float eps, void* Y, int64_t ldy,
+                                  const fqt_kept* xh8, float* rstd, fqt_stream_t s) {
+  if (!valid_type(type) || !side(rows) || !side(cols) || !(eps >= 0.0f) || !isfinite(eps)) return FQT_EINVAL;
+  if (!input(X, type, ldx) || !output(Y, type, cols, ldy) || !checkpoint(xh8) || !rstd) return FQT_EINVAL;
+  if (!aligned(gamma, 4) || !aligned(beta, 4) || !aligned(rstd, 4)) return FQT_EINVAL;
+  NormParams p{};
+  p.x = X;
+  p.ldx = ldx;
+  p.rows = rows;
+  p.cols = cols;
+  p.gamma = gamma;
+  p.beta = beta;
+  p.eps = eps;
+  p.y = Y;
+  p.ldy = ldy;
+  p.rstd = rstd;
+  p.q8 = xh8->q;
+  p.e8 = xh8->exp;
+  FQT_TRY(launch_norm_forward(type, p, s));
+  return FQT_OK;
+}
+
+fqt_status fqt_layernorm_backward8(const void* G, int64_t ldg, const fqt_kept* xh8, fqt_dtype type, int64_t rows,
+                                   int64_t cols, const float* rstd, const float* gamma, void* grad_X, int64_t ldgx,
+                                   float* grad_gamma, float* grad_beta, void* ws, size_t ws_bytes, fqt_stream_t s) {
+  if (!valid_type(type) || !side(rows) || !side(cols) || !rstd || !checkpoint(xh8)) return FQT_EINVAL;
+  if (!input(G, type, ldg) || !output(grad_X, type, cols, ldgx)) return FQT_EINVAL;
+  if (!aligned(gamma, 4) || !aligned(rstd, 4) || !aligned(grad_gamma, 4) || !aligned(grad_beta, 4)) return FQT_EINVAL;
+  if (grad_gamma || grad_beta) {
+    if (!ws || !aligned(ws, 16) || ws_bytes < fqt_layernorm_backward_workspace(rows, cols)) return FQT_EWORKSPACE;
+  }
+  NormParams p{};
+  p.g = G;
+  p.ldg = ldg;
+  p.rows = rows;
+  p.cols = cols;
+  p.rstd = const_cast<float*>(rstd);
+  p.gamma = gamma;
+  p.y = grad_X;
+  p.ldy = ldgx;
+  p.grad_gamma = grad_gamma;
+  p.grad_beta = grad_beta;
+  p.part = static_cast<float*>(ws);
+  p.q8 = xh8->q;
+  p.e8 = xh8->exp;
+  FQT_TRY(launch_norm_backward(type, p, s));
+  return FQT_OK;
+}
+
 // ---------------------------------------------------------------------------
 // 8-bit floating point layers
 // ---------------------------------------------------------------------------
+size_t fqt_fp8_kept_pitch(int64_t cols) { return side(cols) ? (size_t)kept_pitch(cols) : 0; }
 size_t fqt_fp8_pitch(int64_t K) { return side(K) ? (size_t)fp8_pitch(K) : 0; }
 size_t fqt_fp8_exp_bytes(int64_t rows, int64_t K) { return side(rows) && side(K) ? (size_t)fp8_exp_bytes(rows, K) : 0; }
 
@@ -339,33 +444,118 @@ fqt_status fqt_fp8_linear_backward(const void* G, fqt_dtype type, int64_t N, int
   const uint8_t* const x8 = grad_W ? rows_of(X8t, d_in, N, w.x, &turn_x) : nullptr;
   const uint8_t* const w8 = grad_X ? rows_of(W8t, d_in, d_out, w.w, &turn_w) : nullptr;
   FQT_TRY(launch_fp8_quantize_turn(type, q, turn_x, turn_w, s));
+  FQT_TRY(gradients_of(type, w, N, d_in, d_out, x8, X8t, w8, W8t, relu_input, ldr, grad_W, grad_X, ldgx, s));
+  return FQT_OK;
+}
+
+// ---------------------------------------------------------------------------
+// gated layer
+// ---------------------------------------------------------------------------
+size_t fqt_fp8_gated_forward_workspace(int64_t N, int64_t d_in, int64_t hidden) {
+  if (!side(N) || !side(d_in) || !half_side(hidden)) return 0;
+  Carver c(nullptr);
+  carve_gated_forward(c, N, d_in, hidden);
+  return c.off;
+}
+
+fqt_status fqt_fp8_gated_forward(const void* X, fqt_dtype type, int64_t N, int64_t d_in, int64_t ldx,
+                                 const fqt_fp8* W8, int64_t hidden, fqt_act act, void* H, int64_t ldh,
+                                 const fqt_fp8* X8t, const fqt_kept* d_gate, const fqt_kept* d_up, void* ws,
+                                 size_t ws_bytes, fqt_stream_t s) {
+  if (!valid_type(type) || !side(N) || !side(d_in) || !half_side(hidden) || !operand(W8)) return FQT_EINVAL;
+  if (!input(X, type, ldx) || !output(H, type, hidden, ldh)) return FQT_EINVAL;
+  if (act != FQT_SILU && act != FQT_GELU_TANH && act != FQT_RELU) return FQT_EINVAL;
+  if ((X8t && !written(X8t)) || (d_gate && !checkpoint(d_gate)) || (d_up && !checkpoint(d_up))) return FQT_EINVAL;
+  if (d_in > MAX_CONTRACTION) return FQT_EUNSUPPORTED;
+  if (!ws || !aligned(ws, 16) || ws_bytes < fqt_fp8_gated_forward_workspace(N, d_in, hidden)) return FQT_EWORKSPACE;
+  Carver c(ws);
+  const GatedForwardWs w = carve_gated_forward(c, N, d_in, hidden);
+  Fp8QuantParams q{};
+  q.x = X;
+  q.rows = N;
+  q.cols = d_in;
+  q.ldx = ldx;
+  q.q_row = w.x.q;
+  q.e_row = w.x.e;
+  if (X8t) {
+    q.q_col = X8t->q;
+    q.e_col = X8t->exp;
+  }
   Fp8GemmParams p{};
+  Fp8Turn turn{};
+  p.A = w.x.q;
+  p.eA = w.x.e;
+  p.B = rows_of(W8, 2 * hidden, d_in, w.w, &turn);
+  p.eB = W8->exp;
+  FQT_TRY(launch_fp8_quantize_turn(type, q, turn, Fp8Turn{}, s));
+  p.M = N;
+  p.N = 2 * hidden;
+  p.K = d_in;
+  p.C = w.both;
+  p.ldc = 2 * hidden;
   p.part = w.part;
-  p.N = d_in;
-  if (grad_W) {
-    p.A = w.gt.q;
-    p.eA = w.gt.e;
-    p.B = x8;
-    p.eB = X8t->exp;
-    p.M = d_out;
-    p.K = N;
-    p.C = grad_W;
-    p.ldc = d_in;
-    FQT_TRY(launch_fp8_gemm(FQT_F32, p, s));
-  }
+  FQT_TRY(launch_fp8_gemm(FQT_F32, p, s));
+  GatedParams g{};
+  g.part = w.both;
+  g.N = N;
+  g.hidden = hidden;
+  g.act = act;
+  g.H = H;
+  g.ldh = ldh;
+  g.gate = kept_of(d_gate);
+  g.up = kept_of(d_up);
+  FQT_TRY(launch_gated_finish(type, g, s));
+  return FQT_OK;
+}
+
+size_t fqt_fp8_gated_backward_workspace(int64_t N, int64_t d_in, int64_t hidden) {
+  if (!side(N) || !side(d_in) || !half_side(hidden)) return 0;
+  Carver c(nullptr);
+  carve_backward(c, N, d_in, 2 * hidden);
+  return c.off;
+}
+
+fqt_status fqt_fp8_gated_backward(const void* G, fqt_dtype type, int64_t N, int64_t hidden, int64_t ldg,
+                                  const fqt_kept* d_gate, const fqt_kept* d_up, const fqt_fp8* X8t,
+                                  const fqt_fp8* W8t, int64_t d_in, int stochastic, uint64_t seed, float* grad_W,
+                                  void* grad_X, int64_t ldgx, void* ws, size_t ws_bytes, fqt_stream_t s) {
+  if (!valid_type(type) || !side(N) || !side(d_in) || !half_side(hidden) || !input(G, type, ldg)) return FQT_EINVAL;
+  if (!checkpoint(d_gate) || !checkpoint(d_up)) return FQT_EINVAL;
+  if ((!grad_W && !grad_X) || (stochastic != 0 && stochastic != 1)) return FQT_EINVAL;
+  if (grad_W && (!operand(X8t) || !aligned(grad_W, 4))) return FQT_EINVAL;
+  if (grad_X && (!operand(W8t) || !output(grad_X, type, d_in, ldgx))) return FQT_EINVAL;
+  const int64_t cols = 2 * hidden;
+  if ((grad_W && N > MAX_CONTRACTION) || (grad_X && cols > MAX_CONTRACTION)) return FQT_EUNSUPPORTED;
+  if (!ws || !aligned(ws, 16) || ws_bytes < fqt_fp8_gated_backward_workspace(N, d_in, hidden)) return FQT_EWORKSPACE;
+  Carver c(ws);
+  const BackwardWs w = carve_backward(c, N, d_in, cols);
+  GatedQuantParams d{};
+  d.q.x = G;
+  d.q.rows = N;
+  d.q.cols = cols;
+  d.q.ldx = ldg;
+  d.q.stochastic = stochastic;
+  d.q.seed = seed;
   if (grad_X) {
-    p.A = w.g.q;
-    p.eA = w.g.e;
-    p.B = w8;
-    p.eB = W8t->exp;
-    p.M = N;
-    p.K = d_out;
-    p.C = grad_X;
-    p.ldc = ldgx;
-    p.mask = relu_input;
-    p.ldmask = ldr;
-    FQT_TRY(launch_fp8_gemm(type, p, s));
+    d.q.q_row = w.g.q;
+    d.q.e_row = w.g.e;
   }
+  if (grad_W) {
+    d.q.q_col = w.gt.q;
+    d.q.e_col = w.gt.e;
+  }
+  d.hidden = hidden;
+  d.q_gate = d_gate->q;
+  d.e_gate = d_gate->exp;
+  d.q_up = d_up->q;
+  d.e_up = d_up->exp;
+  FQT_TRY(launch_gated_quantize(type, d, s));
+  Fp8Turn turn_x{}, turn_w{};
+  const uint8_t* const x8 = grad_W ? rows_of(X8t, d_in, N, w.x, &turn_x) : nullptr;
+  const uint8_t* const w8 = grad_X ? rows_of(W8t, d_in, cols, w.w, &turn_w) : nullptr;
+  FQT_TRY(launch_fp8_turn(turn_x, s));
+  FQT_TRY(launch_fp8_turn(turn_w, s));
+  FQT_TRY(gradients_of(type, w, N, d_in, cols, x8, X8t, w8, W8t, nullptr, 0, grad_W, grad_X, ldgx, s));
   return FQT_OK;
 }
 

@@ -90,9 +90,24 @@ __device__ __forceinline__ u32x4 quad_words(uint64_t e, uint64_t seed, uint32_t 
   return u;
 }
 
+// Where a tile's elements come from: quads of rows row .. row + GROUP - 1 at
+// column col, and their random words.
+template <class T>
+struct MatrixSource {
+  typedef T Elem;
+  static constexpr bool HALVES = false;  // the two operands' words are of streams 1 and 0
+  const T* x;
+  int64_t ldx, rows, left;  // rows and columns from (row, col) on
+  __device__ __forceinline__ MatrixSource(const Fp8QuantParams& p, int64_t row, int64_t col)
+      : x(static_cast<const T*>(p.x) + row * p.ldx + col), ldx(p.ldx), rows(p.rows - row), left(p.cols - col) {}
+  __device__ __forceinline__ void load(int i, Quad<T>& v) const { v.load(x + i * ldx, i < rows ? left : 0); }
+};
+
 // One tile of 128 x 128, by a block of threads; `turned`: LDS, 16 KB where COL.
-template <class T, bool ROW, bool COL, bool SQUARE, bool SR>
-__device__ __forceinline__ void quantize_tile(const Fp8QuantParams& p, uint32_t block, uint8_t* turned) {
+template <class Source, bool ROW, bool COL, bool SQUARE, bool SR, class Params>
+__device__ __forceinline__ void quantize_tile(const Params& params, uint32_t block, uint8_t* turned) {
+  typedef typename Source::Elem T;
+  const Fp8QuantParams& p = params;
   __shared__ uint32_t col_top[QT / 32][TILE / 2];
   __shared__ __attribute__((aligned(8))) uint16_t keys[2][TILE];  // of the rows, of the columns
   const int tid = threadIdx.x, quad = tid & 31, grp = tid >> 5;
@@ -100,10 +115,10 @@ __device__ __forceinline__ void quantize_tile(const Fp8QuantParams& p, uint32_t 
   const uint32_t cb = block / row_blocks, rb = block - cb * row_blocks;
   const int64_t r0 = (int64_t)rb * TILE, c0 = (int64_t)cb * TILE;
   const int64_t row = r0 + grp * GROUP, col = c0 + 4 * quad;
-  const T* x = static_cast<const T*>(p.x) + row * p.ldx + col;
+  const Source x(params, row, col);
   Quad<T> v[GROUP];
 #pragma unroll
-  for (int i = 0; i < GROUP; ++i) v[i].load(x + i * p.ldx, row + i < p.rows ? p.cols - col : 0);
+  for (int i = 0; i < GROUP; ++i) x.load(i, v[i]);
 
   // keys of the rows (two to a word) and columns
   typename Quad<T>::ColTop ct{};
@@ -184,16 +199,29 @@ __device__ __forceinline__ void quantize_tile(const Fp8QuantParams& p, uint32_t 
         const float f[4] = {v[i + k].at(0), v[i + k].at(1), v[i + k].at(2), v[i + k].at(3)};
         const uint32_t sign = v[i + k].signs();
         const uint64_t e = (uint64_t)(row + i + k) * (uint64_t)p.cols + (uint64_t)col;
+        // 2^8 times the low half of a word for one operand, the high half for the other
+        u32x4 both{};
+        if constexpr (Source::HALVES) both = quad_words(e, p.seed, 2u, whole);
         if constexpr (ROW) {
           const int sh = 16 * (k & 1);
           const uint32_t rkey = rk[(i + k) / 2] >> sh & 0xffffu, rbyte = scale_bytes(rk[(i + k) / 2]) >> sh & 0xffffu;
           const float s = scale_down(rbyte);
           const float down[4] = {s, s, s, s};
-          store_row(i + k, rkey, quad_codes(f, down, quad_words(e, p.seed, 1u, whole), sign));
+          u32x4 u{};
+          if constexpr (Source::HALVES)
+            u = u32x4{both.x >> 8 & 0xffff00u, both.y >> 8 & 0xffff00u, both.z >> 8 & 0xffff00u, both.w >> 8 & 0xffff00u};
+          else
+            u = quad_words(e, p.seed, 1u, whole);
+          store_row(i + k, rkey, quad_codes(f, down, u, sign));
         }
         if constexpr (COL) {
           const float down[4] = {scale_down(byte[0]), scale_down(byte[1]), scale_down(byte[2]), scale_down(byte[3])};
-          r[k] = quad_codes(f, down, quad_words(e, p.seed, 0u, whole), sign);
+          u32x4 u{};
+          if constexpr (Source::HALVES)
+            u = u32x4{both.x << 8, both.y << 8, both.z << 8, both.w << 8};  // the low 24 bits count
+          else
+            u = quad_words(e, p.seed, 0u, whole);
+          r[k] = quad_codes(f, down, u, sign);
         }
         __builtin_amdgcn_sched_barrier(0);  // one row at a time: fewer registers, more waves
       }
@@ -283,7 +311,7 @@ __global__ __launch_bounds__(QT) void fp8_tile_kernel(Fp8QuantParams p) {
   __shared__ __attribute__((aligned(16))) uint8_t turned[COL ? TILE * TILE : 16];
   const int64_t block = block_id();
   if (block >= fp8_blocks(p.rows) * fp8_blocks(p.cols)) return;
-  quantize_tile<T, ROW, COL, SQUARE, SR>(p, (uint32_t)block, turned);
+  quantize_tile<MatrixSource<T>, ROW, COL, SQUARE, SR>(p, (uint32_t)block, turned);
 }
 __global__ __launch_bounds__(QT) void fp8_turn_kernel(Fp8Turn t) {
   __shared__ TurnLds sh;
@@ -299,12 +327,117 @@ __global__ __launch_bounds__(QT) void fp8_tile_turn_kernel(Fp8QuantParams p, Fp8
   __shared__ __attribute__((aligned(16))) uint8_t room[sizeof(TurnLds) > TILE * TILE ? sizeof(TurnLds) : TILE * TILE];
   const uint32_t before = blockIdx.x / step;  // of those that lay out, up to `turns`
   if (before >= turns || blockIdx.x - before * step != step - 1) {
-    quantize_tile<T, true, true, false, SR>(p, blockIdx.x - (before < turns ? before : turns), room);
+    quantize_tile<MatrixSource<T>, true, true, false, SR>(p, blockIdx.x - (before < turns ? before : turns), room);
   } else {
     const bool first = before < turns_a;
     const Fp8Turn t = first ? a : b;
     turn_tile(t.src, t.rows, fp8_pitch(t.K), t.dst, first ? before : before - turns_a, *reinterpret_cast<TurnLds*>(room));
   }
+}
+
+// ---------------------------------------------------------------------------
+// The gradients of a gated layer's two pre-activations, D = [G d_gate | G d_up]
+// [rows, 2 hidden], formed in float32 as they are quantized: G and the
+// checkpoints are read, both operands written, nothing in between.  A tile is
+// one of D, whose columns hidden .. 2 hidden - 1 read G once more.
+// ---------------------------------------------------------------------------
+template <class G>
+struct GatedSource {
+  typedef float Elem;
+  static constexpr bool HALVES = true;
+  const G* g;
+  const uint8_t *q, *e, *q_up, *e_up;  // of the half that col lies in; of the second
+  const G* g0;                         // column 0 of g's rows
+  int64_t ldx, pitch, rows;
+  int at, left, col, hidden;           // column within the half, columns of it from there on; column of D
+  __device__ __forceinline__ GatedSource(const GatedQuantParams& p, int64_t row, int64_t c)
+      : ldx(p.q.ldx), pitch(kept_pitch(p.hidden)), rows(p.q.rows - row), col((int)c), hidden((int)p.hidden) {
+    const bool up = c >= hidden;
+    at = col - (up ? hidden : 0);
+    left = hidden - at;
+    g0 = static_cast<const G*>(p.q.x) + row * ldx;
+    g = g0 + at;
+    q_up = p.q_up + row * pitch;
+    e_up = p.e_up + row * (pitch / KEPT_BLOCK);
+    q = up ? q_up : p.q_gate + row * pitch;
+    e = up ? e_up : p.e_gate + row * (pitch / KEPT_BLOCK);
+  }
+  static __device__ __forceinline__ void decode(uint32_t codes, float scale, float (&d)[4]) {
+    const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, scale, false);
+    const auto hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, scale, true);
+    d[0] = lo[0];
+    d[1] = lo[1];
+    d[2] = hi[0];
+    d[3] = hi[1];
+  }
+  __device__ __forceinline__ void load(int i, Quad<float>& v) const {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v.v[j] = 0.0f;
+    if (i >= rows || left <= 0) return;
+    const uint8_t* const qi = q + i * pitch;
+    const uint8_t* const ei = e + i * (pitch / KEPT_BLOCK);
+    float gv[4], d[4];
+    if ((hidden & 3) == 0) {  // four columns of one half and one block
+      load_vec<G, 4>(g + i * ldx, gv);
+      uint32_t codes;
+      __builtin_memcpy(&codes, qi + at, 4);
+      decode(codes, scale_up(ei[at / KEPT_BLOCK]), d);
+    } else if (left >= 4) {  // four of one half, but perhaps of two blocks
+      load_vec<G, 4>(g + i * ldx, gv);
+      uint32_t codes;
+      __builtin_memcpy(&codes, qi + at, 4);
+      decode(codes, 1.0f, d);
+      const float s0 = scale_up(ei[at / KEPT_BLOCK]), s1 = scale_up(ei[(at + 3) / KEPT_BLOCK]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) d[j] *= (at + j) / KEPT_BLOCK == at / KEPT_BLOCK ? s0 : s1;
+    } else {  // across the halves, or the last ones
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bool here = j < left, next = !here && col + j < 2 * hidden;
+        const int c = here ? at + j : j - left;
+        float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        gv[j] = 0.0f;
+        if (here || next) {
+          gv[j] = (float)g0[i * ldx + c];
+          const uint8_t* const qj = here ? qi : q_up + i * pitch;
+          const uint8_t* const ej = here ? ei : e_up + i * (pitch / KEPT_BLOCK);
+          decode(qj[c], scale_up(ej[c / KEPT_BLOCK]), f);
+        }
+        d[j] = f[0];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v.v[j] = gv[j] * d[j];
+  }
+};
+struct GatedTile : GatedQuantParams {
+  __device__ __forceinline__ operator const Fp8QuantParams&() const { return q; }
+};
+template <class G, bool ROW, bool COL, bool SR>
+__global__ __launch_bounds__(QT) void gated_tile_kernel(GatedTile p) {
+  __shared__ __attribute__((aligned(16))) uint8_t turned[COL ? TILE * TILE : 16];
+  const int64_t block = block_id();
+  if (block >= fp8_blocks(p.q.rows) * fp8_blocks(p.q.cols)) return;
+  quantize_tile<GatedSource<G>, ROW, COL, false, SR>(p, (uint32_t)block, turned);
+}
+
+hipError_t launch_gated_quantize(fqt_dtype type, const GatedQuantParams& params, hipStream_t s) {
+  const GatedTile p{params};
+  const int64_t blocks = fp8_blocks(p.q.rows) * fp8_blocks(p.q.cols);
+  if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+  return with_type(type, [&](auto e) {
+    using T = decltype(e);
+    auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, grid_of(blocks, QT), dim3(QT), 0, s, p);
+      return hipGetLastError();
+    };
+    auto pick = [&](auto sr) {
+      constexpr bool S = decltype(sr)::value;
+      if (p.q.q_row && p.q.q_col) return go(gated_tile_kernel<T, true, true, S>);
+      return p.q.q_row ? go(gated_tile_kernel<T, true, false, S>) : go(gated_tile_kernel<T, false, true, S>);
+    };
+    return p.q.stochastic ? pick(std::true_type{}) : pick(std::false_type{});
+  });
 }
 
 constexpr int64_t MOST_BLOCKS = (((int64_t)1 << 32) - 1) / QT;  // of one dimension: operands of 2^38 bytes

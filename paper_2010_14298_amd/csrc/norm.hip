@@ -15,7 +15,7 @@
 // quarters of the time for their loads.  float32 (101 MB): 24.0 us, 4.2 TB/s, waits
 // half of the time.  One row of 4096 bfloat16 forward: 3.0 us, a launch and a chain
 // of latencies.
-#include "train_kernels.h"
+#include "fp8_codes.h"
 
 namespace fqt {
 
@@ -53,7 +53,64 @@ __device__ __forceinline__ void team_sum(float (&v)[N], float (*sh)[N]) {
   }
 }
 
-template <class T, class C>
+// ---------------------------------------------------------------------------
+// Checkpoints of xh: V neighbouring elements a thread, so that the threads of a
+// block of 32 are neighbours in a wave (and all of them, or none, come here).
+// ---------------------------------------------------------------------------
+template <int V>
+struct CodesOf {
+  typedef uint8_t type __attribute__((ext_vector_type(V), aligned(V)));
+};
+// The thread's codes of v at column col of a row; values past the row are 0.
+template <int V>
+__device__ __forceinline__ void keep_codes(uint8_t* q, uint8_t* e, int64_t cols, int64_t col, const float (&v)[V]) {
+  static_assert(V == 2 || V == 4 || V == 8, "16, 8 or 4 threads a block");
+  uint32_t key = 0u;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const uint32_t m = __float_as_uint(v[i]) & 0x7fffffffu;
+    key = key > m ? key : m;
+  }
+  auto larger = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
+  key = larger(key, dpp<0xB1>(key));                         // lanes 1, 0, 3, 2 of four
+  key = larger(key, dpp<0x4E>(key));                         // lanes 2, 3, 0, 1
+  if constexpr (V <= 4) key = larger(key, dpp<0x141>(key));  // eight lanes reversed
+  if constexpr (V == 2) key = larger(key, dpp<0x140>(key));  // sixteen lanes reversed
+  key = Quad<float>::key(key);
+  if (col >= kept_pitch(cols)) return;
+  const uint32_t byte = scale_bytes(key) & 0xffffu;
+  const float scale = scale_up(byte);
+  typename CodesOf<V>::type w;
+#pragma unroll
+  for (int i = 0; i < V; i += 2) {
+    const s16x2 c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(s16x2{0, 0}, v[i], v[i + 1], scale, false);
+    const uint32_t both = key >= NAN_KEY ? 0x7f7fu : as<uint32_t>(c);
+    w[i] = (uint8_t)both;
+    w[i + 1] = (uint8_t)(both >> 8);
+  }
+  *reinterpret_cast<typename CodesOf<V>::type*>(q + col) = w;
+  if (col % KEPT_BLOCK == 0) e[col / KEPT_BLOCK] = stored_byte(key, byte);
+}
+// What the checkpoint has there: 0 past the row.
+template <int V>
+__device__ __forceinline__ void kept_values(const uint8_t* q, const uint8_t* e, int64_t n, int64_t col, float (&v)[V]) {
+  if (n <= 0) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = 0.0f;
+    return;
+  }
+  const auto w = *reinterpret_cast<const typename CodesOf<V>::type*>(q + col);
+  const float scale = scale_up(e[col / KEPT_BLOCK]);
+#pragma unroll
+  for (int i = 0; i < V; i += 2) {
+    const auto f = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[i] | (uint32_t)w[i + 1] << 8, scale, false);
+    v[i] = i < n ? f[0] : 0.0f;
+    v[i + 1] = i + 1 < n ? f[1] : 0.0f;
+  }
+}
+
+// KEEP: also the checkpoint of xh.
+template <class T, class C, bool KEEP>
 __global__ __launch_bounds__(C::THREADS) void norm_forward_kernel(NormParams p) {
   __shared__ float sh[C::WAVES][1];
   const int t = threadIdx.x % C::TPR;
@@ -102,15 +159,21 @@ __global__ __launch_bounds__(C::THREADS) void norm_forward_kernel(NormParams p) 
     }
     if (p.gamma) load_part<float, C::VEC>(p.gamma + col, p.cols - col, ga);
     if (p.beta) load_part<float, C::VEC>(p.beta + col, p.cols - col, be);
+    if constexpr (KEEP) {
 #pragma unroll
-    for (int i = 0; i < C::VEC; ++i) o[i] = fmaf((v[k][i] - mean) * rstd, ga[i], be[i]);
+      for (int i = 0; i < C::VEC; ++i) v[k][i] = col + i < p.cols ? (v[k][i] - mean) * rstd : 0.0f;
+      const int64_t pitch = kept_pitch(p.cols);
+      keep_codes<C::VEC>(p.q8 + row * pitch, p.e8 + row * (pitch / KEPT_BLOCK), p.cols, col, v[k]);
+    }
+#pragma unroll
+    for (int i = 0; i < C::VEC; ++i) o[i] = fmaf(KEEP ? v[k][i] : (v[k][i] - mean) * rstd, ga[i], be[i]);
     store_part<T, C::VEC>(y + col, p.cols - col, o);
   }
 }
 
 // Rows longer than a team's registers: the row is read three times (sum,
 // squares, output), the later ones from the caches.
-template <class T, class C>
+template <class T, class C, bool KEEP>
 __global__ __launch_bounds__(C::THREADS) void norm_forward_long_kernel(NormParams p) {
   __shared__ float sh[C::WAVES][1];
   const int64_t row = block_id();
@@ -143,12 +206,16 @@ __global__ __launch_bounds__(C::THREADS) void norm_forward_long_kernel(NormParam
     if (p.rstd) p.rstd[row] = rstd;
   }
   T* y = static_cast<T*>(p.y) + row * p.ldy;
-  for (int64_t col = first; col < p.cols; col += step) {
+  const int64_t pitch = kept_pitch(p.cols);
+  for (int64_t col = first; col < (KEEP ? pitch : p.cols); col += step) {  // KEEP: whole blocks stay together
     load_part<T, C::VEC>(x + col, p.cols - col, v);
 #pragma unroll
+    for (int i = 0; i < C::VEC; ++i) v[i] = col + i < p.cols ? (v[i] - mean) * rstd : 0.0f;
+    if constexpr (KEEP)
+      keep_codes<C::VEC>(p.q8 + row * pitch, p.e8 + row * (pitch / KEPT_BLOCK), p.cols, col, v);
+#pragma unroll
     for (int i = 0; i < C::VEC; ++i)
-      if (col + i < p.cols)
-        v[i] = fmaf((v[i] - mean) * rstd, p.gamma ? p.gamma[col + i] : 1.0f, p.beta ? p.beta[col + i] : 0.0f);
+      if (col + i < p.cols) v[i] = fmaf(v[i], p.gamma ? p.gamma[col + i] : 1.0f, p.beta ? p.beta[col + i] : 0.0f);
     store_part<T, C::VEC>(y + col, p.cols - col, v);
   }
 }
@@ -159,7 +226,8 @@ __global__ __launch_bounds__(C::THREADS) void norm_forward_long_kernel(NormParam
 // sums of g xh and g in registers; at the end the block's teams meet in LDS
 // pairwise and one writes the block's partial row (an only block writes the
 // parameter gradients themselves).
-template <class T, class C>
+// KEPT: xh from its checkpoint.
+template <class T, class C, bool KEPT>
 __global__ __launch_bounds__(C::THREADS) void norm_backward_kernel(NormParams p) {
   __shared__ float sh[C::PER_BLOCK][C::WAVES][2];
   __shared__ __attribute__((aligned(16))) float col_sum[C::PER_BLOCK > 1 ? C::PER_BLOCK / 2 : 1][2][C::PER_BLOCK > 1 ? C::COLS : 4];
@@ -178,14 +246,18 @@ __global__ __launch_bounds__(C::THREADS) void norm_backward_kernel(NormParams p)
     const int cols = any ? (int)p.cols : 0;
     const T* x = static_cast<const T*>(p.x) + row * p.ldx;
     const T* g = static_cast<const T*>(p.g) + row * p.ldg;
+    const int64_t pitch = kept_pitch(p.cols);
     float xh[C::NV][C::VEC], gv[C::NV][C::VEC];
 #pragma unroll
     for (int k = 0; k < C::NV; ++k) {
       const int col = (k * C::TPR + t) * C::VEC;
-      load_part<T, C::VEC>(x + col, cols - col, xh[k]);
+      if constexpr (KEPT)
+        kept_values<C::VEC>(p.q8 + row * pitch, p.e8 + row * (pitch / KEPT_BLOCK), cols - col, col, xh[k]);
+      else
+        load_part<T, C::VEC>(x + col, cols - col, xh[k]);
       load_part<T, C::VEC>(g + col, cols - col, gv[k]);
     }
-    const float mean = p.mean[row], rstd = p.rstd[row];
+    const float mean = KEPT ? 0.0f : p.mean[row], rstd = p.rstd[row];
     float s[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int k = 0; k < C::NV; ++k) {
@@ -199,7 +271,7 @@ __global__ __launch_bounds__(C::THREADS) void norm_backward_kernel(NormParams p)
 #pragma unroll
       for (int i = 0; i < C::VEC; ++i) {
         // no column (or no row): xh is 0 like g, since (0 - mean) rstd may be infinite
-        xh[k][i] = col + i < cols ? (xh[k][i] - mean) * rstd : 0.0f;
+        if constexpr (!KEPT) xh[k][i] = col + i < cols ? (xh[k][i] - mean) * rstd : 0.0f;
         sg[k][i] = fmaf(gv[k][i], xh[k][i], sg[k][i]);
         sb[k][i] += gv[k][i];
         gv[k][i] *= ga[i];
@@ -260,7 +332,7 @@ __global__ __launch_bounds__(C::THREADS) void norm_backward_kernel(NormParams p)
 }
 
 // Rows longer than a team's registers: inputs read twice, no parameter sums.
-template <class T, class C>
+template <class T, class C, bool KEPT>
 __global__ __launch_bounds__(C::THREADS) void norm_backward_long_kernel(NormParams p) {
   __shared__ float sh[C::WAVES][2];
   const int64_t row = block_id();
@@ -268,30 +340,40 @@ __global__ __launch_bounds__(C::THREADS) void norm_backward_long_kernel(NormPara
   const T* x = static_cast<const T*>(p.x) + row * p.ldx;
   const T* g = static_cast<const T*>(p.g) + row * p.ldg;
   T* y = static_cast<T*>(p.y) + row * p.ldy;
-  const float mean = p.mean[row], rstd = p.rstd[row], inv = 1.0f / (float)p.cols;
+  const float mean = KEPT ? 0.0f : p.mean[row], rstd = p.rstd[row], inv = 1.0f / (float)p.cols;
+  const uint8_t* const q8 = p.q8 + row * kept_pitch(p.cols);
+  const uint8_t* const e8 = p.e8 + row * kept_blocks(p.cols);
+  auto load_xh = [&](int64_t col, float (&v)[C::VEC]) __attribute__((always_inline)) {
+    if constexpr (KEPT) {
+      kept_values<C::VEC>(q8, e8, p.cols - col, col, v);
+    } else {
+      load_part<T, C::VEC>(x + col, p.cols - col, v);
+#pragma unroll
+      for (int i = 0; i < C::VEC; ++i) v[i] = col + i < p.cols ? (v[i] - mean) * rstd : 0.0f;  // (0 - mean) rstd may be infinite
+    }
+  };
   const int64_t step = (int64_t)C::TPR * C::VEC, first = (int64_t)threadIdx.x * C::VEC;
   float xv[C::VEC], gv[C::VEC];
   float s[2] = {0.0f, 0.0f};
   for (int64_t col = first; col < p.cols; col += step) {
-    load_part<T, C::VEC>(x + col, p.cols - col, xv);
+    load_xh(col, xv);
     load_part<T, C::VEC>(g + col, p.cols - col, gv);
 #pragma unroll
     for (int i = 0; i < C::VEC; ++i) {
-      const bool in = col + i < p.cols;
-      const float c = gv[i] * (p.gamma && in ? p.gamma[col + i] : 1.0f);
+      const float c = gv[i] * (p.gamma && col + i < p.cols ? p.gamma[col + i] : 1.0f);
       s[0] += c;
-      s[1] = fmaf(c, in ? (xv[i] - mean) * rstd : 0.0f, s[1]);  // (0 - mean) rstd may be infinite
+      s[1] = fmaf(c, xv[i], s[1]);
     }
   }
   team_sum<C, 2>(s, sh);
   const float a = s[0] * inv, b = s[1] * inv;
   for (int64_t col = first; col < p.cols; col += step) {
-    load_part<T, C::VEC>(x + col, p.cols - col, xv);
+    load_xh(col, xv);
     load_part<T, C::VEC>(g + col, p.cols - col, gv);
 #pragma unroll
     for (int i = 0; i < C::VEC; ++i) {
       const float c = gv[i] * (p.gamma && col + i < p.cols ? p.gamma[col + i] : 1.0f);
-      gv[i] = rstd * ((c - a) - (xv[i] - mean) * rstd * b);
+      gv[i] = rstd * ((c - a) - xv[i] * b);
     }
     store_part<T, C::VEC>(y + col, p.cols - col, gv);
   }
@@ -299,15 +381,21 @@ __global__ __launch_bounds__(C::THREADS) void norm_backward_long_kernel(NormPara
 
 // The parameter sums of long rows: a block takes 256 columns of a run of rows.
 constexpr int LONG_RUNS = 64;
-template <class T>
+template <class T, bool KEPT>
 __global__ __launch_bounds__(256) void norm_columns_kernel(NormParams p) {
   const int64_t col = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (col >= p.cols) return;
   float sg = 0.0f, sb = 0.0f;
   for (int64_t row = blockIdx.y; row < p.rows; row += gridDim.y) {
     const float g = (float)static_cast<const T*>(p.g)[row * p.ldg + col];
-    const float x = (float)static_cast<const T*>(p.x)[row * p.ldx + col];
-    sg = fmaf(g, (x - p.mean[row]) * p.rstd[row], sg);
+    float xh;
+    if constexpr (KEPT) {
+      const int64_t pitch = kept_pitch(p.cols);
+      xh = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(p.q8[row * pitch + col], scale_up(p.e8[(row * pitch + col) / KEPT_BLOCK]), false)[0];
+    } else {
+      xh = ((float)static_cast<const T*>(p.x)[row * p.ldx + col] - p.mean[row]) * p.rstd[row];
+    }
+    sg = fmaf(g, xh, sg);
     sb += g;
   }
   p.part[(int64_t)blockIdx.y * 2 * p.cols + col] = sg;
@@ -363,19 +451,23 @@ static hipError_t with_team(int64_t cols, F f) {
 }
 constexpr int64_t TEAM_COLS = 1024 * 16;
 
+template <class T, bool KEEP>
+static hipError_t norm_forward(const NormParams& p, hipStream_t s) {
+  return with_team<T>(p.cols, [&](auto c) {
+    using C = decltype(c);
+    const int64_t blocks = (p.rows + C::PER_BLOCK - 1) / C::PER_BLOCK;
+    const dim3 grid = grid_of(blocks, C::THREADS);
+    if (p.cols <= TEAM_COLS)
+      hipLaunchKernelGGL((norm_forward_kernel<T, C, KEEP>), grid, dim3(C::THREADS), 0, s, p);
+    else if constexpr (C::TPR == 1024)
+      hipLaunchKernelGGL((norm_forward_long_kernel<T, C, KEEP>), grid, dim3(C::THREADS), 0, s, p);
+    return hipGetLastError();
+  });
+}
 hipError_t launch_norm_forward(fqt_dtype type, const NormParams& p, hipStream_t s) {
   return with_type(type, [&](auto e) {
     using T = decltype(e);
-    return with_team<T>(p.cols, [&](auto c) {
-      using C = decltype(c);
-      const int64_t blocks = (p.rows + C::PER_BLOCK - 1) / C::PER_BLOCK;
-      const dim3 grid = grid_of(blocks, C::THREADS);
-      if (p.cols <= TEAM_COLS)
-        hipLaunchKernelGGL((norm_forward_kernel<T, C>), grid, dim3(C::THREADS), 0, s, p);
-      else if constexpr (C::TPR == 1024)
-        hipLaunchKernelGGL((norm_forward_long_kernel<T, C>), grid, dim3(C::THREADS), 0, s, p);
-      return hipGetLastError();
-    });
+    return p.q8 ? norm_forward<T, true>(p, s) : norm_forward<T, false>(p, s);
   });
 }
 
@@ -401,23 +493,27 @@ static int64_t backward_blocks(int64_t rows, int64_t cols) {
 }
 int64_t norm_backward_partials(int64_t rows, int64_t cols) { return backward_blocks(rows, cols) * 2 * cols; }
 
+template <class T, bool KEPT>
+static hipError_t norm_backward(const NormParams& p, bool sums, int64_t blocks, hipStream_t s) {
+  return with_block<T>(p.cols, [&](auto c) {
+    using C = decltype(c);
+    if (p.cols <= TEAM_COLS) {
+      hipLaunchKernelGGL((norm_backward_kernel<T, C, KEPT>), dim3((unsigned)blocks), dim3(C::THREADS), 0, s, p);
+    } else if constexpr (C::TPR == 1024) {
+      hipLaunchKernelGGL((norm_backward_long_kernel<T, C, KEPT>), grid_of(p.rows, C::THREADS), dim3(C::THREADS), 0, s, p);
+      if (sums)
+        hipLaunchKernelGGL((norm_columns_kernel<T, KEPT>), dim3((unsigned)((p.cols + 255) / 256), (unsigned)blocks),
+                           dim3(256), 0, s, p);
+    }
+    return hipGetLastError();
+  });
+}
 hipError_t launch_norm_backward(fqt_dtype type, const NormParams& p, hipStream_t s) {
   const bool sums = p.grad_gamma || p.grad_beta;
   const int64_t blocks = backward_blocks(p.rows, p.cols);
   const hipError_t e = with_type(type, [&](auto el) {
     using T = decltype(el);
-    return with_block<T>(p.cols, [&](auto c) {
-      using C = decltype(c);
-      if (p.cols <= TEAM_COLS) {
-        hipLaunchKernelGGL((norm_backward_kernel<T, C>), dim3((unsigned)blocks), dim3(C::THREADS), 0, s, p);
-      } else if constexpr (C::TPR == 1024) {
-        hipLaunchKernelGGL((norm_backward_long_kernel<T, C>), grid_of(p.rows, C::THREADS), dim3(C::THREADS), 0, s, p);
-        if (sums)
-          hipLaunchKernelGGL((norm_columns_kernel<T>), dim3((unsigned)((p.cols + 255) / 256), (unsigned)blocks),
-                             dim3(256), 0, s, p);
-      }
-      return hipGetLastError();
-    });
+    return p.q8 ? norm_backward<T, true>(p, sums, blocks, s) : norm_backward<T, false>(p, sums, blocks, s);
   });
   if (e != hipSuccess || !sums || (blocks == 1 && p.cols <= TEAM_COLS)) return e;
   hipLaunchKernelGGL(norm_reduce_kernel, grid_of((2 * p.cols + 63) / 64, 64 * REDUCE_WAVES), dim3(64 * REDUCE_WAVES),

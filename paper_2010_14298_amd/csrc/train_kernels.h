@@ -136,6 +136,10 @@ struct NormParams {
   float* grad_gamma;   // both null: not formed
   float* grad_beta;
   float* part;         // [blocks][2][cols]
+  // checkpoint of xh (null: none): written by the forward, read by the backward
+  // in place of x and mean
+  uint8_t* q8;
+  uint8_t* e8;
 };
 hipError_t launch_norm_forward(fqt_dtype type, const NormParams& p, hipStream_t s);
 int64_t norm_backward_partials(int64_t rows, int64_t cols);  // floats
@@ -149,6 +153,16 @@ constexpr int FP8_BLOCK = 128;
 __host__ __device__ inline int64_t fp8_blocks(int64_t K) { return (K + FP8_BLOCK - 1) / FP8_BLOCK; }
 __host__ __device__ inline int64_t fp8_pitch(int64_t K) { return fp8_blocks(K) * FP8_BLOCK; }
 __host__ __device__ inline int64_t fp8_exp_bytes(int64_t rows, int64_t K) { return (fp8_blocks(K) + 3) / 4 * 4 * rows; }
+
+// Checkpoints: codes [rows, pitch], pitch = whole blocks of 32, and one scale
+// byte for each block, [rows, pitch / 32].
+constexpr int KEPT_BLOCK = 32;
+__host__ __device__ inline int64_t kept_blocks(int64_t cols) { return (cols + KEPT_BLOCK - 1) / KEPT_BLOCK; }
+__host__ __device__ inline int64_t kept_pitch(int64_t cols) { return kept_blocks(cols) * KEPT_BLOCK; }
+struct Kept {
+  uint8_t* q;  // null: none
+  uint8_t* e;
+};
 
 struct Fp8QuantParams {
   const void* x;
@@ -195,6 +209,28 @@ hipError_t launch_fp8_rows(fqt_dtype type, const Fp8GemmParams& p, const void* x
 int64_t fp8_gemm_partials(int64_t M, int64_t N, int64_t K);  // floats
 fqt_fp8_form fp8_gemm_form(int64_t M, int64_t N, int64_t K, bool masked, bool lines);
 hipError_t launch_fp8_gemm(fqt_dtype type, const Fp8GemmParams& p, hipStream_t s);
+
+// ---------------------------------------------------------------------------
+// gated layer
+// ---------------------------------------------------------------------------
+struct GatedParams {
+  const float* part;  // [N, 2 hidden]: a, then b
+  int64_t N, hidden;
+  fqt_act act;
+  void* H;
+  int64_t ldh;
+  Kept gate, up;
+};
+hipError_t launch_gated_finish(fqt_dtype type, const GatedParams& p, hipStream_t s);
+
+// The quantizer of D = [G gate | G up] [rows, cols = 2 hidden]: q.x, q.ldx are
+// G's.
+struct GatedQuantParams {
+  Fp8QuantParams q;
+  int64_t hidden;
+  const uint8_t *q_gate, *e_gate, *q_up, *e_up;
+};
+hipError_t launch_gated_quantize(fqt_dtype type, const GatedQuantParams& p, hipStream_t s);
 
 // ---------------------------------------------------------------------------
 // gradient norm and clipping

@@ -62,6 +62,10 @@ class Fp8(ctypes.Structure):
     _fields_ = [("q", ctypes.c_void_p), ("exp", ctypes.c_void_p), ("k_major", ctypes.c_int32)]
 
 
+class Kept(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("exp", ctypes.c_void_p)]
+
+
 EXPORTS = [
     "fqt_quantize_ptq", "fqt_quantize_psq", "fqt_quantize_psq_noalloc", "fqt_quantize_bhq", "fqt_quantize_shift", "fqt_quantize_workspace",
     "fqt_quantize_seeds",
@@ -75,6 +79,9 @@ EXPORTS = [
     "fqt_fp8_gemm_form",
     "fqt_fp8_linear_forward", "fqt_fp8_linear_forward_workspace",
     "fqt_fp8_linear_backward", "fqt_fp8_linear_backward_workspace",
+    "fqt_fp8_kept_pitch", "fqt_layernorm_forward8", "fqt_layernorm_backward8",
+    "fqt_fp8_gated_forward", "fqt_fp8_gated_forward_workspace",
+    "fqt_fp8_gated_backward", "fqt_fp8_gated_backward_workspace",
     "fqt_grad_norm_clip", "fqt_grad_norm_clip_workspace",
     "fqt_probe_mfma_i8", "fqt_probe_copy",
     "fqt_workspace_status", "fqt_status_str", "fqt_version",
@@ -97,6 +104,7 @@ def load(path=LIB_PATH):
     cfgp = ctypes.POINTER(BwdCfg)
     shp = ctypes.POINTER(ConvShape)
     f8p = ctypes.POINTER(Fp8)
+    kep = ctypes.POINTER(Kept)
     f32 = ctypes.c_float
     sig = {
         "fqt_quantize_ptq": ([vp, i64, i64, i32, i32, u64, u32, i32, qtp, vp, sz, vp], i32),
@@ -132,6 +140,14 @@ def load(path=LIB_PATH):
         "fqt_fp8_linear_backward": ([vp, i32, i64, i64, i64, f8p, f8p, i64, i32, u64, vp, i64, vp, vp, i64, vp, sz,
                                      vp], i32),
         "fqt_fp8_linear_backward_workspace": ([i64, i64, i64], sz),
+        "fqt_fp8_kept_pitch": ([i64], sz),
+        "fqt_layernorm_forward8": ([vp, i32, i64, i64, i64, vp, vp, f32, vp, i64, kep, vp, vp], i32),
+        "fqt_layernorm_backward8": ([vp, i64, kep, i32, i64, i64, vp, vp, vp, i64, vp, vp, vp, sz, vp], i32),
+        "fqt_fp8_gated_forward": ([vp, i32, i64, i64, i64, f8p, i64, i32, vp, i64, f8p, kep, kep, vp, sz, vp], i32),
+        "fqt_fp8_gated_forward_workspace": ([i64, i64, i64], sz),
+        "fqt_fp8_gated_backward": ([vp, i32, i64, i64, i64, kep, kep, f8p, f8p, i64, i32, u64, vp, vp, i64, vp, sz,
+                                    vp], i32),
+        "fqt_fp8_gated_backward_workspace": ([i64, i64, i64], sz),
         "fqt_grad_norm_clip": ([vp, vp, vp, vp, i64, ctypes.c_double, vp, vp, sz, vp], i32),
         "fqt_grad_norm_clip_workspace": ([i64], sz),
         "fqt_probe_mfma_i8": ([i64, vp, ctypes.POINTER(ctypes.c_double), vp], i32),
@@ -703,6 +719,161 @@ def fqt_fp8_linear_backward(G, X8t, W8t, seed=0, stochastic=True, relu_input=Non
                                      _here(grad_W, "grad_W", dev).data_ptr(), px, ldgx, ws.data_ptr(), ws.numel(),
                                      _raw_stream(dev))
     _check("fqt_fp8_linear_backward", rc)
+    return grad_W, grad_X, ws
+
+
+def fp8_kept(rows, cols, device):
+    """An empty checkpoint of activations [rows, cols] in 8 bits: dict(q=codes [rows, cols padded to whole blocks of
+    32], exp=scale bytes [rows, blocks], cols=cols)."""
+    blocks = (cols + 31) // 32
+    return dict(q=torch.empty((rows, blocks * 32), dtype=torch.float8_e4m3fn, device=device),
+                exp=torch.empty((rows, blocks), dtype=torch.uint8, device=device), cols=cols)
+
+
+def _new_kept(like, rows, cols):
+    """fp8_kept on the device of `like`, and its C struct."""
+    blocks = (cols + 31) // 32
+    q = like.new_empty((rows, blocks * 32), dtype=torch.float8_e4m3fn)
+    e = like.new_empty((rows, blocks), dtype=torch.uint8)
+    return dict(q=q, exp=e, cols=cols), Kept(q.data_ptr(), e.data_ptr())
+
+
+def _kept(a, name, dev, rows, cols):
+    """The C struct of a checkpoint, checked against the rows and columns that the call needs."""
+    q, e = a["q"], a["exp"]
+    blocks = (cols + 31) // 32
+    if a["cols"] != cols or q.shape != (rows, blocks * 32) or e.shape != (rows, blocks):
+        raise ValueError(f"{name} is not a checkpoint of [{rows}, {cols}]")
+    if q.dtype != torch.float8_e4m3fn or e.dtype != torch.uint8 or not q.is_contiguous() or not e.is_contiguous():
+        raise ValueError(f"{name} is not a checkpoint as fp8_kept lays it out")
+    return Kept(_here(q, name, dev).data_ptr(), _here(e, name, dev).data_ptr())
+
+
+def fqt_layernorm_forward8(X, gamma=None, beta=None, eps=1e-5, Y=None):
+    """Layer norm over the columns of X [rows, cols] with an 8-bit checkpoint of the normalized rows for its backward;
+    returns (Y, xh8, rstd)."""
+    dev = _device()
+    px, dt, rows, cols, ldx = _matrix(X, "X", dev)
+    if Y is None:
+        Y = X.new_empty((rows, cols))
+        py, ldy = Y.data_ptr(), cols
+    else:
+        py, _, _, _, ldy = _matrix(Y, "Y", dev, X.shape, X.dtype)
+    xh8, c8 = _new_kept(X, rows, cols)
+    rstd = X.new_empty(rows, dtype=torch.float32)
+    rc = load().fqt_layernorm_forward8(px, dt, rows, cols, ldx, _vector(gamma, "gamma", cols, dev),
+                                       _vector(beta, "beta", cols, dev), eps, py, ldy, c8, rstd.data_ptr(),
+                                       _raw_stream(dev))
+    _check("fqt_layernorm_forward8", rc)
+    return Y, xh8, rstd
+
+
+def fqt_layernorm_backward8(G, xh8, rstd, gamma=None, grad_X=None, params=True, ws=None):
+    """Gradient of fqt_layernorm_forward8; returns (grad_X, grad_gamma, grad_beta, ws).  params=False forms grad_X
+    only (the others are None).  The workspace is fqt_layernorm_backward's."""
+    dev = _device()
+    pg, dt, rows, cols, ldg = _matrix(G, "G", dev)
+    c8 = _kept(xh8, "xh8", dev, rows, cols)
+    if grad_X is None:
+        grad_X = G.new_empty((rows, cols))
+        py, ldgx = grad_X.data_ptr(), cols
+    else:
+        py, _, _, _, ldgx = _matrix(grad_X, "grad_X", dev, G.shape, G.dtype)
+    lib = load()
+    gg = gb = pgg = pgb = None
+    if ws is not None:
+        _room(ws, dev)
+    if params:
+        gg, gb = G.new_empty((2, cols), dtype=torch.float32).unbind(0)
+        pgg, pgb = gg.data_ptr(), gb.data_ptr()
+        if ws is None:
+            ws = G.new_empty(max(lib.fqt_layernorm_backward_workspace(rows, cols), 16), dtype=torch.uint8)
+    rc = lib.fqt_layernorm_backward8(pg, ldg, c8, dt, rows, cols, _vector(rstd, "rstd", rows, dev),
+                                     _vector(gamma, "gamma", cols, dev), py, ldgx, pgg, pgb,
+                                     ws.data_ptr() if ws is not None else None, ws.numel() if ws is not None else 0,
+                                     _raw_stream(dev))
+    _check("fqt_layernorm_backward8", rc)
+    return grad_X, gg, gb, ws
+
+
+ACTS = {"silu": 0, "gelu_tanh": 1, "relu": 2}
+
+
+def fqt_fp8_gated_forward_workspace(N, d_in, hidden):
+    return load().fqt_fp8_gated_forward_workspace(N, d_in, hidden)
+
+
+def fqt_fp8_gated_forward(X, W8, act="silu", save=True, H=None, ws=None):
+    """H = act(Q(X) W_gate^T) Q(X) W_up^T, W8 the by_row operand (tile=True) of [W_gate; W_up].  save: also what
+    fqt_fp8_gated_backward reads, dict(X8t=operand of X^T, d_gate, d_up=checkpoints of H's derivatives by the two
+    products).  Returns (H, kept or None, ws)."""
+    dev = _device()
+    px, dt, N, d_in, ldx = _matrix(X, "X", dev)
+    code = ACTS.get(act)
+    if code is None:
+        raise ValueError(f"act must be one of {', '.join(ACTS)}")
+    rows = W8["q"].shape[0]
+    if rows & 1:
+        raise ValueError("W8 holds the gate's rows, then as many others")
+    w8 = _fp8(W8, "W8", dev, rows, d_in)
+    hidden = rows // 2
+    if H is None:
+        H = X.new_empty((N, hidden))
+        ph, ldh = H.data_ptr(), hidden
+    else:
+        ph, _, _, _, ldh = _matrix(H, "H", dev, (N, hidden), X.dtype)
+    kept = x8t = cg = cu = None
+    if save:
+        X8t, x8t = _new_fp8(X, d_in, N)
+        d_gate, cg = _new_kept(X, N, hidden)
+        d_up, cu = _new_kept(X, N, hidden)
+        kept = dict(X8t=X8t, d_gate=d_gate, d_up=d_up)
+    lib = load()
+    if ws is None:
+        ws = X.new_empty(lib.fqt_fp8_gated_forward_workspace(N, d_in, hidden), dtype=torch.uint8)
+    else:
+        _room(ws, dev)
+    rc = lib.fqt_fp8_gated_forward(px, dt, N, d_in, ldx, w8, hidden, code, ph, ldh, x8t, cg, cu, ws.data_ptr(),
+                                   ws.numel(), _raw_stream(dev))
+    _check("fqt_fp8_gated_forward", rc)
+    return H, kept, ws
+
+
+def fqt_fp8_gated_backward_workspace(N, d_in, hidden):
+    return load().fqt_fp8_gated_backward_workspace(N, d_in, hidden)
+
+
+def fqt_fp8_gated_backward(G, kept, W8t, seed=0, stochastic=True, input_grad=True, grad_W=None, grad_X=None, ws=None):
+    """Gradients of fqt_fp8_gated_forward from G = dL/dH [N, hidden] and what it kept: grad_W [2 hidden, d_in]
+    (float32) and grad_X [N, d_in] (G's type), W8t the by_col operand of [W_gate; W_up].  input_grad=False forms
+    grad_W only (grad_X is None; W8t may be None).  Returns (grad_W, grad_X, ws)."""
+    dev = _device()
+    pg, dt, N, hidden, ldg = _matrix(G, "G", dev)
+    d_in = kept["X8t"]["q"].shape[0]
+    x8t = _fp8(kept["X8t"], "X8t", dev, d_in, N)
+    cg, cu = _kept(kept["d_gate"], "d_gate", dev, N, hidden), _kept(kept["d_up"], "d_up", dev, N, hidden)
+    w8t = _fp8(W8t, "W8t", dev, d_in, 2 * hidden)
+    if grad_W is None:
+        grad_W = G.new_empty((2 * hidden, d_in), dtype=torch.float32)
+    elif grad_W.dtype != torch.float32 or grad_W.shape != (2 * hidden, d_in) or not grad_W.is_contiguous():
+        raise ValueError("grad_W must be a contiguous float32 tensor [2 hidden, d_in]")
+    px, ldgx = None, 0
+    if not input_grad:
+        grad_X = None
+    elif grad_X is None:
+        grad_X = G.new_empty((N, d_in))
+        px, ldgx = grad_X.data_ptr(), d_in
+    else:
+        px, _, _, _, ldgx = _matrix(grad_X, "grad_X", dev, (N, d_in), G.dtype)
+    lib = load()
+    if ws is None:
+        ws = G.new_empty(lib.fqt_fp8_gated_backward_workspace(N, d_in, hidden), dtype=torch.uint8)
+    else:
+        _room(ws, dev)
+    rc = lib.fqt_fp8_gated_backward(pg, dt, N, hidden, ldg, cg, cu, x8t, w8t, d_in, int(bool(stochastic)), seed,
+                                    _here(grad_W, "grad_W", dev).data_ptr(), px, ldgx, ws.data_ptr(), ws.numel(),
+                                    _raw_stream(dev))
+    _check("fqt_fp8_gated_backward", rc)
     return grad_W, grad_X, ws
 
 

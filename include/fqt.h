@@ -508,8 +508,10 @@ size_t fqt_fp8_gated_forward_workspace(int64_t N, int64_t d_in, int64_t hidden);
  *   grad_W [2 hidden, d_in] = Q1(D)^T X8t^T   (D^T in blocks of 128 along N)
  *   grad_X [N, d_in]        = Q2(D) W8t^T     (D in blocks of 128 along 2 hidden)
  * to nearest or (stochastic != 0) unbiased with one random word an element of D
- * (stream 2), as in the other quantizers with u = 2^8 times the word's low 16
- * bits for Q1 and its high 16 bits for Q2.  X8t [d_in, K = N], d_gate and d_up
+ * (stream 2), u its low 16 bits for Q1 and its high 16 bits for Q2: up iff
+ * 2^4 u < floor(frac 2^20), frac as in fqt_fp8_quantize.  (Up to 2^-16 of a step
+ * that is exact where frac has 16 bits, as for 16-bit G and results that are
+ * not below the format's normal numbers.)  X8t [d_in, K = N], d_gate and d_up
  * from the forward, W8t [d_in, K = 2 hidden] the weights' by_col operand.
  * grad_W or grad_X may be NULL (not formed; its operand may then be NULL too).
  * N and 2 hidden up to 2^23 where they are contracted (FQT_EUNSUPPORTED).     */

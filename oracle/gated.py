@@ -66,8 +66,14 @@ def gradient_operands(g, d_gate, d_up, seed=None):
     if seed is None:
         return F.operand(D.T), F.operand(D)
     w = philox.draws(np.arange(D.size, dtype=np.uint64), seed, 2).reshape(D.shape)
-    low, high = ((v * np.uint64(256)).astype(np.float64) for v in (w & np.uint64(0xFFFF), w >> np.uint64(16)))
-    return F.operand(D.T, u=low.T), F.operand(D, u=high)
+    low, high = (v.astype(np.float64) for v in (w & np.uint64(0xFFFF), w >> np.uint64(16)))
+    return stochastic_operand(D.T, low.T), stochastic_operand(D, high)
+
+
+def stochastic_operand(x, u):
+    """F.operand with 16-bit uniforms: up iff 2^4 u < floor(frac 2^20), which is frac 2^24 >= 2^8 u + 16; F.encode's rule is
+    a strict inequality, so its uniform is the number below that bound."""
+    return F.operand(x, u=np.nextafter(256.0 * u + 16.0, 0.0))
 
 
 def gated_backward(g, d_gate, d_up, x, w, seed=None):

@@ -78,6 +78,19 @@ def test_half_word_rounding_is_unbiased_and_independent():
     assert abs(c) < 5 / np.sqrt(n)
 
 
+def test_half_word_rounding_rule():
+    """Around the border, and where frac has more than 20 bits (results below the format's normal numbers)."""
+    top = 448.0
+    for frac, u, up in ((0.5, 32767, True), (0.5, 32768, False), (0.0, 0, False), (2.0 ** -20, 0, True),
+                        (2.0 ** -21, 0, False), (2.0 ** -16, 1, False), (2.0 ** -16 + 2.0 ** -20, 1, True),
+                        (1 - 2.0 ** -20, 65535, True), (1 - 2.0 ** -16, 65535, False)):
+        for base, step in ((16.0, 2.0), (0.0, 2.0 ** -9), (3 * 2.0 ** -9, 2.0 ** -9)):
+            x = np.zeros((1, 128))
+            x[0, 0], x[0, 1] = top, base + frac * step
+            got = G.stochastic_operand(x, np.full((1, 128), float(u)))["value"][0, 1]
+            assert got == base + (step if up else 0.0), (frac, u, base)
+
+
 def test_norm_gradient_from_an_exact_checkpoint():
     rng = np.random.default_rng(3)
     x, g, gamma = rng.standard_normal((5, 40)), rng.standard_normal((5, 40)), rng.standard_normal(40)

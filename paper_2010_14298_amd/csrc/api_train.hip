@@ -143,17 +143,11 @@ hipError_t gradients_of(fqt_dtype type, const BackwardWs& w, int64_t N, int64_t 
   return hipSuccess;
 }
 
-struct GatedForwardWs {
-  Fp8Buffers x;
-  uint8_t* w;
-  float *both, *part;  // a and b; their partial sums
-};
-GatedForwardWs carve_gated_forward(Carver& c, int64_t N, int64_t d_in, int64_t hidden) {
-  GatedForwardWs w;
+ForwardWs carve_gated_forward(Carver& c, int64_t N, int64_t d_in, int64_t hidden) {
+  ForwardWs w;
   w.w = c.take<uint8_t>(2 * hidden * fp8_pitch(d_in));
   w.x = take_operand(c, N, d_in);
-  w.both = c.take<float>(N * 2 * hidden);
-  w.part = c.take<float>(fp8_gemm_partials(N, 2 * hidden, d_in));
+  w.part = c.take<float>(gated_partials(N, hidden, d_in));
   return w;
 }
 
@@ -469,42 +463,38 @@ fqt_status fqt_fp8_gated_forward(const void* X, fqt_dtype type, int64_t N, int64
   if (d_in > MAX_CONTRACTION) return FQT_EUNSUPPORTED;
   if (!ws || !aligned(ws, 16) || ws_bytes < fqt_fp8_gated_forward_workspace(N, d_in, hidden)) return FQT_EWORKSPACE;
   Carver c(ws);
-  const GatedForwardWs w = carve_gated_forward(c, N, d_in, hidden);
+  const ForwardWs w = carve_gated_forward(c, N, d_in, hidden);
+  GatedGemmParams p{};
+  p.M = N;
+  p.N = 2 * hidden;
+  p.K = d_in;
+  p.C = H;
+  p.ldc = ldh;
+  p.part = w.part;
+  p.hidden = hidden;
+  p.act = act;
+  p.gate = kept_of(d_gate);
+  p.up = kept_of(d_up);
   Fp8QuantParams q{};
   q.x = X;
   q.rows = N;
   q.cols = d_in;
   q.ldx = ldx;
-  q.q_row = w.x.q;
-  q.e_row = w.x.e;
+  if (!gated_rows_raw(p)) {
+    q.q_row = w.x.q;
+    q.e_row = w.x.e;
+  }
   if (X8t) {
     q.q_col = X8t->q;
     q.e_col = X8t->exp;
   }
-  Fp8GemmParams p{};
   Fp8Turn turn{};
   p.A = w.x.q;
   p.eA = w.x.e;
   p.B = rows_of(W8, 2 * hidden, d_in, w.w, &turn);
   p.eB = W8->exp;
   FQT_TRY(launch_fp8_quantize_turn(type, q, turn, Fp8Turn{}, s));
-  p.M = N;
-  p.N = 2 * hidden;
-  p.K = d_in;
-  p.C = w.both;
-  p.ldc = 2 * hidden;
-  p.part = w.part;
-  FQT_TRY(launch_fp8_gemm(FQT_F32, p, s));
-  GatedParams g{};
-  g.part = w.both;
-  g.N = N;
-  g.hidden = hidden;
-  g.act = act;
-  g.H = H;
-  g.ldh = ldh;
-  g.gate = kept_of(d_gate);
-  g.up = kept_of(d_up);
-  FQT_TRY(launch_gated_finish(type, g, s));
+  FQT_TRY(launch_gated_gemm(type, p, X, ldx, s));
   return FQT_OK;
 }
 

@@ -2,22 +2,38 @@
 //
 //   a = Q(X) W_gate^T,  b = Q(X) W_up^T,  H = act(a) b
 //   d_gate = Q8(b act'(a)),  d_up = Q8(act(a))    (kept for the backward)
-#include "fp8_codes.h"
-#include "gated_act.h"
+//
+// The products' loops of fp8_loops.h over both halves of the weights at once;
+// a and b stay in registers.
+#include "fp8_loops.h"
 
 namespace fqt {
 
-// H and the checkpoints from a and b in memory: a thread four columns, eight
-// threads a block of a checkpoint.
+template <bool SAVE>
+struct GatedGemm : GatedGemmParams {
+  static constexpr bool KEEP = SAVE;
+};
+
+// H and the checkpoints from parts of a and b in memory, [splits][M][2 hidden]: a
+// thread four columns, eight threads a block of a checkpoint.
 template <class T>
-__global__ __launch_bounds__(256) void gated_finish_kernel(GatedParams p) {
+__global__ __launch_bounds__(256) void gated_finish_kernel(GatedGemmParams p, int splits) {
   const int64_t quads = kept_pitch(p.hidden) / 4, i = block_id() * 256 + threadIdx.x;
-  if (i >= p.N * quads) return;  // eight threads of a block leave together
+  if (i >= p.M * quads) return;  // eight threads of a block leave together
   const int64_t row = i / quads, col = (i - row * quads) * 4, n = p.hidden - col;
-  const float* const at = p.part + row * 2 * p.hidden + col;
-  float a[4], b[4], h[4], dg[4], du[4];
-  load_part<float, 4>(at, n, a);
-  load_part<float, 4>(at + p.hidden, n, b);
+  float a[4] = {0.0f, 0.0f, 0.0f, 0.0f}, b[4] = {0.0f, 0.0f, 0.0f, 0.0f}, h[4], dg[4], du[4];
+#pragma unroll 4
+  for (int s = 0; s < splits; ++s) {
+    const float* const at = p.part + (s * p.M + row) * p.N + col;
+    float va[4], vb[4];
+    load_part<float, 4>(at, n, va);
+    load_part<float, 4>(at + p.hidden, n, vb);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      a[j] += va[j];
+      b[j] += vb[j];
+    }
+  }
   with_act(p.act, [&](auto act) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -28,7 +44,7 @@ __global__ __launch_bounds__(256) void gated_finish_kernel(GatedParams p) {
       if (j >= n) dg[j] = du[j] = 0.0f;
     }
   });
-  store_part<T, 4>(static_cast<T*>(p.H) + row * p.ldh + col, n, h);
+  store_part<T, 4>(static_cast<T*>(p.C) + row * p.ldc + col, n, h);
   auto keep = [&](const Kept& k, const float (&v)[4]) {
     if (!k.q) return;
     uint32_t key = 0u;
@@ -51,12 +67,64 @@ __global__ __launch_bounds__(256) void gated_finish_kernel(GatedParams p) {
   keep(p.up, du);
 }
 
-hipError_t launch_gated_finish(fqt_dtype type, const GatedParams& p, hipStream_t s) {
+// ---------------------------------------------------------------------------
+// launches
+// ---------------------------------------------------------------------------
+constexpr int64_t GATED_ROWS_MAX = 64, GATED_RAW_MAX = 16;
+static bool few_rows(const GatedGemmParams& p) { return p.M <= GATED_ROWS_MAX && !p.gate.q && !p.up.q; }
+bool gated_rows_raw(const GatedGemmParams& p) { return few_rows(p) && p.M <= GATED_RAW_MAX; }
+int64_t gated_partials(int64_t M, int64_t hidden, int64_t K) {
+  const int64_t s = fp8_plan(M, 2 * hidden, K).splits;
+  return s > 1 ? s * M * 2 * hidden : 0;
+}
+
+template <class T, bool SAVE>
+static hipError_t gated_tiles(const GatedGemm<SAVE>& p, const Fp8Plan& plan, hipStream_t s) {
+  auto tiles = [&](auto c) {
+    using C = decltype(c);
+    return tiles_of(p.M, p.hidden, C::BM, C::BN / 2);
+  };
+  const int64_t blocks = plan.tile == Fp8Plan::LARGE ? tiles(LargeTile{}) : plan.tile == Fp8Plan::MID ? tiles(MidTile{}) : tiles(SmallTile{});
+  if (blocks > 0x7FFFFF) return hipErrorInvalidValue;
+  auto go = [&](auto kernel, int64_t grid, auto... more) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(512), 0, s, p, more...);
+    return hipGetLastError();
+  };
+  if (plan.tile == Fp8Plan::LARGE) {
+    const bool several = blocks > 256 && p.hidden % (LargeTile::BN / 2) == 0 && plan.chunk % 2 == 0 && plan.chunk >= 4 &&
+                         (!SAVE || (p.gate.q && p.up.q));
+    if (several) return go(fp8_gemm_large_kernel<T, false, true, GatedGemm<SAVE>>, 256);
+    return go(fp8_gemm_large_kernel<T, false, false, GatedGemm<SAVE>>, blocks);
+  }
+  if (plan.tile == Fp8Plan::MID)
+    return go(fp8_gemm_pipe_kernel<T, MidTile, false, false, GatedGemm<SAVE>>, blocks, plan.chunk);
+  return go(fp8_gemm_pipe_kernel<T, SmallTile, false, false, GatedGemm<SAVE>>, blocks, plan.chunk);
+}
+
+hipError_t launch_gated_gemm(fqt_dtype type, const GatedGemmParams& params, const void* x, int64_t ldx, hipStream_t s) {
   return with_type(type, [&](auto e) {
     using T = decltype(e);
-    const int64_t threads = p.N * (kept_pitch(p.hidden) / 4);
-    hipLaunchKernelGGL((gated_finish_kernel<T>), grid_of((threads + 255) / 256, 256), dim3(256), 0, s, p);
-    return hipGetLastError();
+    if (few_rows(params)) {
+      const GatedGemm<false> p{params};
+      const int64_t blocks = (p.hidden + 15) / 16;
+      auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid_of(blocks, 64 * ROW_WAVES), dim3(64 * ROW_WAVES), 0, s, p, x, ldx);
+        return hipGetLastError();
+      };
+      if (gated_rows_raw(params)) return go(fp8_rows_kernel<T, T, 1, GatedGemm<false>>);
+      if (p.M <= 16) return go(fp8_rows_kernel<T, void, 1, GatedGemm<false>>);
+      return p.M <= 32 ? go(fp8_rows_kernel<T, void, 2, GatedGemm<false>>) : go(fp8_rows_kernel<T, void, 4, GatedGemm<false>>);
+    }
+    const Fp8Plan plan = fp8_plan(params.M, params.N, params.K);
+    if (plan.splits > 1) {
+      const hipError_t err = launch_fp8_parts(params, plan, s);
+      if (err != hipSuccess) return err;
+      const int64_t threads = params.M * (kept_pitch(params.hidden) / 4);
+      hipLaunchKernelGGL((gated_finish_kernel<T>), grid_of((threads + 255) / 256, 256), dim3(256), 0, s, params, plan.splits);
+      return hipGetLastError();
+    }
+    return params.gate.q || params.up.q ? gated_tiles<T, true>(GatedGemm<true>{params}, plan, s)
+                                        : gated_tiles<T, false>(GatedGemm<false>{params}, plan, s);
   });
 }
 

@@ -33,7 +33,7 @@ __device__ __forceinline__ void activate(float a, float& value, float& slope) {
 
 // Calls f with the activation as a constant.
 template <class F>
-__device__ __forceinline__ void with_act(fqt_act act, F f) {
+__device__ __forceinline__ void with_act(fqt_act act, const F& f) {
   if (act == FQT_SILU)
     f(std::integral_constant<fqt_act, FQT_SILU>{});
   else if (act == FQT_GELU_TANH)

@@ -191,6 +191,7 @@ hipError_t launch_fp8_quantize_turn(fqt_dtype type, const Fp8QuantParams& p, con
                                     hipStream_t s);
 
 struct Fp8GemmParams {
+  static constexpr bool GATED = false, KEEP = false;  // gated; checkpoints too
   const uint8_t* A;   // [M, pitch(K)]
   const uint8_t* eA;
   const uint8_t* B;   // [N, pitch(K)]
@@ -207,21 +208,31 @@ struct Fp8GemmParams {
 bool fp8_rows_raw(int64_t M);
 hipError_t launch_fp8_rows(fqt_dtype type, const Fp8GemmParams& p, const void* x, int64_t ldx, hipStream_t s);
 int64_t fp8_gemm_partials(int64_t M, int64_t N, int64_t K);  // floats
+// Which tile, and for small tiles into how many parts along K a product is split.
+struct Fp8Plan {
+  enum Tile { SMALL, MID, LARGE } tile;
+  int splits, chunk;  // parts along K, stages of each
+};
+Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K);
+hipError_t launch_fp8_parts(const Fp8GemmParams& p, const Fp8Plan& plan, hipStream_t s);  // to p.part
 fqt_fp8_form fp8_gemm_form(int64_t M, int64_t N, int64_t K, bool masked, bool lines);
 hipError_t launch_fp8_gemm(fqt_dtype type, const Fp8GemmParams& p, hipStream_t s);
 
 // ---------------------------------------------------------------------------
 // gated layer
 // ---------------------------------------------------------------------------
-struct GatedParams {
-  const float* part;  // [N, 2 hidden]: a, then b
-  int64_t N, hidden;
+// A product whose outputs are H [M, hidden]: B is [W_gate; W_up] (N = 2 hidden
+// rows), C is H.  Checkpoints may be null.
+struct GatedGemmParams : Fp8GemmParams {
+  static constexpr bool GATED = true;
+  int64_t hidden;
   fqt_act act;
-  void* H;
-  int64_t ldh;
   Kept gate, up;
 };
-hipError_t launch_gated_finish(fqt_dtype type, const GatedParams& p, hipStream_t s);
+// Whether X [M, K] is read as it is (p.A is not).
+bool gated_rows_raw(const GatedGemmParams& p);
+int64_t gated_partials(int64_t M, int64_t hidden, int64_t K);  // floats
+hipError_t launch_gated_gemm(fqt_dtype type, const GatedGemmParams& p, const void* x, int64_t ldx, hipStream_t s);
 
 // The quantizer of D = [G gate | G up] [rows, cols = 2 hidden]: q.x, q.ldx are
 // G's.

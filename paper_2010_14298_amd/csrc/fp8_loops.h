@@ -212,13 +212,13 @@ template <class T, bool NT, bool RUN, class P = Fp8GemmParams>
 __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(P p) {
   using C = LargeTile;
   constexpr int COLS = P::GATED ? C::BN / 2 : C::BN;  // output columns of a tile
+  static_assert(!(P::GATED && RUN), "the waits count plain stores");
   // separate arrays, so that a pending load into one does not hold up reads of another
   __shared__ __attribute__((aligned(16))) uint8_t h00[C::HALF], h01[C::HALF], h10[C::HALF], h11[C::HALF];
   __shared__ int e0[C::BM + C::BN], e1[C::BM + C::BN];
   // RUN: strips of outputs, 2 KB and padding a wave
   constexpr int V = 16 / (int)sizeof(T), STRIP = 2 * V, STRIP_LD = C::WN + V;
-  constexpr bool STRIPS = RUN && !P::GATED;
-  __shared__ __attribute__((aligned(16))) T out[STRIPS ? C::WAVES : 1][STRIPS ? STRIP * STRIP_LD : 1];
+  __shared__ __attribute__((aligned(16))) T out[RUN ? C::WAVES : 1][RUN ? STRIP * STRIP_LD : 1];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / C::WAVES_N, wn = wave % C::WAVES_N;
@@ -383,7 +383,7 @@ __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(P p)
   };
   auto store_all = [&](int64_t row0, int64_t col0) __attribute__((always_inline)) {
     if constexpr (P::GATED) {
-      gated_store<T, C::IT, RUN>(p, acc, row0 + wm * C::WM, p.M, col0 + wn * 32);
+      gated_store(p, acc, row0 + wm * C::WM, p.M, col0 + wn * 32, T{});
     } else if constexpr (RUN) {
       // STRIP rows at a time through LDS of their own, whole lines out of it;
       // rows past the edge hold what the last row does and store it there again.
@@ -455,7 +455,7 @@ __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(P p)
     stages_from(0);
     store_all(m0, n0);
   } else {
-    constexpr std::integral_constant<int, stores_of<T, P>(C::IT, C::WM / STRIP * 2)> STORES{};
+    constexpr std::integral_constant<int, C::WM / STRIP * 2> STORES{};
     // the first two stages, behind `more` stores
     auto begin = [&](auto more) __attribute__((always_inline)) {
       wait_loads<N1 + N0 + N1 + more>();  // (0, 0) is there
@@ -538,7 +538,6 @@ __global__ __launch_bounds__(512) void fp8_gemm_pipe_kernel(P p, int chunk) {
   const int lastA = p.M - 1 - m0 < C::BM - 1 ? (int)(p.M - 1 - m0) : C::BM - 1;
   const int lastB = columns(p) - 1 - n0 < COLS - 1 ? (int)(columns(p) - 1 - n0) : COLS - 1;
   const Rows rowsA(p.A + m0 * pitch + (int64_t)first * FP8_BLOCK), rowsB(p.B + n0 * pitch + (int64_t)first * FP8_BLOCK);
-  const Rows rowsU(P::GATED ? p.B + (n0 + columns(p)) * pitch : p.B);  // gated: rows of the second half
   // this wave's 1 KB loads, eight rows each: of A, then of B
   int src[C::INS];
 #pragma unroll
@@ -557,9 +556,17 @@ __global__ __launch_bounds__(512) void fp8_gemm_pipe_kernel(P p, int chunk) {
   const int64_t estep = (eA ? p.M : p.N) * 4;
   int esrc = 4 * (er < elast ? er : elast);
   if (P::GATED && !eA) esrc += (int)(4 * (uint32_t)columns(p) * (lane >> 5));
-  auto rows_of_load = [&](int i) __attribute__((always_inline)) -> const Rows& {
+  // (a choice among descriptors costs a loop a load where the compiler does not see that it is uniform)
+  const uint8_t* const baseA = p.A + m0 * pitch + (int64_t)first * FP8_BLOCK;
+  const uint8_t* const baseB = p.B + n0 * pitch + (int64_t)first * FP8_BLOCK;
+  auto rows_of_load = [&](int i) __attribute__((always_inline)) {
     const int at = 8 * (wave * C::INS + i);
-    return at < C::BM ? rowsA : P::GATED && ((at - C::BM) & 32) ? rowsU : rowsB;
+    if constexpr (P::GATED) {
+      const uint8_t* const b = at < C::BM ? baseA : baseB + (((at - C::BM) & 32) ? columns(p) * pitch : 0);
+      return Rows(b);
+    } else {
+      return at < C::BM ? rowsA : rowsB;
+    }
   };
   auto load = [&](uint8_t* d, int* e, int t) __attribute__((always_inline)) {
 #pragma unroll
@@ -729,7 +736,7 @@ __global__ __launch_bounds__(512) void fp8_gemm_pipe_kernel(P p, int chunk) {
     for (int i = 0; i < STRIPS; ++i)
 #pragma unroll
       for (int j = 0; j < C::JT; ++j) mine[i][j] = acc[i][j];
-    gated_store<T, STRIPS, false>(p, mine, m0 + wm * C::WM + kg * STRIPS * 32, p.M, n0 + wn * 32);
+    gated_store(p, mine, m0 + wm * C::WM + kg * STRIPS * 32, p.M, n0 + wn * 32, T{});
     return;
   } else {
     constexpr int STRIP = 32 * C::OUT_LD * 4, FIT = C::CODES / STRIP;
@@ -757,6 +764,151 @@ __global__ __launch_bounds__(512) void fp8_gemm_pipe_kernel(P p, int chunk) {
       __builtin_amdgcn_wave_barrier();
     }
   }
+}
+
+// ---------------------------------------------------------------------------
+// Two blocks a unit: four waves of 128 x 64 each, so that one block's stores (and,
+// gated, its activations) and first loads run while the other feeds the matrix
+// cores.  Half stages of 64 along K in three buffers: the wait and the barrier of
+// half stage t say that it has landed and that everyone has read t - 1, whose
+// buffer then takes t + 2.  Scale words, four stages in each, in two buffers.
+// ---------------------------------------------------------------------------
+struct PairTile {
+  static constexpr int BM = 128, BN = 256, WM = 128, WN = 64;
+  static constexpr int WAVES_N = BN / WN, WAVES = (BM / WM) * WAVES_N, THREADS = WAVES * 64;
+  static constexpr int IT = WM / 32, JT = WN / 32;
+  static constexpr int HALF = (BM + BN) * 64;
+  static constexpr int A_INS = BM / 16 / WAVES, B_INS = BN / 16 / WAVES, INS = A_INS + B_INS;
+  static constexpr int E_SEGS = (BM + BN) / 64, E_INS = (E_SEGS + WAVES - 1) / WAVES;
+};
+
+template <class T, class P>
+__global__ __launch_bounds__(PairTile::THREADS, 2) void fp8_gemm_pair_kernel(P p) {
+  using C = PairTile;
+  static_assert(P::GATED, "outputs from registers");
+  constexpr int COLS = C::BN / 2;
+  __shared__ __attribute__((aligned(16))) uint8_t q0[C::HALF], q1[C::HALF], q2[C::HALF];
+  __shared__ int e0[C::BM + C::BN], e1[C::BM + C::BN];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / C::WAVES_N, wn = wave % C::WAVES_N;
+  int64_t tm, tn;
+  block_tile(blockIdx.x, (p.M + C::BM - 1) / C::BM, (columns(p) + COLS - 1) / COLS, tm, tn);
+  const int64_t m0 = tm * C::BM, n0 = tn * COLS;
+  const int64_t pitch = fp8_pitch(p.K);
+  const int n = 2 * (int)fp8_blocks(p.K);  // half stages
+  const int lastA = p.M - 1 - m0 < C::BM - 1 ? (int)(p.M - 1 - m0) : C::BM - 1;
+  const int lastB = columns(p) - 1 - n0 < COLS - 1 ? (int)(columns(p) - 1 - n0) : COLS - 1;
+  static_assert(C::B_INS == 4, "a wave loads 32 rows of B of each half");
+  const Rows rowsA(p.A + m0 * pitch), rowsB(p.B + n0 * pitch), rowsU(p.B + (n0 + columns(p)) * pitch);
+  int src[C::INS];
+#pragma unroll
+  for (int i = 0; i < C::INS; ++i) {
+    const bool a = i < C::A_INS;
+    const int r = 16 * (a ? wave * C::A_INS + i : wave * C::B_INS + i - C::A_INS) + (lane >> 2);
+    const int last = a ? lastA : lastB, at = a ? r : hidden_of(r);
+    src[i] = (at < last ? at : last) * (int)pitch + 16 * ((lane & 3) ^ ((r >> 2) & 3));
+  }
+  const uint8_t* ebase[C::E_INS];
+  int64_t estep[C::E_INS];
+  int esrc[C::E_INS], eseg[C::E_INS];
+#pragma unroll
+  for (int i = 0; i < C::E_INS; ++i) {
+    eseg[i] = (wave + i * C::WAVES) % C::E_SEGS;  // fewer runs than waves: some load one twice
+    const bool a = eseg[i] * 64 < C::BM;
+    const int r = eseg[i] * 64 - (a ? 0 : C::BM) + lane, last = a ? lastA : lastB, at = a ? r : hidden_of(r);
+    ebase[i] = a ? p.eA + m0 * 4 : p.eB + n0 * 4;
+    esrc[i] = 4 * (at < last ? at : last);
+    if (!a) esrc[i] += (int)(4 * (uint32_t)columns(p) * (lane >> 5));
+    estep[i] = (a ? p.M : p.N) * 4;
+  }
+  // the scale words go first: a wait for all but INS loads includes them
+  auto load = [&](uint8_t* d, int t) __attribute__((always_inline)) {
+    if ((t & 7) == 0) {
+      int* const e = (t & 8) ? e1 : e0;
+#pragma unroll
+      for (int i = 0; i < C::E_INS; ++i) Rows(ebase[i] + (t >> 3) * estep[i]).to_lds4(e + eseg[i] * 64, esrc[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < C::INS; ++i) {
+      const bool a = i < C::A_INS;
+      uint8_t* const to = d + (a ? (wave * C::A_INS + i) * 1024 : C::BM * 64 + (wave * C::B_INS + i - C::A_INS) * 1024);
+      (a ? rowsA : i < C::A_INS + 2 ? rowsB : rowsU).to_lds16(to, src[i], t * 64);
+    }
+  };
+  v16f acc[C::IT][C::JT];
+#pragma unroll
+  for (int i = 0; i < C::IT; ++i)
+#pragma unroll
+    for (int j = 0; j < C::JT; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+  const int lrow = lane & 31, half = lane >> 5;
+  const int sw = (lrow >> 2) & 3;
+  const int offA = (wm * C::WM + lrow) * 64, offB = C::BM * 64 + (wn * C::WN + lrow) * 64;
+  const int c0 = 16 * ((2 * half) ^ sw), c1 = 16 * ((2 * half + 1) ^ sw);
+  auto step = [&](auto inner, int t, const uint8_t* q, uint8_t* next) __attribute__((always_inline)) {
+    if (inner || t + 1 < n)
+      wait_loads<C::INS>();
+    else
+      wait_loads<0>();
+    meet();
+    if (inner || t + 2 < n) load(next, t + 2);
+    auto frag = [&](const uint8_t* f) __attribute__((always_inline)) {
+      const v4i x = *reinterpret_cast<const v4i*>(f + c0);
+      const v4i y = *reinterpret_cast<const v4i*>(f + c1);
+      return v8i{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+    };
+    v8i a[C::IT], b[C::JT];
+    float fa[C::IT], fb[C::JT];
+    const int* const e = (t & 8) ? e1 : e0;
+    const int sh = 8 * ((t >> 1) & 3);
+#pragma unroll
+    for (int j = 0; j < C::JT; ++j) b[j] = frag(q + offB + j * 32 * 64);
+#pragma unroll
+    for (int i = 0; i < C::IT; ++i) a[i] = frag(q + offA + i * 32 * 64);
+#pragma unroll
+    for (int j = 0; j < C::JT; ++j) fb[j] = scale_of(e[C::BM + wn * C::WN + j * 32 + lrow] >> sh);
+#pragma unroll
+    for (int i = 0; i < C::IT; ++i) fa[i] = scale_of(e[wm * C::WM + i * 32 + lrow] >> sh);
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v8b wa[C::IT], wb[C::JT];
+#pragma unroll
+      for (int j = 0; j < C::JT; ++j) wb[j] = widen(b[j][2 * k], b[j][2 * k + 1], fb[j]);
+#pragma unroll
+      for (int i = 0; i < C::IT; ++i) wa[i] = widen(a[i][2 * k], a[i][2 * k + 1], fa[i]);
+#pragma unroll
+      for (int i = 0; i < C::IT; ++i)
+#pragma unroll
+        for (int j = 0; j < C::JT; ++j) acc[i][j] = product<P::GATED>(wa[i], wb[j], acc[i][j]);
+    }
+    interleave<4, C::IT * C::JT, 4 * (C::IT + C::JT)>();
+    __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+    for (int i = 0; i < C::IT; ++i)
+#pragma unroll
+      for (int j = 0; j < C::JT; ++j) asm volatile("" : "+v"(acc[i][j]));
+  };
+  load(q0, 0);
+  load(q1, 1);  // n is even
+  constexpr std::true_type inner{};
+  constexpr std::false_type last{};
+  int t = 0;
+  for (; t + 4 < n; t += 3) {
+    step(inner, t, q0, q2);
+    step(inner, t + 1, q1, q0);
+    step(inner, t + 2, q2, q1);
+  }
+  for (; t < n; t += 3) {
+    step(last, t, q0, q2);
+    if (t + 1 < n) step(last, t + 1, q1, q0);
+    if (t + 2 < n) step(last, t + 2, q2, q1);
+  }
+  gated_store(p, acc, m0 + wm * C::WM, p.M, n0 + wn * 32, T{});
 }
 
 using MidTile = PipeTile<256, 128, 64, 64, 1, 3>;

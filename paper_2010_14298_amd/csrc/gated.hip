@@ -85,15 +85,19 @@ static hipError_t gated_tiles(const GatedGemm<SAVE>& p, const Fp8Plan& plan, hip
     return tiles_of(p.M, p.hidden, C::BM, C::BN / 2);
   };
   const int64_t blocks = plan.tile == Fp8Plan::LARGE ? tiles(LargeTile{}) : plan.tile == Fp8Plan::MID ? tiles(MidTile{}) : tiles(SmallTile{});
-  if (blocks > 0x7FFFFF) return hipErrorInvalidValue;
+  if (blocks > 0x3FFFFF) return hipErrorInvalidValue;  // and twice as many of two a unit
   auto go = [&](auto kernel, int64_t grid, auto... more) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(512), 0, s, p, more...);
     return hipGetLastError();
   };
   if (plan.tile == Fp8Plan::LARGE) {
-    const bool several = blocks > 256 && p.hidden % (LargeTile::BN / 2) == 0 && plan.chunk % 2 == 0 && plan.chunk >= 4 &&
-                         (!SAVE || (p.gate.q && p.up.q));
-    if (several) return go(fp8_gemm_large_kernel<T, false, true, GatedGemm<SAVE>>, 256);
+    // us, 8192 tokens, 4096 hidden units, bfloat16, two blocks a unit / 256 x 256, with checkpoints (without): 512 wide
+    // 90 / 98 (70 / 74), 1024 139 / 142 (119 / 119), 2048 238 / 230 (217 / 202), 8192 863 / 798 (826 / 758)
+    if (plan.chunk <= 8) {
+      hipLaunchKernelGGL((fp8_gemm_pair_kernel<T, GatedGemm<SAVE>>), dim3((unsigned)tiles(PairTile{})),
+                         dim3(PairTile::THREADS), 0, s, p);
+      return hipGetLastError();
+    }
     return go(fp8_gemm_large_kernel<T, false, false, GatedGemm<SAVE>>, blocks);
   }
   if (plan.tile == Fp8Plan::MID)

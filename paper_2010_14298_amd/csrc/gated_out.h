@@ -23,12 +23,6 @@ __device__ __forceinline__ void swap_halves(uint32_t& a, uint32_t& b) {
   b = s[1];  // lower lanes: the upper ones' a; upper lanes: their b
 }
 
-// Vector stores of one wave for 32 tokens.
-template <class T, class P>
-constexpr int stores_of(int strips, int plain) {
-  return P::GATED ? strips * ((int)sizeof(T) + (P::KEEP ? 4 : 0)) : plain;
-}
-
 // The checkpoint's codes and scale byte of a token's block.
 __device__ __forceinline__ void keep_block(const Kept& k, const float (&v)[16], int64_t row, int64_t pitch, int64_t col0,
                                            bool store) {
@@ -57,21 +51,19 @@ __device__ __forceinline__ void keep_block(const Kept& k, const float (&v)[16], 
 }
 
 // Tokens row0 .. row0 + 32 STRIPS - 1 (the lane's at lane % 32), hidden units
-// col0 .. col0 + 31.  RUN: whole blocks, and tokens past the last are stored
-// like it, so that every wave issues the same number of stores.
-template <class T, int STRIPS, bool RUN, class P>
+// col0 .. col0 + 31; T: the type of H.
+template <class T, int STRIPS, class P>
 __device__ __forceinline__ void gated_store(const P& p, const v16f (&acc)[STRIPS][2], int64_t row0, int64_t rows,
-                                            int64_t col0) {
-  if (!RUN && col0 >= p.hidden) return;
+                                            int64_t col0, T) {
+  if (col0 >= p.hidden) return;
   const int lane = threadIdx.x & 63, half = lane >> 5;
-  const bool whole = RUN || col0 + 32 <= p.hidden;
+  const bool whole = col0 + 32 <= p.hidden;
   const int64_t pitch = kept_pitch(p.hidden);
   with_act(p.act, [&](auto act) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < STRIPS; ++i) {
-      int64_t row = row0 + i * 32 + (lane & 31);
-      const bool store = RUN || row < rows;
-      if (row >= rows) row = rows - 1;
+      const int64_t row = row0 + i * 32 + (lane & 31);
+      const bool store = row < rows;
       float h[16], dg[16], du[16];
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -115,8 +107,8 @@ __device__ __forceinline__ void gated_store(const P& p, const v16f (&acc)[STRIPS
         }
       }
       if constexpr (P::KEEP) {
-        if (RUN || p.gate.q) keep_block(p.gate, dg, row, pitch, col0, store);
-        if (RUN || p.up.q) keep_block(p.up, du, row, pitch, col0, store);
+        if (p.gate.q) keep_block(p.gate, dg, row, pitch, col0, store);
+        if (p.up.q) keep_block(p.up, du, row, pitch, col0, store);
       }
     }
   });

@@ -93,17 +93,18 @@ ForwardWs carve_forward(Carver& c, int64_t N, int64_t d_in, int64_t d_out) {
 struct BackwardWs {
   Fp8Buffers g, gt;
   uint8_t *x, *w;
-  float* part;
+  float *part_w, *part_x;  // the products' partial sums, the same room where they run one behind the other
 };
-// The two products run one behind the other and share their partial sums.
 BackwardWs carve_backward(Carver& c, int64_t N, int64_t d_in, int64_t d_out) {
   BackwardWs w;
   w.g = take_operand(c, N, d_out);
   w.gt = take_operand(c, d_out, N);
   w.x = c.take<uint8_t>(d_in * fp8_pitch(N));
   w.w = c.take<uint8_t>(d_in * fp8_pitch(d_out));
-  const int64_t a = fp8_gemm_partials(N, d_in, d_out), b = fp8_gemm_partials(d_out, d_in, N);
-  w.part = c.take<float>(a > b ? a : b);
+  const int64_t a = fp8_gemm_partials(d_out, d_in, N), b = fp8_gemm_partials(N, d_in, d_out);
+  const bool both = fp8_two_at_once(d_out, d_in, N, N, d_in, d_out);
+  w.part_w = c.take<float>(both || a > b ? a : b);
+  w.part_x = both ? c.take<float>(b) : w.part_w;
   return w;
 }
 
@@ -112,9 +113,8 @@ BackwardWs carve_backward(Carver& c, int64_t N, int64_t d_in, int64_t d_out) {
 hipError_t gradients_of(fqt_dtype type, const BackwardWs& w, int64_t N, int64_t d_in, int64_t d_out, const uint8_t* x8,
                         const fqt_fp8* X8t, const uint8_t* w8, const fqt_fp8* W8t, const void* relu_input, int64_t ldr,
                         float* grad_W, void* grad_X, int64_t ldgx, hipStream_t s) {
-  Fp8GemmParams p{};
-  p.part = w.part;
-  p.N = d_in;
+  Fp8GemmParams p{}, r{};
+  p.N = r.N = d_in;
   if (grad_W) {
     p.A = w.gt.q;
     p.eA = w.gt.e;
@@ -124,23 +124,23 @@ hipError_t gradients_of(fqt_dtype type, const BackwardWs& w, int64_t N, int64_t 
     p.K = N;
     p.C = grad_W;
     p.ldc = d_in;
-    const hipError_t e = launch_fp8_gemm(FQT_F32, p, s);
-    if (e != hipSuccess) return e;
+    p.part = w.part_w;
   }
   if (grad_X) {
-    p.A = w.g.q;
-    p.eA = w.g.e;
-    p.B = w8;
-    p.eB = W8t->exp;
-    p.M = N;
-    p.K = d_out;
-    p.C = grad_X;
-    p.ldc = ldgx;
-    p.mask = relu_input;
-    p.ldmask = ldr;
-    return launch_fp8_gemm(type, p, s);
+    r.A = w.g.q;
+    r.eA = w.g.e;
+    r.B = w8;
+    r.eB = W8t->exp;
+    r.M = N;
+    r.K = d_out;
+    r.C = grad_X;
+    r.ldc = ldgx;
+    r.mask = relu_input;
+    r.ldmask = ldr;
+    r.part = w.part_x;
   }
-  return hipSuccess;
+  if (grad_W && grad_X) return launch_fp8_two(type, p, r, s);
+  return grad_W ? launch_fp8_gemm(FQT_F32, p, s) : launch_fp8_gemm(type, r, s);
 }
 
 ForwardWs carve_gated_forward(Carver& c, int64_t N, int64_t d_in, int64_t hidden) {
@@ -539,12 +539,10 @@ fqt_status fqt_fp8_gated_backward(const void* G, fqt_dtype type, int64_t N, int6
   d.e_gate = d_gate->exp;
   d.q_up = d_up->q;
   d.e_up = d_up->exp;
-  FQT_TRY(launch_gated_quantize(type, d, s));
   Fp8Turn turn_x{}, turn_w{};
   const uint8_t* const x8 = grad_W ? rows_of(X8t, d_in, N, w.x, &turn_x) : nullptr;
   const uint8_t* const w8 = grad_X ? rows_of(W8t, d_in, cols, w.w, &turn_w) : nullptr;
-  FQT_TRY(launch_fp8_turn(turn_x, s));
-  FQT_TRY(launch_fp8_turn(turn_w, s));
+  FQT_TRY(launch_gated_quantize(type, d, turn_x, turn_w, s));
   FQT_TRY(gradients_of(type, w, N, d_in, cols, x8, X8t, w8, W8t, nullptr, 0, grad_W, grad_X, ldgx, s));
   return FQT_OK;
 }

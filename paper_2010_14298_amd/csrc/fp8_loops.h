@@ -503,7 +503,7 @@ __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(P p)
 // second, and their sums meet in LDS at the end, so that a wave's tile is
 // twice as large and reads (and widens) less for each product.  NS whole
 // stages of 128-byte rows in LDS, the 16-byte chunk index XOR-ed with (r / 2)
-// mod 8.  SPLIT: blockIdx.y takes `chunk` stages and leaves float32 sums in
+// mod 8.  SPLIT: part by part, `chunk` stages each, which leave float32 sums in
 // p.part.  256 x 256 tiles do not fit this loop: their accumulators and a second
 // set of operands spill.
 // ---------------------------------------------------------------------------
@@ -521,8 +521,8 @@ struct PipeTile {
 };
 
 // T: the stored type (SPLIT: float).
-template <class T, class C, bool SPLIT, bool NT, class P = Fp8GemmParams>
-__global__ __launch_bounds__(512) void fp8_gemm_pipe_kernel(P p, int chunk) {
+template <class T, class C, bool SPLIT, bool NT, class P>
+__device__ __forceinline__ void pipe_tile(const P& p, int chunk, uint32_t tile, uint32_t part) {
   constexpr int COLS = P::GATED ? C::BN / 2 : C::BN;  // output columns of a tile
   __shared__ __attribute__((aligned(16))) uint8_t q0[C::CODES], q1[C::CODES], q2[C::CODES], q3[C::NS > 3 ? C::CODES : 16];
   __shared__ int x0[C::BM + C::BN], x1[C::BM + C::BN], x2[C::BM + C::BN], x3[C::NS > 3 ? C::BM + C::BN : 4];
@@ -530,10 +530,10 @@ __global__ __launch_bounds__(512) void fp8_gemm_pipe_kernel(P p, int chunk) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kg = wave / C::PLANE, wm = wave % C::PLANE / C::WAVES_N, wn = wave % C::WAVES_N;
   int64_t tm, tn;
-  block_tile(blockIdx.x, (p.M + C::BM - 1) / C::BM, (columns(p) + COLS - 1) / COLS, tm, tn);
+  block_tile(tile, (p.M + C::BM - 1) / C::BM, (columns(p) + COLS - 1) / COLS, tm, tn);
   const int64_t m0 = tm * C::BM, n0 = tn * COLS;
   const int64_t pitch = fp8_pitch(p.K);
-  const int all = (int)fp8_blocks(p.K), first = SPLIT ? (int)blockIdx.y * chunk : 0;
+  const int all = (int)fp8_blocks(p.K), first = SPLIT ? (int)part * chunk : 0;
   const int nk = SPLIT && first + chunk < all ? chunk : all - first;
   const int lastA = p.M - 1 - m0 < C::BM - 1 ? (int)(p.M - 1 - m0) : C::BM - 1;
   const int lastB = columns(p) - 1 - n0 < COLS - 1 ? (int)(columns(p) - 1 - n0) : COLS - 1;
@@ -745,7 +745,7 @@ __global__ __launch_bounds__(512) void fp8_gemm_pipe_kernel(P p, int chunk) {
     float* const strip = reinterpret_cast<float*>(own);
     Fp8GemmParams to = p;
     if constexpr (SPLIT) {
-      to.C = p.part + (int64_t)blockIdx.y * p.M * p.N;
+      to.C = p.part + (int64_t)part * p.M * p.N;
       to.ldc = p.N;
       to.relu = 0;
       to.mask = nullptr;
@@ -764,6 +764,10 @@ __global__ __launch_bounds__(512) void fp8_gemm_pipe_kernel(P p, int chunk) {
       __builtin_amdgcn_wave_barrier();
     }
   }
+}
+template <class T, class C, bool SPLIT, bool NT, class P = Fp8GemmParams>
+__global__ __launch_bounds__(512) void fp8_gemm_pipe_kernel(P p, int chunk) {
+  pipe_tile<T, C, SPLIT, NT, P>(p, chunk, blockIdx.x, blockIdx.y);
 }
 
 // ---------------------------------------------------------------------------

@@ -99,6 +99,10 @@ __device__ __forceinline__ uint32_t half_code(uint32_t w, float v, uint32_t n, f
   return (uint32_t)__builtin_amdgcn_cvt_scalef32_sr_fp8_f32((int)w, v, (int)(n | 0xffffu), scale, BYTE);
 }
 
+__device__ __forceinline__ float larger(float a, float b) {
+  return __builtin_elementwise_maximum(__builtin_fabsf(a), __builtin_fabsf(b));
+}
+
 // Where a tile's elements come from: quads of rows row .. row + GROUP - 1 at
 // column col, and their random words.
 template <class T>
@@ -129,12 +133,28 @@ __device__ __forceinline__ void quantize_tile(const Fp8QuantParams& p, uint32_t 
   // keys of the rows (two to a word) and columns
   typename Quad<T>::ColTop ct{};
   uint32_t rk[GROUP / 2], ck[2];
+  if constexpr (Source::HALVES) {  // the larger magnitudes of float32, NaN above all, three at a time
+    float top[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-  for (int i = 0; i < GROUP; i += 2) {
-    typename Quad<T>::RowTop a, b;
-    v[i].top(a, ct);
-    v[i + 1].top(b, ct);
-    if (ROW && !SQUARE) rk[i / 2] = Quad<T>::row_key(a) | Quad<T>::row_key(b) << 16;
+    for (int i = 0; i < GROUP; i += 2) {
+      float r[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        r[k] = larger(larger(v[i + k].v[0], v[i + k].v[1]), larger(v[i + k].v[2], v[i + k].v[3]));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) top[j] = larger(larger(v[i].v[j], v[i + 1].v[j]), top[j]);
+      if (ROW) rk[i / 2] = Quad<T>::row_key(__float_as_uint(r[0])) | Quad<T>::row_key(__float_as_uint(r[1])) << 16;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) ct.m[j] = __float_as_uint(top[j]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < GROUP; i += 2) {
+      typename Quad<T>::RowTop a, b;
+      v[i].top(a, ct);
+      v[i + 1].top(b, ct);
+      if (ROW && !SQUARE) rk[i / 2] = Quad<T>::row_key(a) | Quad<T>::row_key(b) << 16;
+    }
   }
   Quad<T>::col_keys(ct, ck);
   if constexpr (COL || SQUARE) {
@@ -195,34 +215,52 @@ __device__ __forceinline__ void quantize_tile(const Fp8QuantParams& p, uint32_t 
     if (row + i < p.rows) *reinterpret_cast<uint32_t*>(q_row + i * row_pitch) = key >= NAN_KEY ? 0x7f7f7f7fu : codes;
   };
   if constexpr (SR && Source::HALVES) {
-    uint64_t e = (uint64_t)row * (uint64_t)p.cols + (uint64_t)col;
     const float up[4] = {scale_up(byte[0]), scale_up(byte[1]), scale_up(byte[2]), scale_up(byte[3])};
+    auto put = [&](int j, int k, uint32_t codes) __attribute__((always_inline)) {
+      *reinterpret_cast<uint32_t*>(turned + (4 * quad + j) * TILE + 16 * (grp ^ (quad & 7)) + 4 * k) =
+          key[j] >= NAN_KEY ? 0x7f7f7f7fu : codes;
+    };
+    // aligned: a quad's elements share one random block; all: no row is past the last
+    auto codes = [&](auto aligned, auto all) __attribute__((always_inline)) {
+      uint64_t e = (uint64_t)row * (uint64_t)p.cols + (uint64_t)col;
+      uint8_t* to = q_row;
 #pragma unroll
-    for (int i = 0; i < GROUP; ++i) {
-      const u32x4 u = quad_words(e, p.seed, 2u, whole);
-      e += (uint64_t)p.cols;
-      const uint32_t n[4] = {~u.x, ~u.y, ~u.z, ~u.w};
-      if constexpr (ROW) {
-        const int sh = 16 * (i & 1);
-        const float s = scale_up(scale_bytes(rk[i / 2]) >> sh & 0xffffu);
-        uint32_t c = half_code<0>(0u, v[i].at(0), n[0], s);
-        c = half_code<1>(c, v[i].at(1), n[1], s);
-        c = half_code<2>(c, v[i].at(2), n[2], s);
-        store_row(i, rk[i / 2] >> sh & 0xffffu, half_code<3>(c, v[i].at(3), n[3], s));
-      }
-      if constexpr (COL) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          uint32_t& c = w[j][i / 4];
-          const uint32_t low = n[j] << 16;
-          if ((i & 3) == 0) c = half_code<0>(0u, v[i].at(j), low, up[j]);
-          if ((i & 3) == 1) c = half_code<1>(c, v[i].at(j), low, up[j]);
-          if ((i & 3) == 2) c = half_code<2>(c, v[i].at(j), low, up[j]);
-          if ((i & 3) == 3) c = half_code<3>(c, v[i].at(j), low, up[j]);
+      for (int i = 0; i < GROUP; ++i) {
+        const u32x4 u = quad_words(e, p.seed, 2u, aligned || whole);
+        e += (uint64_t)p.cols;
+        const uint32_t n[4] = {~u.x, ~u.y, ~u.z, ~u.w};
+        if constexpr (ROW) {
+          const int sh = 16 * (i & 1);
+          const uint32_t key = rk[i / 2] >> sh & 0xffffu;
+          const uint32_t exponent = (scale_bytes(rk[i / 2]) >> sh & 0xffffu) << 23;
+          const float s = __uint_as_float(exponent > 0x400000u ? exponent : 0x400000u);  // scale_up
+          uint32_t c = half_code<0>(0u, v[i].at(0), n[0], s);
+          c = half_code<1>(c, v[i].at(1), n[1], s);
+          c = half_code<2>(c, v[i].at(2), n[2], s);
+          c = half_code<3>(c, v[i].at(3), n[3], s);
+          if (all || row + i < p.rows) *reinterpret_cast<uint32_t*>(to) = key >= NAN_KEY ? 0x7f7f7f7fu : c;
+          to += row_pitch;
         }
+        if constexpr (COL) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint32_t& c = w[j][0];
+            const uint32_t low = n[j] << 16;
+            if ((i & 3) == 0) c = half_code<0>(0u, v[i].at(j), low, up[j]);
+            if ((i & 3) == 1) c = half_code<1>(c, v[i].at(j), low, up[j]);
+            if ((i & 3) == 2) c = half_code<2>(c, v[i].at(j), low, up[j]);
+            if ((i & 3) == 3) c = half_code<3>(c, v[i].at(j), low, up[j]);
+            asm volatile("" : "+v"(c));  // now: the compiler would keep the random words of all rows to the end
+            if ((i & 3) == 3) put(j, i / 4, c);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);  // one row at a time: fewer registers, more waves
       }
-      __builtin_amdgcn_sched_barrier(0);  // one row at a time: fewer registers, more waves
-    }
+    };
+    if (whole && r0 + TILE <= p.rows)
+      codes(std::true_type{}, std::true_type{});
+    else
+      codes(std::false_type{}, std::false_type{});
   } else if constexpr (SR) {
     // both operands' codes of a row together: what their random words share is
     // not kept over all rows
@@ -272,13 +310,15 @@ __device__ __forceinline__ void quantize_tile(const Fp8QuantParams& p, uint32_t 
   }
   if constexpr (COL) {
     const int64_t pitch = fp8_pitch(p.rows);
+    if constexpr (!(SR && Source::HALVES)) {  // (there they lie in LDS already)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (key[j] >= NAN_KEY) w[j][0] = w[j][1] = w[j][2] = w[j][3] = 0x7f7f7f7fu;
-      // column 4 quad + j, rows 16 grp ..: chunk index swizzled by the quad so
-      // that eight lanes' 16-byte words fall on distinct banks
-      *reinterpret_cast<uint4*>(turned + (4 * quad + j) * TILE + 16 * (grp ^ (quad & 7))) =
-          make_uint4(w[j][0], w[j][1], w[j][2], w[j][3]);
+      for (int j = 0; j < 4; ++j) {
+        if (key[j] >= NAN_KEY) w[j][0] = w[j][1] = w[j][2] = w[j][3] = 0x7f7f7f7fu;
+        // column 4 quad + j, rows 16 grp ..: chunk index swizzled by the quad so
+        // that eight lanes' 16-byte words fall on distinct banks
+        *reinterpret_cast<uint4*>(turned + (4 * quad + j) * TILE + 16 * (grp ^ (quad & 7))) =
+            make_uint4(w[j][0], w[j][1], w[j][2], w[j][3]);
+      }
     }
     __syncthreads();
     // eight lanes store one column's 128-byte block
@@ -343,18 +383,85 @@ __global__ __launch_bounds__(QT) void fp8_turn_kernel(Fp8Turn t) {
 // are `turns` of them.  They wait for memory while the others compute: a
 // backward of 8192, 1024 -> 4096 bfloat16 with both kept operands to lay out takes
 // 170 us, in three launches 174.5; of 1000, 512 -> 512 31.6 us, 36.6.
-template <class T, bool SR>
-__global__ __launch_bounds__(QT) void fp8_tile_turn_kernel(Fp8QuantParams p, Fp8Turn a, Fp8Turn b, uint32_t turns_a,
-                                                           uint32_t turns, uint32_t step) {
-  __shared__ __attribute__((aligned(16))) uint8_t room[sizeof(TurnLds) > TILE * TILE ? sizeof(TurnLds) : TILE * TILE];
-  const uint32_t before = blockIdx.x / step;  // of those that lay out, up to `turns`
-  if (before >= turns || blockIdx.x - before * step != step - 1) {
-    quantize_tile<MatrixSource<T>, true, true, false, SR>(p, blockIdx.x - (before < turns ? before : turns), room, p);
-  } else {
+struct TurnPlan {
+  Fp8Turn a, b;
+  uint32_t turns_a, turns, step;
+  // Lays this block's codes out, or names the tile that it quantizes.
+  __device__ __forceinline__ bool turns_here(uint32_t& tile, uint8_t* room) const {
+    const uint32_t before = blockIdx.x / step;  // of those that lay out, up to `turns`
+    if (before >= turns || blockIdx.x - before * step != step - 1) {
+      tile = blockIdx.x - (before < turns ? before : turns);
+      return false;
+    }
     const bool first = before < turns_a;
     const Fp8Turn t = first ? a : b;
     turn_tile(t.src, t.rows, fp8_pitch(t.K), t.dst, first ? before : before - turns_a, *reinterpret_cast<TurnLds*>(room));
+    return true;
   }
+};
+template <class T, bool SR>
+__global__ __launch_bounds__(QT) void fp8_tile_turn_kernel(Fp8QuantParams p, TurnPlan t) {
+  __shared__ __attribute__((aligned(16))) uint8_t room[sizeof(TurnLds) > TILE * TILE ? sizeof(TurnLds) : TILE * TILE];
+  uint32_t block;
+  if (t.turns_here(block, room)) return;
+  quantize_tile<MatrixSource<T>, true, true, false, SR>(p, block, room, p);
+}
+
+constexpr int64_t MOST_BLOCKS = (((int64_t)1 << 32) - 1) / QT;  // of one dimension: operands of 2^38 bytes
+static int64_t turn_blocks(const Fp8Turn& t) { return t.src ? fp8_blocks(t.rows) * fp8_blocks(t.K) : 0; }
+// For a launch of `blocks`, tiles and those that lay out (some).
+static TurnPlan turn_plan(const Fp8Turn& a, const Fp8Turn& b, int64_t blocks) {
+  const int64_t na = turn_blocks(a), n = na + turn_blocks(b);
+  return TurnPlan{a, b, (uint32_t)na, (uint32_t)n, (uint32_t)(blocks / n)};
+}
+
+hipError_t launch_fp8_turn(const Fp8Turn& t, hipStream_t s) {
+  const int64_t blocks = turn_blocks(t);
+  if (blocks == 0) return hipSuccess;
+  if (blocks > MOST_BLOCKS) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(fp8_turn_kernel, dim3((unsigned)blocks), dim3(QT), 0, s, t);
+  return hipGetLastError();
+}
+
+hipError_t launch_fp8_quantize_turn(fqt_dtype type, const Fp8QuantParams& p, const Fp8Turn& a, const Fp8Turn& b,
+                                    hipStream_t s) {
+  const int64_t tiles = fp8_blocks(p.rows) * fp8_blocks(p.cols), blocks = tiles + turn_blocks(a) + turn_blocks(b);
+  if (blocks > tiles && p.q_row && p.q_col && !p.tile && blocks <= MOST_BLOCKS) {
+    return with_type(type, [&](auto e) {
+      using T = decltype(e);
+      auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(QT), 0, s, p, turn_plan(a, b, blocks));
+        return hipGetLastError();
+      };
+      return p.stochastic ? go(fp8_tile_turn_kernel<T, true>) : go(fp8_tile_turn_kernel<T, false>);
+    });
+  }
+  hipError_t e = launch_fp8_turn(a, s);
+  if (e == hipSuccess) e = launch_fp8_turn(b, s);
+  if (e == hipSuccess && (p.q_row || p.q_col)) e = launch_fp8_quantize(type, p, s);
+  return e;
+}
+
+hipError_t launch_fp8_quantize(fqt_dtype type, const Fp8QuantParams& p, hipStream_t s) {
+  const int64_t blocks = fp8_blocks(p.rows) * fp8_blocks(p.cols);
+  if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+  return with_type(type, [&](auto e) {
+    using T = decltype(e);
+    const bool row = p.q_row, col = p.q_col;
+    auto go = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, grid_of(blocks, QT), dim3(QT), 0, s, p);
+      return hipGetLastError();
+    };
+    auto pick = [&](auto square, auto sr) {
+      constexpr bool Q = decltype(square)::value, S = decltype(sr)::value;
+      if (row && col) return go(fp8_tile_kernel<T, true, true, Q, S>);
+      return row ? go(fp8_tile_kernel<T, true, false, Q, S>) : go(fp8_tile_kernel<T, false, true, Q, S>);
+    };
+    using yes = std::true_type;
+    using no = std::false_type;
+    if (p.tile) return p.stochastic ? pick(yes{}, yes{}) : pick(yes{}, no{});
+    return p.stochastic ? pick(no{}, yes{}) : pick(no{}, no{});
+  });
 }
 
 // ---------------------------------------------------------------------------
@@ -395,32 +502,54 @@ struct GatedSource {
   static __device__ __forceinline__ void load(const GatedQuantParams& p, int64_t row, int64_t col, Quad<float> (&v)[GROUP]) {
     GatedSource(p, row, col).load(v);
   }
-  // A wave's rows (two groups) of a tile inside one half, with four columns of
-  // one block in each quad: all loads are under way before the first product.
+  // A wave's rows (two groups) of a tile inside one half: all loads are under
+  // way before the first product.
   __device__ __forceinline__ void load(Quad<float> (&v)[GROUP]) const {
     const int c0 = col / TILE * TILE;  // the tile's first column
-    const bool one = (hidden & 3) == 0 && (c0 >= hidden ? c0 + TILE <= 2 * hidden : c0 + TILE <= hidden);
-    if (__builtin_amdgcn_readfirstlane(one && rows >= 2 * GROUP)) {
-      typename Packed<G, 4>::type gv[GROUP];
-      uint32_t codes[GROUP];
-      uint8_t byte[GROUP];
-#pragma unroll
-      for (int i = 0; i < GROUP; ++i) {
-        gv[i] = *reinterpret_cast<const typename Packed<G, 4>::type*>(g + i * ldx);
-        codes[i] = *reinterpret_cast<const uint32_t*>(q + i * pitch + at);
-        byte[i] = e[i * (pitch / KEPT_BLOCK) + at / KEPT_BLOCK];
-      }
-#pragma unroll
-      for (int i = 0; i < GROUP; ++i) {
-        float d[4];
-        decode(codes[i], scale_up(byte[i]), d);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[i].v[j] = (float)gv[i][j] * d[j];
-      }
+    const bool inside = c0 >= hidden ? c0 + TILE <= 2 * hidden : c0 + TILE <= hidden;
+    if (__builtin_amdgcn_readfirstlane(inside && rows >= 2 * GROUP)) {
+      if ((hidden & 3) == 0)
+        load_all<true>(v);
+      else
+        load_all<false>(v);
       return;
     }
 #pragma unroll
     for (int i = 0; i < GROUP; ++i) load_one(i, v[i]);
+  }
+  // ONE: the four columns of a quad lie in one block, at a word.
+  template <bool ONE>
+  __device__ __forceinline__ void load_all(Quad<float> (&v)[GROUP]) const {
+    typedef uint32_t word __attribute__((aligned(1)));
+    typename Packed<G, 4>::type gv[GROUP];
+    uint32_t codes[GROUP];
+    uint8_t byte[GROUP], byte2[GROUP];
+    const G* gi = g;
+    const uint8_t *qi = q + at, *ei = e + at / KEPT_BLOCK;
+    const int next = (at + 3) / KEPT_BLOCK - at / KEPT_BLOCK;
+#pragma unroll
+    for (int i = 0; i < GROUP; ++i) {
+      gv[i] = *reinterpret_cast<const typename Packed<G, 4>::type*>(gi);
+      codes[i] = *reinterpret_cast<const word*>(qi);
+      byte[i] = *ei;
+      if (!ONE) byte2[i] = ei[next];
+      gi += ldx;
+      qi += pitch;
+      ei += pitch / KEPT_BLOCK;
+    }
+#pragma unroll
+    for (int i = 0; i < GROUP; ++i) {
+      float d[4];
+      decode(codes[i], scale_up(byte[i]), d);
+      if (!ONE) {
+        float d2[4];
+        decode(codes[i], scale_up(byte2[i]), d2);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) d[j] = (at + j) / KEPT_BLOCK == at / KEPT_BLOCK ? d[j] : d2[j];
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[i].v[j] = (float)gv[i][j] * d[j];
+    }
   }
   __device__ __forceinline__ void load_one(int i, Quad<float>& v) const {
 #pragma unroll
@@ -463,20 +592,43 @@ struct GatedSource {
   }
 };
 template <class G, bool ROW, bool COL, bool SR>
-__global__ __launch_bounds__(QT) void gated_tile_kernel(GatedQuantParams p) {
+__global__ __launch_bounds__(QT, sizeof(G) == 2 ? 4 : 3) void gated_tile_kernel(GatedQuantParams p) {
   __shared__ __attribute__((aligned(16))) uint8_t turned[COL ? TILE * TILE : 16];
   const int64_t block = block_id();
   if (block >= fp8_blocks(p.q.rows) * fp8_blocks(p.q.cols)) return;
   quantize_tile<GatedSource<G>, ROW, COL, false, SR>(p.q, (uint32_t)block, turned, p);
 }
 
-hipError_t launch_gated_quantize(fqt_dtype type, const GatedQuantParams& p, hipStream_t s) {
-  const int64_t blocks = fp8_blocks(p.q.rows) * fp8_blocks(p.q.cols);
-  if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+// With kept operands to lay out in the same launch, as above.
+template <class G, bool SR>
+__global__ __launch_bounds__(QT, sizeof(G) == 2 ? 4 : 3) void gated_tile_turn_kernel(GatedQuantParams p, TurnPlan t) {
+  __shared__ __attribute__((aligned(16))) uint8_t room[sizeof(TurnLds) > TILE * TILE ? sizeof(TurnLds) : TILE * TILE];
+  uint32_t block;
+  if (t.turns_here(block, room)) return;
+  quantize_tile<GatedSource<G>, true, true, false, SR>(p.q, block, room, p);
+}
+
+hipError_t launch_gated_quantize(fqt_dtype type, const GatedQuantParams& p, const Fp8Turn& a, const Fp8Turn& b,
+                                 hipStream_t s) {
+  const int64_t tiles = fp8_blocks(p.q.rows) * fp8_blocks(p.q.cols), blocks = tiles + turn_blocks(a) + turn_blocks(b);
+  if (tiles > 0x7FFFFFFF) return hipErrorInvalidValue;
+  if (blocks > tiles && p.q.q_row && p.q.q_col && blocks <= MOST_BLOCKS) {
+    return with_type(type, [&](auto e) {
+      using T = decltype(e);
+      auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(QT), 0, s, p, turn_plan(a, b, blocks));
+        return hipGetLastError();
+      };
+      return p.q.stochastic ? go(gated_tile_turn_kernel<T, true>) : go(gated_tile_turn_kernel<T, false>);
+    });
+  }
+  hipError_t err = launch_fp8_turn(a, s);
+  if (err == hipSuccess) err = launch_fp8_turn(b, s);
+  if (err != hipSuccess) return err;
   return with_type(type, [&](auto e) {
     using T = decltype(e);
     auto go = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, grid_of(blocks, QT), dim3(QT), 0, s, p);
+      hipLaunchKernelGGL(kernel, grid_of(tiles, QT), dim3(QT), 0, s, p);
       return hipGetLastError();
     };
     auto pick = [&](auto sr) {
@@ -485,59 +637,6 @@ hipError_t launch_gated_quantize(fqt_dtype type, const GatedQuantParams& p, hipS
       return p.q.q_row ? go(gated_tile_kernel<T, true, false, S>) : go(gated_tile_kernel<T, false, true, S>);
     };
     return p.q.stochastic ? pick(std::true_type{}) : pick(std::false_type{});
-  });
-}
-
-constexpr int64_t MOST_BLOCKS = (((int64_t)1 << 32) - 1) / QT;  // of one dimension: operands of 2^38 bytes
-static int64_t turn_blocks(const Fp8Turn& t) { return t.src ? fp8_blocks(t.rows) * fp8_blocks(t.K) : 0; }
-
-hipError_t launch_fp8_turn(const Fp8Turn& t, hipStream_t s) {
-  const int64_t blocks = turn_blocks(t);
-  if (blocks == 0) return hipSuccess;
-  if (blocks > MOST_BLOCKS) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(fp8_turn_kernel, dim3((unsigned)blocks), dim3(QT), 0, s, t);
-  return hipGetLastError();
-}
-
-hipError_t launch_fp8_quantize_turn(fqt_dtype type, const Fp8QuantParams& p, const Fp8Turn& a, const Fp8Turn& b,
-                                    hipStream_t s) {
-  const int64_t na = turn_blocks(a), nb = turn_blocks(b), blocks = fp8_blocks(p.rows) * fp8_blocks(p.cols) + na + nb;
-  if (na + nb > 0 && p.q_row && p.q_col && !p.tile && blocks <= MOST_BLOCKS) {
-    return with_type(type, [&](auto e) {
-      using T = decltype(e);
-      auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(QT), 0, s, p, a, b, (uint32_t)na, (uint32_t)(na + nb),
-                           (uint32_t)(blocks / (na + nb)));
-        return hipGetLastError();
-      };
-      return p.stochastic ? go(fp8_tile_turn_kernel<T, true>) : go(fp8_tile_turn_kernel<T, false>);
-    });
-  }
-  hipError_t e = launch_fp8_turn(a, s);
-  if (e == hipSuccess) e = launch_fp8_turn(b, s);
-  if (e == hipSuccess && (p.q_row || p.q_col)) e = launch_fp8_quantize(type, p, s);
-  return e;
-}
-
-hipError_t launch_fp8_quantize(fqt_dtype type, const Fp8QuantParams& p, hipStream_t s) {
-  const int64_t blocks = fp8_blocks(p.rows) * fp8_blocks(p.cols);
-  if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
-  return with_type(type, [&](auto e) {
-    using T = decltype(e);
-    const bool row = p.q_row, col = p.q_col;
-    auto go = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, grid_of(blocks, QT), dim3(QT), 0, s, p);
-      return hipGetLastError();
-    };
-    auto pick = [&](auto square, auto sr) {
-      constexpr bool Q = decltype(square)::value, S = decltype(sr)::value;
-      if (row && col) return go(fp8_tile_kernel<T, true, true, Q, S>);
-      return row ? go(fp8_tile_kernel<T, true, false, Q, S>) : go(fp8_tile_kernel<T, false, true, Q, S>);
-    };
-    using yes = std::true_type;
-    using no = std::false_type;
-    if (p.tile) return p.stochastic ? pick(yes{}, yes{}) : pick(yes{}, no{});
-    return p.stochastic ? pick(no{}, yes{}) : pick(no{}, no{});
   });
 }
 

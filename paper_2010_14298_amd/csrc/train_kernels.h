@@ -217,6 +217,10 @@ Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K);
 hipError_t launch_fp8_parts(const Fp8GemmParams& p, const Fp8Plan& plan, hipStream_t s);  // to p.part
 fqt_fp8_form fp8_gemm_form(int64_t M, int64_t N, int64_t K, bool masked, bool lines);
 hipError_t launch_fp8_gemm(fqt_dtype type, const Fp8GemmParams& p, hipStream_t s);
+// Two products that do not depend on each other, a with float32 outputs; whether
+// they run at once (and need partial sums of their own) or one behind the other.
+bool fp8_two_at_once(int64_t Ma, int64_t Na, int64_t Ka, int64_t Mb, int64_t Nb, int64_t Kb);
+hipError_t launch_fp8_two(fqt_dtype type, const Fp8GemmParams& a, const Fp8GemmParams& b, hipStream_t s);
 
 // ---------------------------------------------------------------------------
 // gated layer
@@ -234,14 +238,15 @@ bool gated_rows_raw(const GatedGemmParams& p);
 int64_t gated_partials(int64_t M, int64_t hidden, int64_t K);  // floats
 hipError_t launch_gated_gemm(fqt_dtype type, const GatedGemmParams& p, const void* x, int64_t ldx, hipStream_t s);
 
-// The quantizer of D = [G gate | G up] [rows, cols = 2 hidden]: q.x, q.ldx are
-// G's.
+// The quantizer of D = [G gate | G up] [rows, cols = 2 hidden], q.x and q.ldx those
+// of G, with kept operands to lay out, as above.
 struct GatedQuantParams {
   Fp8QuantParams q;
   int64_t hidden;
   const uint8_t *q_gate, *e_gate, *q_up, *e_up;
 };
-hipError_t launch_gated_quantize(fqt_dtype type, const GatedQuantParams& p, hipStream_t s);
+hipError_t launch_gated_quantize(fqt_dtype type, const GatedQuantParams& p, const Fp8Turn& a, const Fp8Turn& b,
+                                 hipStream_t s);
 
 // ---------------------------------------------------------------------------
 // gradient norm and clipping

@@ -500,7 +500,9 @@ fqt_status fqt_fp8_gated_forward(const void* X, fqt_dtype type, int64_t N, int64
                                  const fqt_fp8* W8, int64_t hidden, fqt_act act, void* H, int64_t ldh,
                                  const fqt_fp8* X8t, const fqt_kept* d_gate, const fqt_kept* d_up, void* ws,
                                  size_t ws_bytes, fqt_stream_t s);
-size_t fqt_fp8_gated_forward_workspace(int64_t N, int64_t d_in, int64_t hidden);
+/* k_major: that of W8; save: d_gate or d_up is wanted.  May be 0: ws may then be
+ * NULL.                                                                      */
+size_t fqt_fp8_gated_forward_workspace(int64_t N, int64_t d_in, int64_t hidden, int k_major, int save);
 
 /* Its backward.  With G = dL/dH [N, hidden], the float32 products
  *   D [N, 2 hidden] = [G d_gate | G d_up]

@@ -143,9 +143,11 @@ hipError_t gradients_of(fqt_dtype type, const BackwardWs& w, int64_t N, int64_t 
   return grad_W ? launch_fp8_gemm(FQT_F32, p, s) : launch_fp8_gemm(type, r, s);
 }
 
-ForwardWs carve_gated_forward(Carver& c, int64_t N, int64_t d_in, int64_t hidden) {
-  ForwardWs w;
-  w.w = c.take<uint8_t>(2 * hidden * fp8_pitch(d_in));
+// raw: X is read as it is; k_major: the weights' codes lie column by column.
+ForwardWs carve_gated_forward(Carver& c, int64_t N, int64_t d_in, int64_t hidden, bool raw, bool k_major) {
+  ForwardWs w{};
+  if (k_major) w.w = c.take<uint8_t>(2 * hidden * fp8_pitch(d_in));
+  if (raw) return w;
   w.x = take_operand(c, N, d_in);
   w.part = c.take<float>(gated_partials(N, hidden, d_in));
   return w;
@@ -445,10 +447,10 @@ fqt_status fqt_fp8_linear_backward(const void* G, fqt_dtype type, int64_t N, int
 // ---------------------------------------------------------------------------
 // gated layer
 // ---------------------------------------------------------------------------
-size_t fqt_fp8_gated_forward_workspace(int64_t N, int64_t d_in, int64_t hidden) {
+size_t fqt_fp8_gated_forward_workspace(int64_t N, int64_t d_in, int64_t hidden, int k_major, int save) {
   if (!side(N) || !side(d_in) || !half_side(hidden)) return 0;
   Carver c(nullptr);
-  carve_gated_forward(c, N, d_in, hidden);
+  carve_gated_forward(c, N, d_in, hidden, !save && gated_rows_raw(N, hidden, d_in), k_major != 0);
   return c.off;
 }
 
@@ -461,9 +463,11 @@ fqt_status fqt_fp8_gated_forward(const void* X, fqt_dtype type, int64_t N, int64
   if (act != FQT_SILU && act != FQT_GELU_TANH && act != FQT_RELU) return FQT_EINVAL;
   if ((X8t && !written(X8t)) || (d_gate && !checkpoint(d_gate)) || (d_up && !checkpoint(d_up))) return FQT_EINVAL;
   if (d_in > MAX_CONTRACTION) return FQT_EUNSUPPORTED;
-  if (!ws || !aligned(ws, 16) || ws_bytes < fqt_fp8_gated_forward_workspace(N, d_in, hidden)) return FQT_EWORKSPACE;
+  const bool raw = !d_gate && !d_up && gated_rows_raw(N, hidden, d_in);
+  const size_t need = fqt_fp8_gated_forward_workspace(N, d_in, hidden, W8->k_major, d_gate || d_up);
+  if (need > 0 && (!ws || !aligned(ws, 16) || ws_bytes < need)) return FQT_EWORKSPACE;
   Carver c(ws);
-  const ForwardWs w = carve_gated_forward(c, N, d_in, hidden);
+  const ForwardWs w = carve_gated_forward(c, N, d_in, hidden, raw, W8->k_major != 0);
   GatedGemmParams p{};
   p.M = N;
   p.N = 2 * hidden;
@@ -480,7 +484,7 @@ fqt_status fqt_fp8_gated_forward(const void* X, fqt_dtype type, int64_t N, int64
   q.rows = N;
   q.cols = d_in;
   q.ldx = ldx;
-  if (!gated_rows_raw(p)) {
+  if (!raw) {
     q.q_row = w.x.q;
     q.e_row = w.x.e;
   }

@@ -939,74 +939,79 @@ inline int64_t tiles_of(int64_t M, int64_t N, int64_t bm, int64_t bn) {
 constexpr int ROW_WAVES = 8;
 
 template <class X>
-__device__ __forceinline__ v8i row_block(const X* x, int64_t left, int& byte) {
+struct RawBlock {
   Quad<X> v[8];
-  uint32_t key = 0u;
-  typename Quad<X>::ColTop unused{};
+  __device__ __forceinline__ void load(const X* x, int64_t left) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i].load(x + 4 * i, left - 4 * i);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    typename Quad<X>::RowTop r;
-    v[i].top(r, unused);
-    const uint32_t k = Quad<X>::row_key(r);
-    key = key > k ? key : k;
+    for (int i = 0; i < 8; ++i) v[i].load(x + 4 * i, left - 4 * i);
   }
-  auto s = __builtin_amdgcn_permlane16_swap(key, key, false, false);
-  key = s[0] > s[1] ? s[0] : s[1];
-  s = __builtin_amdgcn_permlane32_swap(key, key, false, false);
-  key = Quad<X>::bf_keys(s[0] > s[1] ? s[0] : s[1]) & 0xffffu;
-  const uint32_t e = scale_bytes(key) & 0xffffu;
-  byte = (int)(key >= NAN_KEY ? 255u : e);
-  v8i q;
+  // All 32 are there: loads without a branch, which would wait for each.
+  __device__ __forceinline__ void load_whole(const X* x) {
+    struct Words {
+      uint32_t w[sizeof(v) / 4];
+    } all;
+    __builtin_memcpy(&all, __builtin_assume_aligned(x, sizeof(X)), sizeof(v));
+    __builtin_memcpy(&v, &all, sizeof(v));
+  }
+  __device__ __forceinline__ v8i codes(int& byte) const {
+    uint32_t key = 0u;
+    typename Quad<X>::ColTop unused{};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) q[i] = key >= NAN_KEY ? 0x7f7f7f7f : (int)v[i].row_codes(scale_up(e));
-  return q;
-}
+    for (int i = 0; i < 8; ++i) {
+      typename Quad<X>::RowTop r;
+      v[i].top(r, unused);
+      const uint32_t k = Quad<X>::row_key(r);
+      key = key > k ? key : k;
+    }
+    auto s = __builtin_amdgcn_permlane16_swap(key, key, false, false);
+    key = s[0] > s[1] ? s[0] : s[1];
+    s = __builtin_amdgcn_permlane32_swap(key, key, false, false);
+    key = Quad<X>::bf_keys(s[0] > s[1] ? s[0] : s[1]) & 0xffffu;
+    const uint32_t e = scale_bytes(key) & 0xffffu;
+    byte = (int)(key >= NAN_KEY ? 255u : e);
+    v8i q;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = key >= NAN_KEY ? 0x7f7f7f7f : (int)v[i].row_codes(scale_up(e));
+    return q;
+  }
+};
 __device__ __forceinline__ v8i code_block(const uint8_t* q) {
   const v4i a = *reinterpret_cast<const v4i*>(q), b = *reinterpret_cast<const v4i*>(q + 16);
   return v8i{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 }
 
-// X: the raw rows' type, or void: codes.  MT: 16 MT >= M.
-// Gated: 16 hidden units a block, their a and b.
-template <class T, class X, int MT, class P = Fp8GemmParams>
-__global__ __launch_bounds__(64 * ROW_WAVES) void fp8_rows_kernel(P p, const void* x, int64_t ldx) {
-  constexpr int H = P::GATED ? 2 : 1;
-  __shared__ float sum[ROW_WAVES][H][MT][256];
+// X: the raw rows' type, or void: codes.  16 MT >= M.
+template <class T, class X, int MT>
+__global__ __launch_bounds__(64 * ROW_WAVES) void fp8_rows_kernel(Fp8GemmParams p, const void* x, int64_t ldx) {
+  __shared__ float sum[ROW_WAVES][MT][256];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
-  const int64_t n0 = block_id() * 16, cols = columns(p);
-  if (n0 >= cols) return;
-  const int64_t n = n0 + r < cols ? n0 + r : cols - 1;
+  const int64_t n0 = block_id() * 16;
+  if (n0 >= p.N) return;
+  const int64_t n = n0 + r < p.N ? n0 + r : p.N - 1;
   const int64_t pitch = fp8_pitch(p.K);
   const int nk = (int)fp8_blocks(p.K);
   const uint8_t* const w = p.B + n * pitch + 32 * g;
-  v4f acc[H][MT];
+  v4f acc[MT];
 #pragma unroll
-  for (int h = 0; h < H; ++h)
-#pragma unroll
-    for (int m = 0; m < MT; ++m) acc[h][m] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int m = 0; m < MT; ++m) acc[m] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
   // the weights two turns ahead
-  struct Weights {
-    v8i b[H];
-    int s[H];
-  } w0{}, w1{};
-  auto weights = [&](int k, Weights& to) __attribute__((always_inline)) {
+  v8i b0{}, b1{};
+  int s0 = 127, s1 = 127;
+  auto weights = [&](int k, v8i& b, int& sb) __attribute__((always_inline)) {
     if (k >= nk) return;
-#pragma unroll
-    for (int h = 0; h < H; ++h) {
-      to.b[h] = code_block(w + h * cols * pitch + (int64_t)k * FP8_BLOCK);
-      to.s[h] = p.eB[((int64_t)(k >> 2) * p.N + h * cols + n) * 4 + (k & 3)];
-    }
+    b = code_block(w + (int64_t)k * FP8_BLOCK);
+    sb = p.eB[((int64_t)(k >> 2) * p.N + n) * 4 + (k & 3)];
   };
-  weights(wave, w0);
-  weights(wave + ROW_WAVES, w1);
+  weights(wave, b0, s0);
+  weights(wave + ROW_WAVES, b1, s1);
   for (int k = wave; k < nk; k += ROW_WAVES) {
-    const Weights now = w0;
-    w0 = w1;
-    weights(k + 2 * ROW_WAVES, w1);
+    const v8i b = b0;
+    const int sb = s0;
+    b0 = b1;
+    s0 = s1;
+    weights(k + 2 * ROW_WAVES, b1, s1);
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
       const int64_t row = 16 * m + r;
@@ -1019,49 +1024,112 @@ __global__ __launch_bounds__(64 * ROW_WAVES) void fp8_rows_kernel(P p, const voi
         }
       } else {
         const int64_t at = (int64_t)k * FP8_BLOCK + 32 * g;
-        a = row_block(static_cast<const X*>(x) + (row < p.M ? row : 0) * ldx + at, row < p.M ? p.K - at : 0, sa);
+        RawBlock<X> raw;
+        raw.load(static_cast<const X*>(x) + (row < p.M ? row : 0) * ldx + at, row < p.M ? p.K - at : 0);
+        a = raw.codes(sa);
       }
-      const float fa = scale_of(sa);
+      const float fa = scale_of(sa), fb = scale_of(sb);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const v8b wa = widen(a[2 * q], a[2 * q + 1], fa);
-#pragma unroll
-        for (int h = 0; h < H; ++h)
-          acc[h][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-              widen(now.b[h][2 * q], now.b[h][2 * q + 1], scale_of(now.s[h])), wa, acc[h][m], 0, 0, 0);
-      }
+      for (int q = 0; q < 4; ++q)
+        acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(b[2 * q], b[2 * q + 1], fb),
+                                                         widen(a[2 * q], a[2 * q + 1], fa), acc[m], 0, 0, 0);
     }
   }
   // lane: output columns n0 + 4 g .., row r
 #pragma unroll
-  for (int h = 0; h < H; ++h)
+  for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sum[wave][h][m][r * 16 + 4 * g + i] = acc[h][m][i];
+    for (int i = 0; i < 4; ++i) sum[wave][m][r * 16 + 4 * g + i] = acc[m][i];
   __syncthreads();
   for (int i = threadIdx.x; i < MT * 256; i += 64 * ROW_WAVES) {
     const int64_t row = i >> 4, col = n0 + (i & 15);
-    if (row >= p.M || col >= cols) continue;
-    float o[H];
+    if (row >= p.M || col >= p.N) continue;
+    float o = 0.0f;
 #pragma unroll
-    for (int h = 0; h < H; ++h) {
-      o[h] = 0.0f;
-#pragma unroll
-      for (int v = 0; v < ROW_WAVES; ++v) o[h] += sum[v][h][i >> 8][i & 255];
-    }
-    if constexpr (P::GATED) {
-      with_act(p.act, [&](auto act) {
-        float slope;
-        activate<decltype(act)::value>(o[0], o[0], slope);
-      });
-      o[0] *= o[H - 1];
-    } else {
-      if (p.relu) o[0] = o[0] < 0.0f ? 0.0f : o[0];
-      if (p.mask) o[0] = (float)static_cast<const T*>(p.mask)[row * p.ldmask + col] > 0.0f ? o[0] : 0.0f;
-    }
-    static_cast<T*>(p.C)[row * p.ldc + col] = (T)o[0];
+    for (int v = 0; v < ROW_WAVES; ++v) o += sum[v][i >> 8][i & 255];
+    if (p.relu) o = o < 0.0f ? 0.0f : o;
+    if (p.mask) o = (float)static_cast<const T*>(p.mask)[row * p.ldmask + col] > 0.0f ? o : 0.0f;
+    static_cast<T*>(p.C)[row * p.ldc + col] = (T)o;
   }
+}
+
+// Gated: a block takes 16 rows of X, as they are, against 16 hidden units.  The
+// rows' blocks of K are loaded a turn ahead, the weights' two.
+template <class T, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void gated_rows_kernel(GatedGemmParams p, const T* x, int64_t ldx) {
+  __shared__ float sum[WAVES][2][256];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, g = lane >> 4;
+  const int64_t n0 = block_id() * 16, m0 = (int64_t)blockIdx.z * 16;
+  if (n0 >= p.hidden) return;
+  const int64_t n = n0 + r < p.hidden ? n0 + r : p.hidden - 1;
+  const int64_t pitch = fp8_pitch(p.K), row = m0 + r;
+  const int nk = (int)fp8_blocks(p.K);
+  const uint8_t* const w = p.B + n * pitch + 32 * g;
+  const T* const xr = x + (row < p.M ? row : m0) * ldx + 32 * g;  // rows past the last are not stored
+  struct Weights {
+    v8i b[2];
+    int s[2];
+  } w0{}, w1{};
+  RawBlock<T> raw{};
+  auto weights = [&](int k, Weights& to) __attribute__((always_inline)) {
+    if (k >= nk) return;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      to.b[h] = code_block(w + h * p.hidden * pitch + (int64_t)k * FP8_BLOCK);
+      to.s[h] = p.eB[((int64_t)(k >> 2) * p.N + h * p.hidden + n) * 4 + (k & 3)];
+    }
+  };
+  auto rows = [&](int k) __attribute__((always_inline)) {
+    const int64_t at = (int64_t)k * FP8_BLOCK;
+    if (at + FP8_BLOCK <= p.K)
+      raw.load_whole(xr + at);
+    else if (k < nk)
+      raw.load(xr + at, p.K - 32 * g - at);
+  };
+  v4f acc[2] = {v4f{0.0f, 0.0f, 0.0f, 0.0f}, v4f{0.0f, 0.0f, 0.0f, 0.0f}};
+  rows(wave);
+  weights(wave, w0);
+  weights(wave + WAVES, w1);
+  for (int k = wave; k < nk; k += WAVES) {
+    const Weights now = w0;
+    const RawBlock<T> here = raw;
+    w0 = w1;
+    rows(k + WAVES);
+    weights(k + 2 * WAVES, w1);
+    int sa;
+    const v8i a = here.codes(sa);
+    const float fa = scale_of(sa), fb[2] = {scale_of(now.s[0]), scale_of(now.s[1])};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const v8b wa = widen(a[2 * q], a[2 * q + 1], fa);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        acc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(now.b[h][2 * q], now.b[h][2 * q + 1], fb[h]), wa, acc[h],
+                                                         0, 0, 0);
+    }
+  }
+  // lane: hidden units n0 + 4 g .., row r
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[wave][h][r * 16 + 4 * g + i] = acc[h][i];
+  __syncthreads();
+  const int i = threadIdx.x;
+  const int64_t to = m0 + (i >> 4), col = n0 + (i & 15);
+  if (i >= 256 || to >= p.M || col >= p.hidden) return;
+  float a = 0.0f, b = 0.0f;
+#pragma unroll
+  for (int v = 0; v < WAVES; ++v) {
+    a += sum[v][0][i];
+    b += sum[v][1][i];
+  }
+  with_act(p.act, [&](auto act) {
+    float slope;
+    activate<decltype(act)::value>(a, a, slope);
+  });
+  static_cast<T*>(p.C)[to * p.ldc + col] = (T)(a * b);
 }
 
 }  // namespace fqt

@@ -70,9 +70,17 @@ __global__ __launch_bounds__(256) void gated_finish_kernel(GatedGemmParams p, in
 // ---------------------------------------------------------------------------
 // launches
 // ---------------------------------------------------------------------------
-constexpr int64_t GATED_ROWS_MAX = 64, GATED_RAW_MAX = 16;
-static bool few_rows(const GatedGemmParams& p) { return p.M <= GATED_ROWS_MAX && !p.gate.q && !p.up.q; }
-bool gated_rows_raw(const GatedGemmParams& p) { return few_rows(p) && p.M <= GATED_RAW_MAX; }
+// Few rows that keep nothing (serving) are read as they are, 16 a block, each of
+// which quantizes them for itself; with more blocks or a longer K a quantizer in
+// front and the tiles are faster.  us in a graph, bfloat16, as they are / tiles:
+// 1024 -> 4096 one row 3.9, 16 rows 4.5, 64 10.8 / 16.1, 96 15.6 / 16.0, 128 20 / 15;
+// 2048 -> 1001 48 rows 7.0 / 20, 128 12.4 / 18.8; 4096 -> 4096 17 rows 18.9 / 24.5,
+// 48 31 / 24.
+bool gated_rows_raw(int64_t M, int64_t hidden, int64_t K) {
+  if (M > 128) return false;
+  const int64_t nk = fp8_blocks(K), turns = ((M + 15) / 16 * ((hidden + 15) / 16) + 255) / 256;
+  return M <= 16 || turns * nk < 40 + nk + nk / 2;
+}
 int64_t gated_partials(int64_t M, int64_t hidden, int64_t K) {
   const int64_t s = fp8_plan(M, 2 * hidden, K).splits;
   return s > 1 ? s * M * 2 * hidden : 0;
@@ -108,16 +116,18 @@ static hipError_t gated_tiles(const GatedGemm<SAVE>& p, const Fp8Plan& plan, hip
 hipError_t launch_gated_gemm(fqt_dtype type, const GatedGemmParams& params, const void* x, int64_t ldx, hipStream_t s) {
   return with_type(type, [&](auto e) {
     using T = decltype(e);
-    if (few_rows(params)) {
-      const GatedGemm<false> p{params};
-      const int64_t blocks = (p.hidden + 15) / 16;
-      auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, grid_of(blocks, 64 * ROW_WAVES), dim3(64 * ROW_WAVES), 0, s, p, x, ldx);
-        return hipGetLastError();
-      };
-      if (gated_rows_raw(params)) return go(fp8_rows_kernel<T, T, 1, GatedGemm<false>>);
-      if (p.M <= 16) return go(fp8_rows_kernel<T, void, 1, GatedGemm<false>>);
-      return p.M <= 32 ? go(fp8_rows_kernel<T, void, 2, GatedGemm<false>>) : go(fp8_rows_kernel<T, void, 4, GatedGemm<false>>);
+    if (!params.gate.q && !params.up.q && gated_rows_raw(params.M, params.hidden, params.K)) {
+      dim3 grid = grid_of((params.hidden + 15) / 16, 64 * 16);
+      grid.z = (unsigned)((params.M + 15) / 16);
+      const T* const rows = static_cast<const T*>(x);
+      if constexpr (sizeof(T) == 2) {  // float32 rows do not fit the registers of sixteen waves
+        if (fp8_blocks(params.K) > 8) {
+          hipLaunchKernelGGL((gated_rows_kernel<T, 16>), grid, dim3(64 * 16), 0, s, params, rows, ldx);
+          return hipGetLastError();
+        }
+      }
+      hipLaunchKernelGGL((gated_rows_kernel<T, 8>), grid, dim3(64 * 8), 0, s, params, rows, ldx);
+      return hipGetLastError();
     }
     const Fp8Plan plan = fp8_plan(params.M, params.N, params.K);
     if (plan.splits > 1) {

@@ -233,8 +233,8 @@ struct GatedGemmParams : Fp8GemmParams {
   fqt_act act;
   Kept gate, up;
 };
-// Whether X [M, K] is read as it is (p.A is not).
-bool gated_rows_raw(const GatedGemmParams& p);
+// Whether a call that keeps nothing reads X [M, K] as it is (p.A is not read).
+bool gated_rows_raw(int64_t M, int64_t hidden, int64_t K);
 int64_t gated_partials(int64_t M, int64_t hidden, int64_t K);  // floats
 hipError_t launch_gated_gemm(fqt_dtype type, const GatedGemmParams& p, const void* x, int64_t ldx, hipStream_t s);
 

@@ -144,7 +144,7 @@ def load(path=LIB_PATH):
         "fqt_layernorm_forward8": ([vp, i32, i64, i64, i64, vp, vp, f32, vp, i64, kep, vp, vp], i32),
         "fqt_layernorm_backward8": ([vp, i64, kep, i32, i64, i64, vp, vp, vp, i64, vp, vp, vp, sz, vp], i32),
         "fqt_fp8_gated_forward": ([vp, i32, i64, i64, i64, f8p, i64, i32, vp, i64, f8p, kep, kep, vp, sz, vp], i32),
-        "fqt_fp8_gated_forward_workspace": ([i64, i64, i64], sz),
+        "fqt_fp8_gated_forward_workspace": ([i64, i64, i64, i32, i32], sz),
         "fqt_fp8_gated_backward": ([vp, i32, i64, i64, i64, kep, kep, f8p, f8p, i64, i32, u64, vp, vp, i64, vp, sz,
                                     vp], i32),
         "fqt_fp8_gated_backward_workspace": ([i64, i64, i64], sz),
@@ -799,14 +799,15 @@ def fqt_layernorm_backward8(G, xh8, rstd, gamma=None, grad_X=None, params=True, 
 ACTS = {"silu": 0, "gelu_tanh": 1, "relu": 2}
 
 
-def fqt_fp8_gated_forward_workspace(N, d_in, hidden):
-    return load().fqt_fp8_gated_forward_workspace(N, d_in, hidden)
+def fqt_fp8_gated_forward_workspace(N, d_in, hidden, k_major=False, save=True):
+    """Bytes; k_major: W8's codes lie column by column."""
+    return load().fqt_fp8_gated_forward_workspace(N, d_in, hidden, int(bool(k_major)), int(bool(save)))
 
 
 def fqt_fp8_gated_forward(X, W8, act="silu", save=True, H=None, ws=None):
     """H = act(Q(X) W_gate^T) Q(X) W_up^T, W8 the by_row operand (tile=True) of [W_gate; W_up].  save: also what
     fqt_fp8_gated_backward reads, dict(X8t=operand of X^T, d_gate, d_up=checkpoints of H's derivatives by the two
-    products).  Returns (H, kept or None, ws)."""
+    products).  Returns (H, kept or None, ws or None: a call of few rows may need none)."""
     dev = _device()
     px, dt, N, d_in, ldx = _matrix(X, "X", dev)
     code = ACTS.get(act)
@@ -829,12 +830,17 @@ def fqt_fp8_gated_forward(X, W8, act="silu", save=True, H=None, ws=None):
         d_up, cu = _new_kept(X, N, hidden)
         kept = dict(X8t=X8t, d_gate=d_gate, d_up=d_up)
     lib = load()
-    if ws is None:
-        ws = X.new_empty(lib.fqt_fp8_gated_forward_workspace(N, d_in, hidden), dtype=torch.uint8)
-    else:
+    pw = room = 0
+    if ws is not None:
         _room(ws, dev)
-    rc = lib.fqt_fp8_gated_forward(px, dt, N, d_in, ldx, w8, hidden, code, ph, ldh, x8t, cg, cu, ws.data_ptr(),
-                                   ws.numel(), _raw_stream(dev))
+    else:
+        room = lib.fqt_fp8_gated_forward_workspace(N, d_in, hidden, w8.k_major, save)
+        if room:
+            ws = X.new_empty(room, dtype=torch.uint8)
+    if ws is not None:
+        pw, room = ws.data_ptr(), ws.numel()
+    rc = lib.fqt_fp8_gated_forward(px, dt, N, d_in, ldx, w8, hidden, code, ph, ldh, x8t, cg, cu, pw, room,
+                                   _raw_stream(dev))
     _check("fqt_fp8_gated_forward", rc)
     return H, kept, ws
 

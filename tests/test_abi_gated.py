@@ -31,10 +31,15 @@ def kept(q=FAKE, e=FAKE):
 
 def test_sizes(lib):
     assert [lib.fqt_fp8_kept_pitch(c) for c in (-1, 0, 1, 32, 33, 1 << 31)] == [0, 0, 32, 32, 64, 0]
-    assert lib.fqt_fp8_gated_forward_workspace(300, 1000, 64) >= 300 * 1024
+    assert lib.fqt_fp8_gated_forward_workspace(300, 1000, 64, 0, 1) >= 300 * 1024
+    assert lib.fqt_fp8_gated_forward_workspace(300, 1000, 64, 1, 0) >= 300 * 1024 + 128 * 1024
+    # few rows that keep nothing are read as they are
+    assert lib.fqt_fp8_gated_forward_workspace(1, 1000, 64, 0, 0) == 0
+    assert lib.fqt_fp8_gated_forward_workspace(1, 1000, 64, 0, 1) > 0
+    assert lib.fqt_fp8_gated_forward_workspace(1, 1000, 64, 1, 0) >= 128 * 1024
     assert lib.fqt_fp8_gated_backward_workspace(300, 1000, 64) >= 300 * 128 + 128 * 384
     for bad in ((0, 8, 8), (8, 0, 8), (8, 8, 0), (8, 8, 1 << 30), (1 << 31, 8, 8), (8, 8, -1)):
-        assert lib.fqt_fp8_gated_forward_workspace(*bad) == 0 and lib.fqt_fp8_gated_backward_workspace(*bad) == 0
+        assert lib.fqt_fp8_gated_forward_workspace(*bad, 1, 1) == 0 and lib.fqt_fp8_gated_backward_workspace(*bad) == 0
 
 
 def test_layernorm8_arguments(lib):
@@ -63,7 +68,7 @@ def test_gated_arguments(lib):
         assert fwd(**bad) == 1, bad
     assert fwd(ws=None) == 4 and fwd(n=64) == 4 and fwd(ws=FAKE + 8) == 4 and fwd(i=(1 << 23) + 1) == 2
     # nothing kept: the next check fails, the workspace's
-    assert fwd(Xt=None, a=None, b=None, n=64) == 4
+    assert fwd(Xt=None, a=None, b=None, W=op(FAKE, FAKE, 1), n=64) == 4
 
     def bwd(G=FAKE, t=0, N=4, h=8, ldg=8, a=kept(), b=kept(), X=op(), W=op(), i=8, sr=1, gw=FAKE, gx=FAKE, ldgx=8,
             ws=FAKE, n=WS):

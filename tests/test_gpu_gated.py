@@ -397,6 +397,7 @@ def test_refusals():
                  lambda: f.fqt_fp8_gated_backward(g, kept, W8), lambda: f.fqt_fp8_gated_backward(g, kept, W8t, grad_W=torch.empty((96, 64)))):
         with pytest.raises(ValueError):
             call()
+    assert f.fqt_fp8_gated_forward(X, W8, save=False)[2] is None  # twenty rows, read as they are
     with pytest.raises(f.FqtError) as e:
         f.fqt_fp8_gated_forward(X, W8, ws=torch.empty(64, dtype=torch.uint8, device="cuda"))
     assert e.value.code == 4

@@ -220,78 +220,13 @@ __global__ __launch_bounds__(C::THREADS) void norm_forward_long_kernel(NormParam
   }
 }
 
-// Backward: one block of 1024 threads a unit, so that there are few partial
-// sums (8192 x 1024 bfloat16: 1024 blocks of four teams leave 8 MB of them, 21.1
-// us in all instead of 17.8; float32 29.5, 27.3).  Each team takes every (teams)-th row and keeps its columns'
-// sums of g xh and g in registers; at the end the block's teams meet in LDS
-// pairwise and one writes the block's partial row (an only block writes the
-// parameter gradients themselves).
-// KEPT: xh from its checkpoint.
-template <class T, class C, bool KEPT>
-__global__ __launch_bounds__(C::THREADS) void norm_backward_kernel(NormParams p) {
-  __shared__ float sh[C::PER_BLOCK][C::WAVES][2];
-  __shared__ __attribute__((aligned(16))) float col_sum[C::PER_BLOCK > 1 ? C::PER_BLOCK / 2 : 1][2][C::PER_BLOCK > 1 ? C::COLS : 4];
-  const int t = threadIdx.x % C::TPR, team = threadIdx.x / C::TPR;
-  const float inv = 1.0f / (float)p.cols;
-  float sg[C::NV][C::VEC], sb[C::NV][C::VEC];
-#pragma unroll
-  for (int k = 0; k < C::NV; ++k)
-#pragma unroll
-    for (int i = 0; i < C::VEC; ++i) sg[k][i] = sb[k][i] = 0.0f;
-  // every team of the block makes the same number of turns (the barriers
-  // inside team_sum meet); a team without a row reads and writes nothing
-  for (int64_t base = (int64_t)blockIdx.x * C::PER_BLOCK; base < p.rows; base += (int64_t)gridDim.x * C::PER_BLOCK) {
-    const bool any = base + team < p.rows;
-    const int64_t row = any ? base + team : 0;
-    const int cols = any ? (int)p.cols : 0;
-    const T* x = static_cast<const T*>(p.x) + row * p.ldx;
-    const T* g = static_cast<const T*>(p.g) + row * p.ldg;
-    const int64_t pitch = kept_pitch(p.cols);
-    float xh[C::NV][C::VEC], gv[C::NV][C::VEC];
-#pragma unroll
-    for (int k = 0; k < C::NV; ++k) {
-      const int col = (k * C::TPR + t) * C::VEC;
-      if constexpr (KEPT)
-        kept_values<C::VEC>(p.q8 + row * pitch, p.e8 + row * (pitch / KEPT_BLOCK), cols - col, col, xh[k]);
-      else
-        load_part<T, C::VEC>(x + col, cols - col, xh[k]);
-      load_part<T, C::VEC>(g + col, cols - col, gv[k]);
-    }
-    const float mean = KEPT ? 0.0f : p.mean[row], rstd = p.rstd[row];
-    float s[2] = {0.0f, 0.0f};
-#pragma unroll
-    for (int k = 0; k < C::NV; ++k) {
-      const int col = (k * C::TPR + t) * C::VEC;
-      float ga[C::VEC];
-#pragma unroll
-      for (int i = 0; i < C::VEC; ++i) ga[i] = 1.0f;
-      // read again for every row: from the nearest cache, and the registers
-      // hold more waves instead
-      if (p.gamma) load_part<float, C::VEC>(p.gamma + col, (int)p.cols - col, ga);
-#pragma unroll
-      for (int i = 0; i < C::VEC; ++i) {
-        // no column (or no row): xh is 0 like g, since (0 - mean) rstd may be infinite
-        if constexpr (!KEPT) xh[k][i] = col + i < cols ? (xh[k][i] - mean) * rstd : 0.0f;
-        sg[k][i] = fmaf(gv[k][i], xh[k][i], sg[k][i]);
-        sb[k][i] += gv[k][i];
-        gv[k][i] *= ga[i];
-        s[0] += gv[k][i];
-        s[1] = fmaf(gv[k][i], xh[k][i], s[1]);
-      }
-    }
-    team_sum<C, 2>(s, sh[team]);
-    const float a = s[0] * inv, b = s[1] * inv;
-    T* y = static_cast<T*>(p.y) + row * p.ldy;
-#pragma unroll
-    for (int k = 0; k < C::NV; ++k) {
-      const int64_t col = (int64_t)(k * C::TPR + t) * C::VEC;
-      float o[C::VEC];
-#pragma unroll
-      for (int i = 0; i < C::VEC; ++i) o[i] = rstd * ((gv[k][i] - a) - xh[k][i] * b);
-      store_part<T, C::VEC>(y + col, cols - col, o);
-    }
-  }
-  if (!p.grad_gamma && !p.grad_beta) return;
+// The sums of a block's teams, added up pairwise in LDS: one partial row (an only
+// block writes the parameter gradients themselves).
+template <class C>
+using ColumnSums = float[C::PER_BLOCK > 1 ? C::PER_BLOCK / 2 : 1][2][C::PER_BLOCK > 1 ? C::COLS : 4];
+template <class C>
+__device__ __forceinline__ void store_columns(const NormParams& p, float (&sg)[C::NV][C::VEC], float (&sb)[C::NV][C::VEC],
+                                              ColumnSums<C>& col_sum, int t, int team) {
 #pragma unroll
   for (int w = C::PER_BLOCK / 2; w > 0; w /= 2) {  // teams w .. 2 w - 1 hand over to 0 .. w - 1
     if (team >= w && team < 2 * w) {
@@ -329,6 +264,213 @@ __global__ __launch_bounds__(C::THREADS) void norm_backward_kernel(NormParams p)
     if (to_gamma) store_part<float, C::VEC>(to_gamma + col, p.cols - col, sg[k]);
     if (to_beta) store_part<float, C::VEC>(to_beta + col, p.cols - col, sb[k]);
   }
+}
+
+// Backward: one block of 1024 threads a unit, so that there are few partial
+// sums (8192 x 1024 bfloat16: 1024 blocks of four teams leave 8 MB of them, 21.1
+// us in all instead of 17.8; float32 29.5, 27.3).  Each team takes every (teams)-th row and keeps its columns'
+// sums of g xh and g in registers.
+template <class T, class C>
+__global__ __launch_bounds__(C::THREADS) void norm_backward_kernel(NormParams p) {
+  __shared__ float sh[C::PER_BLOCK][C::WAVES][2];
+  __shared__ __attribute__((aligned(16))) ColumnSums<C> col_sum;
+  const int t = threadIdx.x % C::TPR, team = threadIdx.x / C::TPR;
+  const float inv = 1.0f / (float)p.cols;
+  float sg[C::NV][C::VEC], sb[C::NV][C::VEC];
+#pragma unroll
+  for (int k = 0; k < C::NV; ++k)
+#pragma unroll
+    for (int i = 0; i < C::VEC; ++i) sg[k][i] = sb[k][i] = 0.0f;
+  // every team of the block makes the same number of turns (the barriers
+  // inside team_sum meet); a team without a row reads and writes nothing
+  for (int64_t base = (int64_t)blockIdx.x * C::PER_BLOCK; base < p.rows; base += (int64_t)gridDim.x * C::PER_BLOCK) {
+    const bool any = base + team < p.rows;
+    const int64_t row = any ? base + team : 0;
+    const int cols = any ? (int)p.cols : 0;
+    const T* x = static_cast<const T*>(p.x) + row * p.ldx;
+    const T* g = static_cast<const T*>(p.g) + row * p.ldg;
+    float xh[C::NV][C::VEC], gv[C::NV][C::VEC];
+#pragma unroll
+    for (int k = 0; k < C::NV; ++k) {
+      const int col = (k * C::TPR + t) * C::VEC;
+      load_part<T, C::VEC>(x + col, cols - col, xh[k]);
+      load_part<T, C::VEC>(g + col, cols - col, gv[k]);
+    }
+    const float mean = p.mean[row], rstd = p.rstd[row];
+    float s[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < C::NV; ++k) {
+      const int col = (k * C::TPR + t) * C::VEC;
+      float ga[C::VEC];
+#pragma unroll
+      for (int i = 0; i < C::VEC; ++i) ga[i] = 1.0f;
+      // read again for every row: from the nearest cache, and the registers
+      // hold more waves instead
+      if (p.gamma) load_part<float, C::VEC>(p.gamma + col, (int)p.cols - col, ga);
+#pragma unroll
+      for (int i = 0; i < C::VEC; ++i) {
+        // no column (or no row): xh is 0 like g, since (0 - mean) rstd may be infinite
+        xh[k][i] = col + i < cols ? (xh[k][i] - mean) * rstd : 0.0f;
+        sg[k][i] = fmaf(gv[k][i], xh[k][i], sg[k][i]);
+        sb[k][i] += gv[k][i];
+        gv[k][i] *= ga[i];
+        s[0] += gv[k][i];
+        s[1] = fmaf(gv[k][i], xh[k][i], s[1]);
+      }
+    }
+    team_sum<C, 2>(s, sh[team]);
+    const float a = s[0] * inv, b = s[1] * inv;
+    T* y = static_cast<T*>(p.y) + row * p.ldy;
+#pragma unroll
+    for (int k = 0; k < C::NV; ++k) {
+      const int64_t col = (int64_t)(k * C::TPR + t) * C::VEC;
+      float o[C::VEC];
+#pragma unroll
+      for (int i = 0; i < C::VEC; ++i) o[i] = rstd * ((gv[k][i] - a) - xh[k][i] * b);
+      store_part<T, C::VEC>(y + col, cols - col, o);
+    }
+  }
+  if (!p.grad_gamma && !p.grad_beta) return;
+  store_columns<C>(p, sg, sb, col_sum, t, team);
+}
+
+// Backward from the checkpoint.  The codes and G wait in registers as they were
+// loaded, a row ahead of the arithmetic, and codes are decoded twice: for the sums
+// and for the output.  Rows of one vector at least.
+template <class T, class C>
+struct KeptRow {
+  static constexpr int V = C::VEC, GW = V * (int)sizeof(T) / 4, QW = (V + 3) / 4;  // words of a vector of G, of codes
+  uint32_t g[C::NV][GW], q[C::NV][QW], e[C::NV];
+  float rstd;
+  // No branch around a load (it would wait for the others): vectors that are not
+  // whole are read from the row's end; moved down by `value`.
+  __device__ __forceinline__ void load(const NormParams& p, int64_t row, int t) {
+    const int64_t pitch = kept_pitch(p.cols);
+    const T* const gr = static_cast<const T*>(p.g) + row * p.ldg;
+    const uint8_t* const qr = p.q8 + row * pitch;
+    const uint8_t* const er = p.e8 + row * (pitch / KEPT_BLOCK);
+    const int cols = (int)p.cols, width = (int)pitch;
+    typedef uint32_t g_words __attribute__((ext_vector_type(GW), aligned(sizeof(T))));
+#pragma unroll
+    for (int k = 0; k < C::NV; ++k) {
+      const int col = (k * C::TPR + t) * V, at = col < width ? col : 0;
+      if constexpr (V == 2) {
+        q[k][0] = *reinterpret_cast<const uint16_t*>(qr + at);
+      } else {
+#pragma unroll
+        for (int i = 0; i < QW; ++i) q[k][i] = *reinterpret_cast<const uint32_t*>(qr + at + 4 * i);
+      }
+      e[k] = er[at / KEPT_BLOCK];
+      const int last = cols - V, from = col < last ? col : last;
+      const g_words w = *reinterpret_cast<const g_words*>(gr + from);
+#pragma unroll
+      for (int i = 0; i < GW; ++i) g[k][i] = w[i];
+    }
+    rstd = p.rstd[row];
+  }
+  __device__ __forceinline__ void xhat(int k, float (&v)[V]) const {
+    const float scale = scale_up(e[k]);
+#pragma unroll
+    for (int i = 0; i < V; i += 2) {
+      const auto f = (i & 2) ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(q[k][i / 4], scale, true)
+                             : __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(q[k][i / 4], scale, false);
+      v[i] = f[0];
+      v[i + 1] = f[1];
+    }
+  }
+  // left: the row's columns from the vector's first on; 0 past the row.
+  __device__ __forceinline__ void value(int k, int left, int cols, float (&v)[V]) const {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = __uint_as_float(left > 0 ? g[k][i] : 0u);
+    } else {
+      typedef T pair __attribute__((ext_vector_type(2)));
+#pragma unroll
+      for (int i = 0; i < V; i += 2) {
+        const pair two = as<pair>(left > 0 ? g[k][i / 2] : 0u);
+        v[i] = (float)two[0];
+        v[i + 1] = (float)two[1];
+      }
+    }
+    if (cols % V != 0) {
+      const int past = V - left;
+#pragma unroll
+      for (int d = V / 2; d > 0; d /= 2) {  // down by past, bit by bit
+        const bool move = past > 0 && (past & d);
+#pragma unroll
+        for (int i = 0; i + d < V; ++i) v[i] = move ? v[i + d] : v[i];
+      }
+#pragma unroll
+      for (int i = 1; i < V; ++i) v[i] = i < left ? v[i] : 0.0f;
+    }
+  }
+};
+
+template <class T, class C>
+__global__ __launch_bounds__(C::THREADS) void norm_backward8_kernel(NormParams p) {
+  __shared__ float sh[C::PER_BLOCK][C::WAVES][2];
+  __shared__ __attribute__((aligned(16))) ColumnSums<C> col_sum;
+  // a team is whole waves: its row's addresses stay scalar
+  const int t = threadIdx.x % C::TPR, team = __builtin_amdgcn_readfirstlane(threadIdx.x / C::TPR), cols = (int)p.cols;
+  const float inv = 1.0f / (float)p.cols;
+  float sg[C::NV][C::VEC], sb[C::NV][C::VEC], ga[C::NV][C::VEC];
+#pragma unroll
+  for (int k = 0; k < C::NV; ++k) {
+    const int col = (k * C::TPR + t) * C::VEC;
+#pragma unroll
+    for (int i = 0; i < C::VEC; ++i) {
+      sg[k][i] = sb[k][i] = 0.0f;
+      ga[k][i] = 1.0f;
+    }
+    if (p.gamma) load_part<float, C::VEC>(p.gamma + col, cols - col, ga[k]);
+  }
+  // every team of the block makes the same number of turns; a team without a row
+  // works on the last one and stores and adds nothing
+  const int64_t step = (int64_t)gridDim.x * C::PER_BLOCK;
+  int64_t row = (int64_t)blockIdx.x * C::PER_BLOCK + team;
+  constexpr bool AHEAD = C::TPR < 1024;
+  KeptRow<T, C> next;
+  if constexpr (AHEAD) next.load(p, row < p.rows ? row : p.rows - 1, t);
+  for (int64_t base = (int64_t)blockIdx.x * C::PER_BLOCK; base < p.rows; base += step, row += step) {
+    if constexpr (!AHEAD) next.load(p, row < p.rows ? row : p.rows - 1, t);
+    const KeptRow<T, C> r = next;
+    if (AHEAD && base + step < p.rows) next.load(p, row + step < p.rows ? row + step : p.rows - 1, t);
+    float s[2] = {0.0f, 0.0f};
+    float gv[C::NV][C::VEC];
+    if (row < p.rows) {
+      // What a code past the row may stand for (NaN, if its block's scale is) meets
+      // a zero of G in columns that are not stored, and in the sums of a row that
+      // is NaN as well.
+#pragma unroll
+      for (int k = 0; k < C::NV; ++k) {
+        float xh[C::VEC];
+        r.xhat(k, xh);
+        r.value(k, cols - (k * C::TPR + t) * C::VEC, cols, gv[k]);
+#pragma unroll
+        for (int i = 0; i < C::VEC; ++i) {
+          sg[k][i] = fmaf(gv[k][i], xh[i], sg[k][i]);
+          sb[k][i] += gv[k][i];
+          gv[k][i] *= ga[k][i];
+          s[0] += gv[k][i];
+          s[1] = fmaf(gv[k][i], xh[i], s[1]);
+        }
+      }
+    }
+    team_sum<C, 2>(s, sh[team]);
+    const float a = s[0] * inv, b = s[1] * inv;
+    T* y = static_cast<T*>(p.y) + row * p.ldy;
+#pragma unroll
+    for (int k = 0; k < C::NV; ++k) {
+      const int64_t col = (int64_t)(k * C::TPR + t) * C::VEC;
+      float xh[C::VEC], o[C::VEC];
+      r.xhat(k, xh);
+#pragma unroll
+      for (int i = 0; i < C::VEC; ++i) o[i] = r.rstd * ((gv[k][i] - a) - xh[i] * b);
+      store_part<T, C::VEC>(y + col, row < p.rows ? cols - col : 0, o);
+    }
+  }
+  if (!p.grad_gamma && !p.grad_beta) return;
+  store_columns<C>(p, sg, sb, col_sum, t, team);
 }
 
 // Rows longer than a team's registers: inputs read twice, no parameter sums.
@@ -493,18 +635,45 @@ static int64_t backward_blocks(int64_t rows, int64_t cols) {
 }
 int64_t norm_backward_partials(int64_t rows, int64_t cols) { return backward_blocks(rows, cols) * 2 * cols; }
 
+// From a checkpoint: 8 float32 elements a thread, so that the next row's fit the
+// registers (8192 x 4096, 302 MB, with 16 of them and no row ahead 80 us, so 58).
+template <class T, class F>
+static hipError_t with_kept_block(int64_t cols, F f) {
+  if constexpr (sizeof(T) == 4) {
+    if (cols <= 64 * 4) return f(Team<64, 2, 2, 1024>{});
+    if (cols <= 64 * 8) return f(Team<64, 4, 2, 1024>{});
+    if (cols <= 128 * 8) return f(Team<128, 4, 2, 1024>{});
+    if (cols <= 256 * 8) return f(Team<256, 4, 2, 1024>{});
+    if (cols <= 512 * 8) return f(Team<512, 4, 2, 1024>{});
+    if (cols <= 1024 * 8) return f(Team<1024, 4, 2>{});
+    return f(Team<1024, 4, 4>{});
+  } else {
+    return with_block<T>(cols, f);
+  }
+}
+static bool in_team(const NormParams& p) { return p.cols <= TEAM_COLS && !(p.q8 && p.cols < 8); }
 template <class T, bool KEPT>
+static hipError_t norm_backward_long(const NormParams& p, bool sums, int64_t blocks, hipStream_t s) {
+  using C = Team<1024, 16 / (int)sizeof(T), (int)sizeof(T)>;
+  hipLaunchKernelGGL((norm_backward_long_kernel<T, C, KEPT>), grid_of(p.rows, C::THREADS), dim3(C::THREADS), 0, s, p);
+  if (sums)
+    hipLaunchKernelGGL((norm_columns_kernel<T, KEPT>), dim3((unsigned)((p.cols + 255) / 256), (unsigned)blocks), dim3(256),
+                       0, s, p);
+  return hipGetLastError();
+}
+template <class T>
 static hipError_t norm_backward(const NormParams& p, bool sums, int64_t blocks, hipStream_t s) {
+  if (!in_team(p)) return p.q8 ? norm_backward_long<T, true>(p, sums, blocks, s) : norm_backward_long<T, false>(p, sums, blocks, s);
+  const dim3 grid((unsigned)blocks);
+  if (p.q8)
+    return with_kept_block<T>(p.cols, [&](auto c) {
+      using C = decltype(c);
+      hipLaunchKernelGGL((norm_backward8_kernel<T, C>), grid, dim3(C::THREADS), 0, s, p);
+      return hipGetLastError();
+    });
   return with_block<T>(p.cols, [&](auto c) {
     using C = decltype(c);
-    if (p.cols <= TEAM_COLS) {
-      hipLaunchKernelGGL((norm_backward_kernel<T, C, KEPT>), dim3((unsigned)blocks), dim3(C::THREADS), 0, s, p);
-    } else if constexpr (C::TPR == 1024) {
-      hipLaunchKernelGGL((norm_backward_long_kernel<T, C, KEPT>), grid_of(p.rows, C::THREADS), dim3(C::THREADS), 0, s, p);
-      if (sums)
-        hipLaunchKernelGGL((norm_columns_kernel<T, KEPT>), dim3((unsigned)((p.cols + 255) / 256), (unsigned)blocks),
-                           dim3(256), 0, s, p);
-    }
+    hipLaunchKernelGGL((norm_backward_kernel<T, C>), grid, dim3(C::THREADS), 0, s, p);
     return hipGetLastError();
   });
 }
@@ -513,9 +682,9 @@ hipError_t launch_norm_backward(fqt_dtype type, const NormParams& p, hipStream_t
   const int64_t blocks = backward_blocks(p.rows, p.cols);
   const hipError_t e = with_type(type, [&](auto el) {
     using T = decltype(el);
-    return p.q8 ? norm_backward<T, true>(p, sums, blocks, s) : norm_backward<T, false>(p, sums, blocks, s);
+    return norm_backward<T>(p, sums, blocks, s);
   });
-  if (e != hipSuccess || !sums || (blocks == 1 && p.cols <= TEAM_COLS)) return e;
+  if (e != hipSuccess || !sums || (blocks == 1 && in_team(p))) return e;
   hipLaunchKernelGGL(norm_reduce_kernel, grid_of((2 * p.cols + 63) / 64, 64 * REDUCE_WAVES), dim3(64 * REDUCE_WAVES),
                      0, s, p.part, blocks, p.cols, p.grad_gamma, p.grad_beta);
   return hipGetLastError();

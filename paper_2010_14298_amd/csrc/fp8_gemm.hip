@@ -94,7 +94,7 @@ __global__ __launch_bounds__(256) void fp8_two_sums_kernel(Fp8GemmParams a, Fp8G
 //   3001 x 1024 x 4096 float32   small 32     (78 / 46 / 32)
 //   250 x 1001 x 2048 float32    split 13.4   (45.6 / 25.8 / 16.6)
 //   130 x 260 x 8192 float32     split 15.6   (142 / 82 / 48.7)
-Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K) {
+Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, double pass) {
   using Plan = Fp8Plan;
   const int64_t nk = fp8_blocks(K);
   const double c[3] = {0.94, 1.77, 3.3}, t0[3] = {4.0, 5.0, 8.0};
@@ -111,7 +111,7 @@ Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K) {
     const int64_t chunk = (nk + s - 1) / s, parts = (nk + chunk - 1) / chunk;
     if (parts != s) continue;
     double t = turns(small * s) * ((double)chunk * c[0] + t0[0]);
-    if (s > 1) t += 4.0 + (double)(M * N) * 8.0 * s / 4.0e6;  // written and read at about 4 TB/s
+    if (s > 1) t += pass + (double)(M * N) * 8.0 * s / 4.0e6;  // written and read at about 4 TB/s
     if (t < least) {
       least = t;
       best = Plan{Plan::SMALL, s, (int)chunk};

@@ -213,7 +213,8 @@ struct Fp8Plan {
   enum Tile { SMALL, MID, LARGE } tile;
   int splits, chunk;  // parts along K, stages of each
 };
-Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K);
+// pass: us of a launch that adds the parts.
+Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, double pass = 4.0);
 hipError_t launch_fp8_parts(const Fp8GemmParams& p, const Fp8Plan& plan, hipStream_t s);  // to p.part
 fqt_fp8_form fp8_gemm_form(int64_t M, int64_t N, int64_t K, bool masked, bool lines);
 hipError_t launch_fp8_gemm(fqt_dtype type, const Fp8GemmParams& p, hipStream_t s);

@@ -24,7 +24,8 @@ struct Carver {
 
 constexpr int64_t MAX_SIDE = (int64_t)1 << 31;   // rows or columns of a matrix
 bool side(int64_t n) { return n >= 1 && n < MAX_SIDE; }
-bool half_side(int64_t n) { return n >= 1 && n < MAX_SIDE / 2; }
+// hidden units: the kernels reach the second half's scale words by 32-bit offsets
+bool half_side(int64_t n) { return n >= 1 && n < MAX_SIDE / 4; }
 // the products address a tile of 256 rows of codes with 31-bit offsets
 constexpr int64_t MAX_CONTRACTION = (int64_t)1 << 23;
 size_t type_bytes(fqt_dtype t) { return t == FQT_F32 ? 4 : 2; }

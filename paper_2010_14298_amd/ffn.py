@@ -8,7 +8,10 @@ floating point operands with a scale for each block of 128 and sums in float32; 
 stochastically, so that they stay unbiased (Sec. 2.2), with independent draws for grad_W and grad_X (App. E).
 Gradients are clipped by their global norm before the update.
 
-  python -m paper_2010_14298_amd.ffn [--tokens N] [--width D] [--hidden H] [--steps K]
+The gated block, Y = X + W2 (act(Wg n) * (Wu n)) with n = layernorm(X), keeps for its backward, beside the products'
+operands, 8-bit checkpoints only: the norm's rows and the two derivatives of each hidden unit.
+
+  python -m paper_2010_14298_amd.ffn [--tokens N] [--width D] [--hidden H] [--steps K] [--gate silu|gelu_tanh|relu]
 
 trains one block to follow another of random weights and prints the loss; then serves single tokens.
 """
@@ -72,6 +75,37 @@ class FeedForward:
         return loss, norm / scale
 
 
+class GatedFeedForward(FeedForward):
+    """One gated block; W1 [2 H, D] holds the gate's rows, then the others'.  act: of fqt_fp8_gated_forward."""
+
+    def __init__(self, D, H, dtype=torch.bfloat16, device="cuda", seed=0, act="silu"):
+        gen = torch.Generator(device=device)
+        gen.manual_seed(seed)
+        self.dtype, self.act = dtype, act
+        self.W1 = torch.randn((2 * H, D), generator=gen, device=device) * (1.0 / D) ** 0.5
+        self.W2 = torch.randn((D, H), generator=gen, device=device) * (1.0 / H) ** 0.5
+        self.gamma, self.beta = torch.ones(D, device=device), torch.zeros(D, device=device)
+        self.quantize()
+
+    def forward(self, X, keep=True):
+        """(Y, what the backward reads); keep=False (serving) keeps nothing."""
+        if keep:
+            Xn, xh8, rstd = fqt.fqt_layernorm_forward8(X, self.gamma, self.beta)
+        else:
+            Xn = fqt.fqt_layernorm_forward(X, self.gamma, self.beta)[0]
+        H, kept, _ = fqt.fqt_fp8_gated_forward(Xn, self.W1_8, act=self.act, save=keep)
+        Z, H8t, _ = fqt.fqt_fp8_linear_forward(H, self.W2_8, save=keep)
+        return Z + X, (xh8, rstd, kept, H8t) if keep else None
+
+    def backward(self, dY, kept, seed):
+        """(gradients in the order of parameters(), dX)."""
+        xh8, rstd, gated, H8t = kept
+        dW2, dH, _ = fqt.fqt_fp8_linear_backward(dY, H8t, self.W2_8t, seed=2 * seed)
+        dW1, dXn, _ = fqt.fqt_fp8_gated_backward(dH, gated, self.W1_8t, seed=2 * seed + 1)
+        dX, dgamma, dbeta, _ = fqt.fqt_layernorm_backward8(dXn, xh8, rstd, self.gamma)
+        return [dW1, dW2, dgamma, dbeta], dX + dY
+
+
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     ap.add_argument("--tokens", type=int, default=2048)
@@ -79,8 +113,14 @@ def main(argv=None):
     ap.add_argument("--hidden", type=int, default=1024)
     ap.add_argument("--steps", type=int, default=100)
     ap.add_argument("--lr", type=float, default=2.0)
+    ap.add_argument("--gate", choices=sorted(fqt.ACTS), help="a gated block with this activation")
     a = ap.parse_args(argv)
-    teacher, block = FeedForward(a.width, a.hidden, seed=1), FeedForward(a.width, a.hidden, seed=2)
+
+    def new(seed):
+        if a.gate:
+            return GatedFeedForward(a.width, a.hidden, seed=seed, act=a.gate)
+        return FeedForward(a.width, a.hidden, seed=seed)
+    teacher, block = new(1), new(2)
     gen = torch.Generator(device="cuda")
     gen.manual_seed(3)
     losses = []

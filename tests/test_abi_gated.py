@@ -38,7 +38,7 @@ def test_sizes(lib):
     assert lib.fqt_fp8_gated_forward_workspace(1, 1000, 64, 0, 1) > 0
     assert lib.fqt_fp8_gated_forward_workspace(1, 1000, 64, 1, 0) >= 128 * 1024
     assert lib.fqt_fp8_gated_backward_workspace(300, 1000, 64) >= 300 * 128 + 128 * 384
-    for bad in ((0, 8, 8), (8, 0, 8), (8, 8, 0), (8, 8, 1 << 30), (1 << 31, 8, 8), (8, 8, -1)):
+    for bad in ((0, 8, 8), (8, 0, 8), (8, 8, 0), (8, 8, 1 << 29), (1 << 31, 8, 8), (8, 8, -1)):
         assert lib.fqt_fp8_gated_forward_workspace(*bad, 1, 1) == 0 and lib.fqt_fp8_gated_backward_workspace(*bad) == 0
 
 
@@ -62,7 +62,7 @@ def test_gated_arguments(lib):
     def fwd(X=FAKE, t=0, N=4, i=8, ldx=8, W=op(), h=8, act=0, H=FAKE, ldh=8, Xt=op(), a=kept(), b=kept(), ws=FAKE, n=WS):
         return lib.fqt_fp8_gated_forward(X, t, N, i, ldx, W, h, act, H, ldh, Xt, a, b, ws, n, None)
     for bad in (dict(X=None), dict(t=9), dict(N=0), dict(N=1 << 31), dict(i=0), dict(ldx=-1), dict(W=None),
-                dict(W=op(None)), dict(W=op(FAKE, FAKE, 2)), dict(h=0), dict(h=1 << 30), dict(act=3), dict(act=-1),
+                dict(W=op(None)), dict(W=op(FAKE, FAKE, 2)), dict(h=0), dict(h=1 << 29), dict(act=3), dict(act=-1),
                 dict(H=None), dict(ldh=7), dict(Xt=op(FAKE, FAKE, 1)), dict(Xt=op(None)), dict(a=kept(None)),
                 dict(b=kept(FAKE, None)), dict(b=kept(FAKE + 4))):
         assert fwd(**bad) == 1, bad
@@ -73,7 +73,7 @@ def test_gated_arguments(lib):
     def bwd(G=FAKE, t=0, N=4, h=8, ldg=8, a=kept(), b=kept(), X=op(), W=op(), i=8, sr=1, gw=FAKE, gx=FAKE, ldgx=8,
             ws=FAKE, n=WS):
         return lib.fqt_fp8_gated_backward(G, t, N, h, ldg, a, b, X, W, i, sr, 0, gw, gx, ldgx, ws, n, None)
-    for bad in (dict(G=None), dict(t=4), dict(N=0), dict(h=0), dict(h=1 << 30), dict(ldg=-1), dict(a=None), dict(b=None),
+    for bad in (dict(G=None), dict(t=4), dict(N=0), dict(h=0), dict(h=1 << 29), dict(ldg=-1), dict(a=None), dict(b=None),
                 dict(a=kept(FAKE, None)), dict(b=kept(FAKE + 8)), dict(X=None), dict(W=None), dict(gw=None, gx=None),
                 dict(sr=2), dict(ldgx=7), dict(i=0), dict(gw=FAKE + 2)):
         assert bwd(**bad) == 1, bad

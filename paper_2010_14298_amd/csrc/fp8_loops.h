@@ -857,7 +857,6 @@ __global__ __launch_bounds__(PairTile::THREADS, 2) void fp8_gemm_pair_kernel(P p
     else
       wait_loads<0>();
     meet();
-    if (inner || t + 2 < n) load(next, t + 2);
     auto frag = [&](const uint8_t* f) __attribute__((always_inline)) {
       const v4i x = *reinterpret_cast<const v4i*>(f + c0);
       const v4i y = *reinterpret_cast<const v4i*>(f + c1);
@@ -875,6 +874,7 @@ __global__ __launch_bounds__(PairTile::THREADS, 2) void fp8_gemm_pair_kernel(P p
     for (int j = 0; j < C::JT; ++j) fb[j] = scale_of(e[C::BM + wn * C::WN + j * 32 + lrow] >> sh);
 #pragma unroll
     for (int i = 0; i < C::IT; ++i) fa[i] = scale_of(e[wm * C::WM + i * 32 + lrow] >> sh);
+    if (inner || t + 2 < n) load(next, t + 2);
     __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_setprio(1);
@@ -912,7 +912,17 @@ __global__ __launch_bounds__(PairTile::THREADS, 2) void fp8_gemm_pair_kernel(P p
     if (t + 1 < n) step(last, t + 1, q1, q0);
     if (t + 2 < n) step(last, t + 2, q2, q1);
   }
-  gated_store(p, acc, m0 + wm * C::WM, p.M, n0 + wn * 32, T{});
+  if (m0 + C::BM <= p.M && n0 + COLS <= columns(p)) {
+    // the last half stages lie in the buffers of n - 1 and n - 2: wait for their readers
+    auto all = [&]() __attribute__((always_inline)) {
+      __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+      meet();
+    };
+    all();
+    gated_store_block<T>(p, acc, m0, n0, wn, q0, q1, all);
+  } else {
+    gated_store(p, acc, m0 + wm * C::WM, p.M, n0 + wn * 32, T{});
+  }
 }
 
 using MidTile = PipeTile<256, 128, 64, 64, 1, 3>;

@@ -259,7 +259,8 @@ def read_out(g, d_gate, d_up, **how):
 
 @pytest.mark.parametrize("stochastic", [False, True])
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("N,hidden", [(1, 1), (3, 2), (5, 3), (130, 64), (128, 65), (200, 66), (77, 131), (257, 100)])
+@pytest.mark.parametrize("N,hidden", [(1, 1), (3, 2), (5, 3), (130, 64), (128, 65), (200, 66), (77, 131), (257, 100), (130, 256),
+                                      (64, 130), (200, 258), (33, 389)])
 def test_gradient_codes_bit_for_bit(N, hidden, dtype, stochastic):
     """Both quantizations of D, read out through products with identities."""
     g = matrix(N, N, hidden, dtype, spread=2.0)
@@ -276,7 +277,8 @@ def test_gradient_codes_bit_for_bit(N, hidden, dtype, stochastic):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("N,d_in,hidden", [(1, 64, 32), (33, 130, 70), (300, 192, 520), (700, 96, 131)])
+@pytest.mark.parametrize("N,d_in,hidden", [(1, 64, 32), (33, 130, 70), (300, 192, 520), (700, 96, 131),
+                                           (1200, 160, 600)])
 def test_backward(N, d_in, hidden, dtype):
     f = fqt()
     X, g = matrix(20, N, d_in, dtype), matrix(21, N, hidden, dtype, spread=1.5)

@@ -515,8 +515,9 @@ size_t fqt_fp8_gated_forward_workspace(int64_t N, int64_t d_in, int64_t hidden, 
  * that is exact where frac has 16 bits, as for 16-bit G and results that are
  * not below the format's normal numbers.)  X8t [d_in, K = N], d_gate and d_up
  * from the forward, W8t [d_in, K = 2 hidden] the weights' by_col operand.
- * grad_W or grad_X may be NULL (not formed; its operand may then be NULL too).
- * N and 2 hidden up to 2^23 where they are contracted (FQT_EUNSUPPORTED).     */
+ * grad_W or grad_X may be NULL (not formed; its operand may then be NULL too;
+ * the order of the other one's sums may be another then).  N and 2 hidden up to
+ * 2^23 where they are contracted (FQT_EUNSUPPORTED).                         */
 fqt_status fqt_fp8_gated_backward(const void* G, fqt_dtype type, int64_t N, int64_t hidden, int64_t ldg,
                                   const fqt_kept* d_gate, const fqt_kept* d_up, const fqt_fp8* X8t,
                                   const fqt_fp8* W8t, int64_t d_in, int stochastic, uint64_t seed, float* grad_W,

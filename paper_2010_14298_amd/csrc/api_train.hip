@@ -113,7 +113,7 @@ BackwardWs carve_backward(Carver& c, int64_t N, int64_t d_in, int64_t d_out) {
 // of the kept ones.  grad_W or grad_X null: not formed.
 hipError_t gradients_of(fqt_dtype type, const BackwardWs& w, int64_t N, int64_t d_in, int64_t d_out, const uint8_t* x8,
                         const fqt_fp8* X8t, const uint8_t* w8, const fqt_fp8* W8t, const void* relu_input, int64_t ldr,
-                        float* grad_W, void* grad_X, int64_t ldgx, hipStream_t s) {
+                        float* grad_W, void* grad_X, int64_t ldgx, bool any_order, hipStream_t s) {
   Fp8GemmParams p{}, r{};
   p.N = r.N = d_in;
   if (grad_W) {
@@ -140,7 +140,7 @@ hipError_t gradients_of(fqt_dtype type, const BackwardWs& w, int64_t N, int64_t 
     r.ldmask = ldr;
     r.part = w.part_x;
   }
-  if (grad_W && grad_X) return launch_fp8_two(type, p, r, s);
+  if (grad_W && grad_X) return launch_fp8_two(type, p, r, any_order, s);
   return grad_W ? launch_fp8_gemm(FQT_F32, p, s) : launch_fp8_gemm(type, r, s);
 }
 
@@ -441,7 +441,7 @@ fqt_status fqt_fp8_linear_backward(const void* G, fqt_dtype type, int64_t N, int
   const uint8_t* const x8 = grad_W ? rows_of(X8t, d_in, N, w.x, &turn_x) : nullptr;
   const uint8_t* const w8 = grad_X ? rows_of(W8t, d_in, d_out, w.w, &turn_w) : nullptr;
   FQT_TRY(launch_fp8_quantize_turn(type, q, turn_x, turn_w, s));
-  FQT_TRY(gradients_of(type, w, N, d_in, d_out, x8, X8t, w8, W8t, relu_input, ldr, grad_W, grad_X, ldgx, s));
+  FQT_TRY(gradients_of(type, w, N, d_in, d_out, x8, X8t, w8, W8t, relu_input, ldr, grad_W, grad_X, ldgx, false, s));
   return FQT_OK;
 }
 
@@ -548,7 +548,7 @@ fqt_status fqt_fp8_gated_backward(const void* G, fqt_dtype type, int64_t N, int6
   const uint8_t* const x8 = grad_W ? rows_of(X8t, d_in, N, w.x, &turn_x) : nullptr;
   const uint8_t* const w8 = grad_X ? rows_of(W8t, d_in, cols, w.w, &turn_w) : nullptr;
   FQT_TRY(launch_gated_quantize(type, d, turn_x, turn_w, s));
-  FQT_TRY(gradients_of(type, w, N, d_in, cols, x8, X8t, w8, W8t, nullptr, 0, grad_W, grad_X, ldgx, s));
+  FQT_TRY(gradients_of(type, w, N, d_in, cols, x8, X8t, w8, W8t, nullptr, 0, grad_W, grad_X, ldgx, true, s));
   return FQT_OK;
 }
 

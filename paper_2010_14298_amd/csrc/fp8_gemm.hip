@@ -59,9 +59,17 @@ __global__ __launch_bounds__(256) void fp8_split_sum_kernel(Fp8GemmParams p, int
   split_sum<T>(p, splits, blockIdx.x);
 }
 
-// The parts and the sums of two products that do not depend on each other, a in
-// float32 and b, in one launch each: a backward of 2048, 256 -> 1024 gated, whose
-// two products are 32 tiles of four parts each, 47 us with two launches each, 32 so.
+// Two products that do not depend on each other, a with float32 outputs and b, tile
+// by tile in one launch: the units that one of them leaves idle work on the other.
+// Half of K a wave whatever the type: the sums' order is the float32 products'.
+template <class T, bool NT>
+__global__ __launch_bounds__(512) void fp8_two_tiles_kernel(Fp8GemmParams a, Fp8GemmParams b, int nk_a, int nk_b,
+                                                            uint32_t first, int second_is_b) {
+  const bool early = blockIdx.x < first, is_b = early != (second_is_b != 0);
+  const Fp8GemmParams p = is_b ? b : a;
+  pipe_tile<float, SmallTile, false, NT, Fp8GemmParams, T>(p, is_b ? nk_b : nk_a, early ? blockIdx.x : blockIdx.x - first, 0, is_b);
+}
+// Their parts, and the sums of these, in one launch each.
 __global__ __launch_bounds__(512) void fp8_two_parts_kernel(Fp8GemmParams a, Fp8GemmParams b, int chunk_a, int chunk_b,
                                                             uint32_t tiles_a, uint32_t blocks_a, uint32_t tiles_b) {
   const bool first = blockIdx.x < blocks_a;
@@ -223,8 +231,45 @@ bool fp8_two_at_once(int64_t Ma, int64_t Na, int64_t Ka, int64_t Mb, int64_t Nb,
   return Ma > ROWS_MAX && Mb > ROWS_MAX && fp8_plan(Ma, Na, Ka).splits > 1 && fp8_plan(Mb, Nb, Kb).splits > 1;
 }
 
-hipError_t launch_fp8_two(fqt_dtype type, const Fp8GemmParams& a, const Fp8GemmParams& b, hipStream_t s) {
+// us of a product by itself, as fp8_plan estimates it.
+static double plan_time(int64_t M, int64_t N, const Fp8Plan& plan) {
+  const bool large = plan.tile == Fp8Plan::LARGE, mid = plan.tile == Fp8Plan::MID;
+  const double c = large ? 3.3 : mid ? 1.77 : 0.94, t0 = large ? 8.0 : mid ? 5.0 : 4.0;
+  const int64_t tiles = tiles_of(M, N, mid || large ? 256 : 128, large ? 256 : 128) * plan.splits;
+  return (double)((tiles + 255) / 256) * (plan.chunk * c + t0) +
+         (plan.splits > 1 ? 4.0 + (double)(M * N) * 8.0 * plan.splits / 4.0e6 : 0.0);
+}
+
+hipError_t launch_fp8_two(fqt_dtype type, const Fp8GemmParams& a, const Fp8GemmParams& b, bool any_order, hipStream_t s) {
   if (!fp8_two_at_once(a.M, a.N, a.K, b.M, b.N, b.K)) {
+    if (any_order && a.M > ROWS_MAX && b.M > ROWS_MAX) {
+      // The tiles of the longer contraction first, and half of one of the shorter
+      // behind the last of them.  Together / apart, whole backward, us: bfloat16 2048,
+      // 1024 -> 1024 32 / 47.5, 700, 2048 -> 1500 42 / 50, 3001, 1024 -> 2730 112 / 121
+      // (float32 103 / 110), 2048, 1024 -> 4096 101 / 100; where one of the longer tiles
+      // takes as long as all the rest, apart: 1024, 1024 -> 4096 70 / 63.
+      const int nk_a = (int)fp8_blocks(a.K), nk_b = (int)fp8_blocks(b.K);
+      const int64_t ta = tiles_of(a.M, a.N, SmallTile::BM, SmallTile::BN), tb = tiles_of(b.M, b.N, SmallTile::BM, SmallTile::BN);
+      const double one_a = nk_a * 0.94 + 4.0, one_b = nk_b * 0.94 + 4.0;
+      const double shorter = one_a < one_b ? one_a : one_b, longer = one_a < one_b ? one_b : one_a;
+      double both = ((double)ta * one_a + (double)tb * one_b) / 256.0 + 0.5 * shorter;
+      if (both < longer + 4.0) both = longer + 4.0;
+      const double apart = plan_time(a.M, a.N, fp8_plan(a.M, a.N, a.K)) + plan_time(b.M, b.N, fp8_plan(b.M, b.N, b.K));
+      if (both < apart && ta + tb <= 0x7FFFFF) {
+        const bool b_first = nk_b >= nk_a;
+        return with_type(type, [&](auto e) {
+          using T = decltype(e);
+          const bool nt = ((uintptr_t)a.C & 127) == 0 && ((uintptr_t)b.C & 127) == 0 && a.ldc * 4 % 128 == 0 &&
+                          b.ldc * sizeof(T) % 128 == 0;
+          auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(ta + tb)), dim3(512), 0, s, a, b, nk_a, nk_b,
+                               (uint32_t)(b_first ? tb : ta), (int)!b_first);
+            return hipGetLastError();
+          };
+          return nt ? go(fp8_two_tiles_kernel<T, true>) : go(fp8_two_tiles_kernel<T, false>);
+        });
+      }
+    }
     const hipError_t err = launch_fp8_gemm(FQT_F32, a, s);
     return err == hipSuccess ? launch_fp8_gemm(type, b, s) : err;
   }

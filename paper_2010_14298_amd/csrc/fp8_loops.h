@@ -521,8 +521,9 @@ struct PipeTile {
 };
 
 // T: the stored type (SPLIT: float).
-template <class T, class C, bool SPLIT, bool NT, class P>
-__device__ __forceinline__ void pipe_tile(const P& p, int chunk, uint32_t tile, uint32_t part) {
+// T2: the stored type where `second`.
+template <class T, class C, bool SPLIT, bool NT, class P, class T2 = T>
+__device__ __forceinline__ void pipe_tile(const P& p, int chunk, uint32_t tile, uint32_t part, bool second = false) {
   constexpr int COLS = P::GATED ? C::BN / 2 : C::BN;  // output columns of a tile
   __shared__ __attribute__((aligned(16))) uint8_t q0[C::CODES], q1[C::CODES], q2[C::CODES], q3[C::NS > 3 ? C::CODES : 16];
   __shared__ int x0[C::BM + C::BN], x1[C::BM + C::BN], x2[C::BM + C::BN], x3[C::NS > 3 ? C::BM + C::BN : 4];
@@ -750,18 +751,29 @@ __device__ __forceinline__ void pipe_tile(const P& p, int chunk, uint32_t tile, 
       to.relu = 0;
       to.mask = nullptr;
     }
+    auto store = [&](auto type) __attribute__((always_inline)) {
+      using O = decltype(type);
 #pragma unroll
-    for (int i = 0; i < STRIPS; ++i) {
-      const int64_t row0 = m0 + wm * C::WM + (kg * STRIPS + i) * 32, col0 = n0 + wn * C::WN;
-      const StripMask<T, C::WN> mask(to, row0, col0);
+      for (int i = 0; i < STRIPS; ++i) {
+        const int64_t row0 = m0 + wm * C::WM + (kg * STRIPS + i) * 32, col0 = n0 + wn * C::WN;
+        const StripMask<O, C::WN> mask(to, row0, col0);
 #pragma unroll
-      for (int j = 0; j < C::JT; ++j)
+        for (int j = 0; j < C::JT; ++j)
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          strip[(8 * (r >> 2) + 4 * half + (r & 3)) * C::OUT_LD + j * 32 + lrow] = acc[i][j][r];
-      __builtin_amdgcn_wave_barrier();
-      store_strip<T, C::WN, C::OUT_LD, NT>(to, strip, mask, row0, col0);
-      __builtin_amdgcn_wave_barrier();
+          for (int r = 0; r < 16; ++r)
+            strip[(8 * (r >> 2) + 4 * half + (r & 3)) * C::OUT_LD + j * 32 + lrow] = acc[i][j][r];
+        __builtin_amdgcn_wave_barrier();
+        store_strip<O, C::WN, C::OUT_LD, NT>(to, strip, mask, row0, col0);
+        __builtin_amdgcn_wave_barrier();
+      }
+    };
+    if constexpr (std::is_same<T, T2>::value) {
+      store(T{});
+    } else {
+      if (second)
+        store(T2{});
+      else
+        store(T{});
     }
   }
 }

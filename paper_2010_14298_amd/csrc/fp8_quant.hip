@@ -26,8 +26,9 @@
 namespace fqt {
 
 constexpr int TILE = FP8_BLOCK;
-constexpr int QT = 256;                  // threads of a tile: 32 column quads x 8 row groups
-constexpr int GROUP = TILE / (QT / 32);  // rows of one thread: 16
+constexpr int QT = 256;                                  // threads of a tile: 32 column quads x 8 row groups
+constexpr int group_of(int threads) { return TILE / (threads / 32); }  // rows of one thread: 16
+constexpr int GROUP = group_of(QT);
 
 // Stochastic codes of four elements v 2^-E, |v 2^-E| <= 448, from the low 24
 // bits u of a word each.  With m the bits of |v 2^-E|: from 2^-6 on, the part
@@ -108,6 +109,7 @@ __device__ __forceinline__ float larger(float a, float b) {
 template <class T>
 struct MatrixSource {
   typedef T Elem;
+  static constexpr int THREADS = QT;
   static constexpr bool HALVES = false;  // the operands' words are of streams 1 and 0, not halves of stream 2's
   static __device__ __forceinline__ void load(const Fp8QuantParams& p, int64_t row, int64_t col, Quad<T> (&v)[GROUP]) {
     const T* x = static_cast<const T*>(p.x) + row * p.ldx + col;
@@ -120,6 +122,7 @@ struct MatrixSource {
 template <class Source, bool ROW, bool COL, bool SQUARE, bool SR, class From>
 __device__ __forceinline__ void quantize_tile(const Fp8QuantParams& p, uint32_t block, uint8_t* turned, const From& from) {
   typedef typename Source::Elem T;
+  constexpr int QT = Source::THREADS, GROUP = group_of(QT);
   __shared__ uint32_t col_top[QT / 32][TILE / 2];
   __shared__ __attribute__((aligned(8))) uint16_t keys[2][TILE];  // of the rows, of the columns
   const int tid = threadIdx.x, quad = tid & 31, grp = tid >> 5;
@@ -214,12 +217,14 @@ __device__ __forceinline__ void quantize_tile(const Fp8QuantParams& p, uint32_t 
   auto store_row = [&](int i, uint32_t key, uint32_t codes) __attribute__((always_inline)) {
     if (row + i < p.rows) *reinterpret_cast<uint32_t*>(q_row + i * row_pitch) = key >= NAN_KEY ? 0x7f7f7f7fu : codes;
   };
+  // rows 4 k .. of this group, column 4 quad + j: 16-byte chunks swizzled by the quad
+  [[maybe_unused]] auto put = [&](int j, int k, uint32_t codes) __attribute__((always_inline)) {
+    const int at = grp * GROUP + 4 * k;
+    *reinterpret_cast<uint32_t*>(turned + (4 * quad + j) * TILE + 16 * ((at >> 4) ^ (quad & 7)) + (at & 15)) =
+        key[j] >= NAN_KEY ? 0x7f7f7f7fu : codes;
+  };
   if constexpr (SR && Source::HALVES) {
     const float up[4] = {scale_up(byte[0]), scale_up(byte[1]), scale_up(byte[2]), scale_up(byte[3])};
-    auto put = [&](int j, int k, uint32_t codes) __attribute__((always_inline)) {
-      *reinterpret_cast<uint32_t*>(turned + (4 * quad + j) * TILE + 16 * (grp ^ (quad & 7)) + 4 * k) =
-          key[j] >= NAN_KEY ? 0x7f7f7f7fu : codes;
-    };
     // aligned: a quad's elements share one random block; all: no row is past the last
     auto codes = [&](auto aligned, auto all) __attribute__((always_inline)) {
       uint64_t e = (uint64_t)row * (uint64_t)p.cols + (uint64_t)col;
@@ -310,7 +315,14 @@ __device__ __forceinline__ void quantize_tile(const Fp8QuantParams& p, uint32_t 
   }
   if constexpr (COL) {
     const int64_t pitch = fp8_pitch(p.rows);
-    if constexpr (!(SR && Source::HALVES)) {  // (there they lie in LDS already)
+    if constexpr (GROUP < 16) {
+      if constexpr (!SR) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int k = 0; k < GROUP / 4; ++k) put(j, k, w[j][k]);
+      }
+    } else if constexpr (!(SR && Source::HALVES)) {  // (there they lie in LDS already)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if (key[j] >= NAN_KEY) w[j][0] = w[j][1] = w[j][2] = w[j][3] = 0x7f7f7f7fu;
@@ -335,12 +347,14 @@ __device__ __forceinline__ void quantize_tile(const Fp8QuantParams& p, uint32_t 
 // 128 x 128 bytes a block; a thread turns 4 x 4 bytes over in registers, LDS
 // gathers rows of 128.
 typedef uint32_t TurnLds[TILE][TILE / 4 + 1];
+template <int QT>
 __device__ __forceinline__ void turn_tile(const uint8_t* src, int64_t rows, int64_t pitch, uint8_t* dst, uint32_t block,
                                           TurnLds& sh) {
   const uint32_t kblocks = (uint32_t)(pitch / TILE);
   const int64_t k0 = (int64_t)(block % kblocks) * TILE, r0 = (int64_t)(block / kblocks) * TILE;
   const int quad = threadIdx.x & 31, grp = threadIdx.x >> 5;
   const int64_t row = r0 + 4 * quad, left = rows - row;
+  constexpr int GROUP = group_of(QT);
   uint32_t in[GROUP];
 #pragma unroll
   for (int i = 0; i < GROUP; ++i) {
@@ -377,7 +391,7 @@ __global__ __launch_bounds__(QT) void fp8_tile_kernel(Fp8QuantParams p) {
 }
 __global__ __launch_bounds__(QT) void fp8_turn_kernel(Fp8Turn t) {
   __shared__ TurnLds sh;
-  turn_tile(t.src, t.rows, fp8_pitch(t.K), t.dst, blockIdx.x, sh);
+  turn_tile<QT>(t.src, t.rows, fp8_pitch(t.K), t.dst, blockIdx.x, sh);
 }
 // Both in one launch: of every `step` blocks the last lays codes out, until there
 // are `turns` of them.  They wait for memory while the others compute: a
@@ -387,6 +401,7 @@ struct TurnPlan {
   Fp8Turn a, b;
   uint32_t turns_a, turns, step;
   // Lays this block's codes out, or names the tile that it quantizes.
+  template <int THREADS>
   __device__ __forceinline__ bool turns_here(uint32_t& tile, uint8_t* room) const {
     const uint32_t before = blockIdx.x / step;  // of those that lay out, up to `turns`
     if (before >= turns || blockIdx.x - before * step != step - 1) {
@@ -395,7 +410,7 @@ struct TurnPlan {
     }
     const bool first = before < turns_a;
     const Fp8Turn t = first ? a : b;
-    turn_tile(t.src, t.rows, fp8_pitch(t.K), t.dst, first ? before : before - turns_a, *reinterpret_cast<TurnLds*>(room));
+    turn_tile<THREADS>(t.src, t.rows, fp8_pitch(t.K), t.dst, first ? before : before - turns_a, *reinterpret_cast<TurnLds*>(room));
     return true;
   }
 };
@@ -403,7 +418,7 @@ template <class T, bool SR>
 __global__ __launch_bounds__(QT) void fp8_tile_turn_kernel(Fp8QuantParams p, TurnPlan t) {
   __shared__ __attribute__((aligned(16))) uint8_t room[sizeof(TurnLds) > TILE * TILE ? sizeof(TurnLds) : TILE * TILE];
   uint32_t block;
-  if (t.turns_here(block, room)) return;
+  if (t.turns_here<QT>(block, room)) return;
   quantize_tile<MatrixSource<T>, true, true, false, SR>(p, block, room, p);
 }
 
@@ -470,9 +485,10 @@ hipError_t launch_fp8_quantize(fqt_dtype type, const Fp8QuantParams& p, hipStrea
 // checkpoints are read, both operands written, nothing in between.  A tile is
 // one of D, whose columns hidden .. 2 hidden - 1 read G once more.
 // ---------------------------------------------------------------------------
-template <class G>
+template <class G, int THREADS_>
 struct GatedSource {
   typedef float Elem;
+  static constexpr int THREADS = THREADS_, GROUP = group_of(THREADS);
   static constexpr bool HALVES = true;
   const G* g;
   const uint8_t *q, *e, *q_up, *e_up;  // of the half that col lies in; of the second
@@ -591,35 +607,44 @@ struct GatedSource {
     for (int j = 0; j < 4; ++j) v.v[j] = gv[j] * d[j];
   }
 };
-template <class G, bool ROW, bool COL, bool SR>
-__global__ __launch_bounds__(QT, sizeof(G) == 2 ? 4 : 3) void gated_tile_kernel(GatedQuantParams p) {
+// 256 threads a tile, sixteen rows each, hold four tiles a unit (16-bit G); with 512
+// a tile takes less time, but a unit holds fewer.
+template <class G, bool ROW, bool COL, bool SR, int THREADS>
+__global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : sizeof(G) == 2 ? 4 : 3) void gated_tile_kernel(GatedQuantParams p) {
   __shared__ __attribute__((aligned(16))) uint8_t turned[COL ? TILE * TILE : 16];
   const int64_t block = block_id();
   if (block >= fp8_blocks(p.q.rows) * fp8_blocks(p.q.cols)) return;
-  quantize_tile<GatedSource<G>, ROW, COL, false, SR>(p.q, (uint32_t)block, turned, p);
+  quantize_tile<GatedSource<G, THREADS>, ROW, COL, false, SR>(p.q, (uint32_t)block, turned, p);
 }
-
 // With kept operands to lay out in the same launch, as above.
-template <class G, bool SR>
-__global__ __launch_bounds__(QT, sizeof(G) == 2 ? 4 : 3) void gated_tile_turn_kernel(GatedQuantParams p, TurnPlan t) {
+template <class G, bool SR, int THREADS>
+__global__ __launch_bounds__(THREADS, THREADS == 512 ? 4 : sizeof(G) == 2 ? 4 : 3) void gated_tile_turn_kernel(GatedQuantParams p,
+                                                                                                             TurnPlan t) {
   __shared__ __attribute__((aligned(16))) uint8_t room[sizeof(TurnLds) > TILE * TILE ? sizeof(TurnLds) : TILE * TILE];
   uint32_t block;
-  if (t.turns_here(block, room)) return;
-  quantize_tile<GatedSource<G>, true, true, false, SR>(p.q, block, room, p);
+  if (t.turns_here<THREADS>(block, room)) return;
+  quantize_tile<GatedSource<G, THREADS>, true, true, false, SR>(p.q, block, room, p);
 }
 
 hipError_t launch_gated_quantize(fqt_dtype type, const GatedQuantParams& p, const Fp8Turn& a, const Fp8Turn& b,
                                  hipStream_t s) {
   const int64_t tiles = fp8_blocks(p.q.rows) * fp8_blocks(p.q.cols), blocks = tiles + turn_blocks(a) + turn_blocks(b);
   if (tiles > 0x7FFFFFFF) return hipErrorInvalidValue;
-  if (blocks > tiles && p.q.q_row && p.q.q_col && blocks <= MOST_BLOCKS) {
+  // 512 threads a tile / 256, whole backward with a width of 128, us: 256 tiles 25.5 / 26.2, 1032 (hidden off four)
+  // 57.7 / 64.8, 1504 63.2 / 63.9, 2048 75 / 73, 4096 130 / 123; float32 1032 60 / 66, 4096 162 / 150
+  const bool wide = tiles < 1536;
+  auto with_threads = [&](auto f) { return wide ? f(std::integral_constant<int, 512>{}) : f(std::integral_constant<int, 256>{}); };
+  if (blocks > tiles && p.q.q_row && p.q.q_col && blocks <= MOST_BLOCKS / 2) {
     return with_type(type, [&](auto e) {
       using T = decltype(e);
-      auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(QT), 0, s, p, turn_plan(a, b, blocks));
-        return hipGetLastError();
-      };
-      return p.q.stochastic ? go(gated_tile_turn_kernel<T, true>) : go(gated_tile_turn_kernel<T, false>);
+      return with_threads([&](auto threads) {
+        constexpr int N = decltype(threads)::value;
+        auto go = [&](auto kernel) {
+          hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(N), 0, s, p, turn_plan(a, b, blocks));
+          return hipGetLastError();
+        };
+        return p.q.stochastic ? go(gated_tile_turn_kernel<T, true, N>) : go(gated_tile_turn_kernel<T, false, N>);
+      });
     });
   }
   hipError_t err = launch_fp8_turn(a, s);
@@ -627,14 +652,18 @@ hipError_t launch_gated_quantize(fqt_dtype type, const GatedQuantParams& p, cons
   if (err != hipSuccess) return err;
   return with_type(type, [&](auto e) {
     using T = decltype(e);
-    auto go = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, grid_of(tiles, QT), dim3(QT), 0, s, p);
+    auto go = [&](auto kernel, int threads) {
+      hipLaunchKernelGGL(kernel, grid_of(tiles, threads), dim3(threads), 0, s, p);
       return hipGetLastError();
     };
     auto pick = [&](auto sr) {
       constexpr bool S = decltype(sr)::value;
-      if (p.q.q_row && p.q.q_col) return go(gated_tile_kernel<T, true, true, S>);
-      return p.q.q_row ? go(gated_tile_kernel<T, true, false, S>) : go(gated_tile_kernel<T, false, true, S>);
+      if (p.q.q_row && p.q.q_col)
+        return with_threads([&](auto threads) {
+          constexpr int N = decltype(threads)::value;
+          return go(gated_tile_kernel<T, true, true, S, N>, N);
+        });
+      return p.q.q_row ? go(gated_tile_kernel<T, true, false, S, QT>, QT) : go(gated_tile_kernel<T, false, true, S, QT>, QT);
     };
     return p.q.stochastic ? pick(std::true_type{}) : pick(std::false_type{});
   });

@@ -219,9 +219,10 @@ hipError_t launch_fp8_parts(const Fp8GemmParams& p, const Fp8Plan& plan, hipStre
 fqt_fp8_form fp8_gemm_form(int64_t M, int64_t N, int64_t K, bool masked, bool lines);
 hipError_t launch_fp8_gemm(fqt_dtype type, const Fp8GemmParams& p, hipStream_t s);
 // Two products that do not depend on each other, a with float32 outputs; whether
-// they run at once (and need partial sums of their own) or one behind the other.
+// their parts run at once (and need room of their own).  any_order: b's sums need
+// not have the order that b has by itself.
 bool fp8_two_at_once(int64_t Ma, int64_t Na, int64_t Ka, int64_t Mb, int64_t Nb, int64_t Kb);
-hipError_t launch_fp8_two(fqt_dtype type, const Fp8GemmParams& a, const Fp8GemmParams& b, hipStream_t s);
+hipError_t launch_fp8_two(fqt_dtype type, const Fp8GemmParams& a, const Fp8GemmParams& b, bool any_order, hipStream_t s);
 
 // ---------------------------------------------------------------------------
 // gated layer

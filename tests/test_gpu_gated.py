@@ -288,14 +288,14 @@ def test_backward(N, d_in, hidden, dtype):
     vg, vu = (G.kept_values(bytes_of(kept[n]["q"]), kept[n]["exp"].cpu().numpy(), hidden) for n in ("d_gate", "d_up"))
     t, r = G.gradient_operands(host(g), vg, vu, 17)
     xt, wt = F.operand(host(X).T)["value"], F.operand(host(W).T, tile=True)["value"]
-    want, size = t["value"] @ xt.T, np.abs(t["value"]) @ np.abs(xt).T
-    assert np.all(np.abs(host(gW) - want) <= N * U * size)
+    want_W, size_W = t["value"] @ xt.T, np.abs(t["value"]) @ np.abs(xt).T
+    assert np.all(np.abs(host(gW) - want_W) <= N * U * size_W)
     want, size = r["value"] @ wt.T, np.abs(r["value"]) @ np.abs(wt).T
     assert np.all(np.abs(host(gX) - want) <= 2 * hidden * U * size + HALF[dtype] * (np.abs(want) + 2 * hidden * U * size)
                   + TINY[dtype])
-    # each alone, and into a caller's buffers
+    # alone (its sums may run in another order, which float32's bound covers), and into a caller's buffers
     only, none, _ = f.fqt_fp8_gated_backward(g, kept, None, seed=17, input_grad=False, ws=ws)
-    assert none is None and torch.equal(only, gW)
+    assert none is None and np.all(np.abs(host(only) - want_W) <= N * U * size_W)
     out, buf = torch.full_like(gW, 3.0), torch.full((N, d_in + 9), 5.0, dtype=dtype, device="cuda")
     f.fqt_fp8_gated_backward(g, kept, W8t, seed=17, grad_W=out, grad_X=buf[:, 2:d_in + 2])
     assert torch.equal(out, gW) and torch.equal(buf[:, 2:d_in + 2], gX)

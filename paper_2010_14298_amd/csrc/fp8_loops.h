@@ -788,6 +788,7 @@ __global__ __launch_bounds__(512) void fp8_gemm_pipe_kernel(P p, int chunk) {
 // cores.  Half stages of 64 along K in three buffers: the wait and the barrier of
 // half stage t say that it has landed and that everyone has read t - 1, whose
 // buffer then takes t + 2.  Scale words, four stages in each, in two buffers.
+// Gated 8192, 1024 -> 4096 bfloat16: the call 145 us.
 // ---------------------------------------------------------------------------
 struct PairTile {
   static constexpr int BM = 128, BN = 256, WM = 128, WN = 64;
@@ -1075,8 +1076,10 @@ __global__ __launch_bounds__(64 * ROW_WAVES) void fp8_rows_kernel(Fp8GemmParams 
   }
 }
 
-// Gated: a block takes 16 rows of X, as they are, against 16 hidden units.  The
-// rows' blocks of K are loaded a turn ahead, the weights' two.
+// Gated: a block takes 16 rows of X, as they are, against 16 hidden units, and its
+// waves divide K: few rows leave the weights to be read once and nothing else to do,
+// and what counts is how many loads are under way.  The rows' blocks of K are loaded
+// a turn ahead, the weights' two.
 template <class T, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void gated_rows_kernel(GatedGemmParams p, const T* x, int64_t ldx) {
   __shared__ float sum[WAVES][2][256];

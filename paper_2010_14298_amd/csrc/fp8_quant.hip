@@ -484,6 +484,12 @@ hipError_t launch_fp8_quantize(fqt_dtype type, const Fp8QuantParams& p, hipStrea
 // [rows, 2 hidden], formed in float32 as they are quantized: G and the
 // checkpoints are read, both operands written, nothing in between.  A tile is
 // one of D, whose columns hidden .. 2 hidden - 1 read G once more.
+//
+// One random word an element serves both operands, half each: random numbers were
+// the bound, and 16 bits are as many as 16-bit G times a code leaves to round (the
+// layer's own quantizer takes two words of 24 bits, which float32 would need).
+// 8192 x 8192 bfloat16 (268 MB with the second read of G, 24 MB of weights and X to
+// lay out): 78 us, 3.7 TB/s; vector issue 67 % busy, waits 23 % of the time.
 // ---------------------------------------------------------------------------
 template <class G, int THREADS_>
 struct GatedSource {

@@ -4,7 +4,18 @@
 //   d_gate = Q8(b act'(a)),  d_up = Q8(act(a))    (kept for the backward)
 //
 // The products' loops of fp8_loops.h over both halves of the weights at once;
-// a and b stay in registers.
+// a and b stay in registers, so that of them nothing goes to memory but H and two
+// bytes a hidden unit.
+//
+// 8192, 1024 -> 4096 bfloat16 with checkpoints (137 GFLOP, 168 MB): the call 145 us,
+// quantizer 10.4, product about 134 (1.02 PFLOP/s), where a library product of the
+// same size with bfloat16 operands and outputs, without codes, scales and
+// activation, takes 127 - 130 in the same run.  Matrix instructions fill 47 % of the
+// cycles, at a clock that falls below 2 GHz under them; what is left between them is
+// the conversions of the codes and each block's activations and stores.
+// Serving: one token of 1024 -> 4096 (8.4 MB of weights) 4.6 us, 1.8 TB/s, 48 of
+// 2048 -> 1001 float16 7.6 us: a launch, and the chain of load, quantize, multiply and
+// the join of the waves' sums.
 #include "fp8_loops.h"
 
 namespace fqt {
@@ -83,7 +94,7 @@ bool gated_rows_raw(int64_t M, int64_t hidden, int64_t K) {
 }
 // The tiles of both halves of B, as if they were columns.  A pass over the parts
 // gates them too, and the call's host time pays for its launch: 250, 2048 -> 1001
-// float32 with checkpoints 22.8 us in parts, 23.8 in one launch, and 28.7, FILLIN as a call.
+// float32 with checkpoints 22.8 us in parts, 23.8 in one launch; as a call 28.7 and 25.5.
 static Fp8Plan gated_plan(int64_t M, int64_t hidden, int64_t K) { return fp8_plan(M, 2 * hidden, K, 8.0); }
 int64_t gated_partials(int64_t M, int64_t hidden, int64_t K) {
   const int64_t s = gated_plan(M, hidden, K).splits;

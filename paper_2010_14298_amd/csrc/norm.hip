@@ -19,7 +19,7 @@
 // With a checkpoint of xh in 8 bits, E + 127 and codes of each block of 32 along a
 // row: the forward finds the blocks' scales across neighbouring lanes of the team,
 // the backward reads one byte an element in place of x.  8192 x 1024 bfloat16 (42 MB)
-// forward 12.8 us, 3.3 TB/s, waits 62 % of the time; backward 13.4 us, 3.1 TB/s, and
+// forward 11.4 us, 3.7 TB/s; backward 12.7 us, 3.3 TB/s, waits 60 % of the time, and
 // 3.8 us for the partial sums.  8192 x 4096 float32 backward (303 MB): 59 us, 5.1
 // TB/s, a large copy's rate.
 #include "fp8_codes.h"
@@ -116,8 +116,7 @@ __device__ __forceinline__ void kept_values(const uint8_t* q, const uint8_t* e, 
   }
 }
 
-// KEEP: also the checkpoint of xh.
-template <class T, class C, bool KEEP>
+template <class T, class C>
 __global__ __launch_bounds__(C::THREADS) void norm_forward_kernel(NormParams p) {
   __shared__ float sh[C::WAVES][1];
   const int t = threadIdx.x % C::TPR;
@@ -166,15 +165,132 @@ __global__ __launch_bounds__(C::THREADS) void norm_forward_kernel(NormParams p) 
     }
     if (p.gamma) load_part<float, C::VEC>(p.gamma + col, p.cols - col, ga);
     if (p.beta) load_part<float, C::VEC>(p.beta + col, p.cols - col, be);
-    if constexpr (KEEP) {
 #pragma unroll
-      for (int i = 0; i < C::VEC; ++i) v[k][i] = col + i < p.cols ? (v[k][i] - mean) * rstd : 0.0f;
-      const int64_t pitch = kept_pitch(p.cols);
-      keep_codes<C::VEC>(p.q8 + row * pitch, p.e8 + row * (pitch / KEPT_BLOCK), p.cols, col, v[k]);
+    for (int i = 0; i < C::VEC; ++i) o[i] = fmaf((v[k][i] - mean) * rstd, ga[i], be[i]);
+    store_part<T, C::VEC>(y + col, p.cols - col, o);
+  }
+}
+
+// A vector of V elements of a row, as it lies in memory.  No branch around a load
+// (it would wait for the others): vectors that are not whole are read from the
+// row's end, and moved down by `value`.  SHORT: the row may be shorter than one.
+template <class T, int V, bool SHORT>
+struct RowVec {
+  static constexpr int W = V * (int)sizeof(T) / 4;
+  uint32_t w[W];
+  __device__ __forceinline__ void load(const T* row, int col, int cols) {
+    typedef uint32_t words __attribute__((ext_vector_type(W), aligned(sizeof(T))));
+    const int last = cols - V, from = col < last ? col : last;
+    words x;
+    if (SHORT && last < 0) {  // all in the first vector
+      T e[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) e[i] = row[i < cols ? i : cols - 1];
+      __builtin_memcpy(&x, e, sizeof(x));
+    } else {
+      x = *reinterpret_cast<const words*>(row + from);
     }
 #pragma unroll
-    for (int i = 0; i < C::VEC; ++i) o[i] = fmaf(KEEP ? v[k][i] : (v[k][i] - mean) * rstd, ga[i], be[i]);
-    store_part<T, C::VEC>(y + col, p.cols - col, o);
+    for (int i = 0; i < W; ++i) w[i] = x[i];
+  }
+  // left: the row's columns from the vector's first on; 0 past the row.
+  __device__ __forceinline__ void value(int left, int cols, float (&v)[V]) const {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = __uint_as_float(left > 0 ? w[i] : 0u);
+    } else {
+      typedef T pair __attribute__((ext_vector_type(2)));
+#pragma unroll
+      for (int i = 0; i < V; i += 2) {
+        const pair two = as<pair>(left > 0 ? w[i / 2] : 0u);
+        v[i] = (float)two[0];
+        v[i + 1] = (float)two[1];
+      }
+    }
+    if (cols % V != 0 && left < V) {
+      const int past = SHORT && cols < V ? 0 : V - left;
+#pragma unroll
+      for (int d = V / 2; d > 0; d /= 2) {  // down by past, bit by bit
+        const bool move = past > 0 && (past & d);
+#pragma unroll
+        for (int i = 0; i + d < V; ++i) {
+          const float up = v[i + d], here = v[i];
+          v[i] = move ? up : here;  // (of v[...] themselves it would choose the address)
+        }
+      }
+#pragma unroll
+      for (int i = 1; i < V; ++i) v[i] = i < left ? v[i] : 0.0f;
+    }
+  }
+};
+
+// With the checkpoint of xh.  All loads are under way before the first sum: 8192 x
+// 1024 bfloat16 11.4 us, 12.5 with gamma and beta loaded when they are needed and
+// branches at the row's end (float32 13.4, 15.2); 70 registers, seven waves a SIMD
+// (held to 64 the loads wait for spilled registers: 15.4).
+template <class T, class C>
+__global__ __launch_bounds__(C::THREADS) void norm_forward8_kernel(NormParams p) {
+  __shared__ float sh[C::WAVES][1];
+  constexpr int V = C::VEC, NV = C::NV;
+  constexpr bool SHORT = C::COLS <= 64 * 4;
+  const int t = threadIdx.x % C::TPR, cols = (int)p.cols;
+  const int64_t row = block_id() * C::PER_BLOCK + threadIdx.x / C::TPR;
+  if (row >= p.rows) return;  // whole waves and no barrier below, or whole blocks
+  RowVec<T, V, SHORT> x[NV];
+  RowVec<float, V, SHORT> ga[NV], be[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) x[k].load(static_cast<const T*>(p.x) + row * p.ldx, (k * C::TPR + t) * V, cols);
+  if (p.gamma) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) ga[k].load(p.gamma, (k * C::TPR + t) * V, cols);
+  }
+  if (p.beta) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) be[k].load(p.beta, (k * C::TPR + t) * V, cols);
+  }
+  float v[NV][V];
+  float s[1] = {0.0f};
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    x[k].value(cols - (k * C::TPR + t) * V, cols, v[k]);
+#pragma unroll
+    for (int i = 0; i < V; ++i) s[0] += v[k][i];
+  }
+  team_sum<C, 1>(s, sh);
+  const float inv = 1.0f / (float)p.cols;
+  const float mean = s[0] * inv;
+  s[0] = 0.0f;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int col = (k * C::TPR + t) * V;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float d = col + i < cols ? v[k][i] - mean : 0.0f;
+      s[0] = fmaf(d, d, s[0]);
+    }
+  }
+  team_sum<C, 1>(s, sh);
+  const float rstd = 1.0f / sqrtf(fmaf(s[0], inv, p.eps));
+  if (t == 0) p.rstd[row] = rstd;
+  T* const y = static_cast<T*>(p.y) + row * p.ldy;
+  const int64_t pitch = kept_pitch(p.cols);
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int col = (k * C::TPR + t) * V;
+    float a[V], b[V], o[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      a[i] = 1.0f;
+      b[i] = 0.0f;
+    }
+    if (p.gamma) ga[k].value(cols - col, cols, a);
+    if (p.beta) be[k].value(cols - col, cols, b);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[k][i] = col + i < cols ? (v[k][i] - mean) * rstd : 0.0f;
+    keep_codes<V>(p.q8 + row * pitch, p.e8 + row * (pitch / KEPT_BLOCK), p.cols, col, v[k]);
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[i] = fmaf(v[k][i], a[i], b[i]);
+    store_part<T, V>(y + col, cols - col, o);
   }
 }
 
@@ -346,18 +462,16 @@ __global__ __launch_bounds__(C::THREADS) void norm_backward_kernel(NormParams p)
 // and for the output.  Rows of one vector at least.
 template <class T, class C>
 struct KeptRow {
-  static constexpr int V = C::VEC, GW = V * (int)sizeof(T) / 4, QW = (V + 3) / 4;  // words of a vector of G, of codes
-  uint32_t g[C::NV][GW], q[C::NV][QW], e[C::NV];
+  static constexpr int V = C::VEC, QW = (V + 3) / 4;  // words of a vector's codes
+  RowVec<T, V, false> g[C::NV];
+  uint32_t q[C::NV][QW], e[C::NV];
   float rstd;
-  // No branch around a load (it would wait for the others): vectors that are not
-  // whole are read from the row's end; moved down by `value`.
   __device__ __forceinline__ void load(const NormParams& p, int64_t row, int t) {
     const int64_t pitch = kept_pitch(p.cols);
     const T* const gr = static_cast<const T*>(p.g) + row * p.ldg;
     const uint8_t* const qr = p.q8 + row * pitch;
     const uint8_t* const er = p.e8 + row * (pitch / KEPT_BLOCK);
     const int cols = (int)p.cols, width = (int)pitch;
-    typedef uint32_t g_words __attribute__((ext_vector_type(GW), aligned(sizeof(T))));
 #pragma unroll
     for (int k = 0; k < C::NV; ++k) {
       const int col = (k * C::TPR + t) * V, at = col < width ? col : 0;
@@ -368,10 +482,7 @@ struct KeptRow {
         for (int i = 0; i < QW; ++i) q[k][i] = *reinterpret_cast<const uint32_t*>(qr + at + 4 * i);
       }
       e[k] = er[at / KEPT_BLOCK];
-      const int last = cols - V, from = col < last ? col : last;
-      const g_words w = *reinterpret_cast<const g_words*>(gr + from);
-#pragma unroll
-      for (int i = 0; i < GW; ++i) g[k][i] = w[i];
+      g[k].load(gr, col, cols);
     }
     rstd = p.rstd[row];
   }
@@ -385,32 +496,6 @@ struct KeptRow {
       v[i + 1] = f[1];
     }
   }
-  // left: the row's columns from the vector's first on; 0 past the row.
-  __device__ __forceinline__ void value(int k, int left, int cols, float (&v)[V]) const {
-    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) v[i] = __uint_as_float(left > 0 ? g[k][i] : 0u);
-    } else {
-      typedef T pair __attribute__((ext_vector_type(2)));
-#pragma unroll
-      for (int i = 0; i < V; i += 2) {
-        const pair two = as<pair>(left > 0 ? g[k][i / 2] : 0u);
-        v[i] = (float)two[0];
-        v[i + 1] = (float)two[1];
-      }
-    }
-    if (cols % V != 0) {
-      const int past = V - left;
-#pragma unroll
-      for (int d = V / 2; d > 0; d /= 2) {  // down by past, bit by bit
-        const bool move = past > 0 && (past & d);
-#pragma unroll
-        for (int i = 0; i + d < V; ++i) v[i] = move ? v[i + d] : v[i];
-      }
-#pragma unroll
-      for (int i = 1; i < V; ++i) v[i] = i < left ? v[i] : 0.0f;
-    }
-  }
 };
 
 template <class T, class C>
@@ -420,17 +505,6 @@ __global__ __launch_bounds__(C::THREADS) void norm_backward8_kernel(NormParams p
   // a team is whole waves: its row's addresses stay scalar
   const int t = threadIdx.x % C::TPR, team = __builtin_amdgcn_readfirstlane(threadIdx.x / C::TPR), cols = (int)p.cols;
   const float inv = 1.0f / (float)p.cols;
-  float sg[C::NV][C::VEC], sb[C::NV][C::VEC], ga[C::NV][C::VEC];
-#pragma unroll
-  for (int k = 0; k < C::NV; ++k) {
-    const int col = (k * C::TPR + t) * C::VEC;
-#pragma unroll
-    for (int i = 0; i < C::VEC; ++i) {
-      sg[k][i] = sb[k][i] = 0.0f;
-      ga[k][i] = 1.0f;
-    }
-    if (p.gamma) load_part<float, C::VEC>(p.gamma + col, cols - col, ga[k]);
-  }
   // every team of the block makes the same number of turns; a team without a row
   // works on the last one and stores and adds nothing
   const int64_t step = (int64_t)gridDim.x * C::PER_BLOCK;
@@ -438,6 +512,21 @@ __global__ __launch_bounds__(C::THREADS) void norm_backward8_kernel(NormParams p
   constexpr bool AHEAD = C::TPR < 1024;
   KeptRow<T, C> next;
   if constexpr (AHEAD) next.load(p, row < p.rows ? row : p.rows - 1, t);
+  RowVec<float, C::VEC, false> gamma[C::NV];
+  if (p.gamma) {
+#pragma unroll
+    for (int k = 0; k < C::NV; ++k) gamma[k].load(p.gamma, (k * C::TPR + t) * C::VEC, cols);
+  }
+  float sg[C::NV][C::VEC], sb[C::NV][C::VEC], ga[C::NV][C::VEC];
+#pragma unroll
+  for (int k = 0; k < C::NV; ++k) {
+#pragma unroll
+    for (int i = 0; i < C::VEC; ++i) {
+      sg[k][i] = sb[k][i] = 0.0f;
+      ga[k][i] = 1.0f;
+    }
+    if (p.gamma) gamma[k].value(cols - (k * C::TPR + t) * C::VEC, cols, ga[k]);
+  }
   for (int64_t base = (int64_t)blockIdx.x * C::PER_BLOCK; base < p.rows; base += step, row += step) {
     if constexpr (!AHEAD) next.load(p, row < p.rows ? row : p.rows - 1, t);
     const KeptRow<T, C> r = next;
@@ -452,7 +541,7 @@ __global__ __launch_bounds__(C::THREADS) void norm_backward8_kernel(NormParams p
       for (int k = 0; k < C::NV; ++k) {
         float xh[C::VEC];
         r.xhat(k, xh);
-        r.value(k, cols - (k * C::TPR + t) * C::VEC, cols, gv[k]);
+        r.g[k].value(cols - (k * C::TPR + t) * C::VEC, cols, gv[k]);
 #pragma unroll
         for (int i = 0; i < C::VEC; ++i) {
           sg[k][i] = fmaf(gv[k][i], xh[i], sg[k][i]);
@@ -606,8 +695,14 @@ static hipError_t norm_forward(const NormParams& p, hipStream_t s) {
     using C = decltype(c);
     const int64_t blocks = (p.rows + C::PER_BLOCK - 1) / C::PER_BLOCK;
     const dim3 grid = grid_of(blocks, C::THREADS);
+    auto kernel = [] {
+      if constexpr (KEEP)
+        return norm_forward8_kernel<T, C>;
+      else
+        return norm_forward_kernel<T, C>;
+    }();
     if (p.cols <= TEAM_COLS)
-      hipLaunchKernelGGL((norm_forward_kernel<T, C, KEEP>), grid, dim3(C::THREADS), 0, s, p);
+      hipLaunchKernelGGL(kernel, grid, dim3(C::THREADS), 0, s, p);
     else if constexpr (C::TPR == 1024)
       hipLaunchKernelGGL((norm_forward_long_kernel<T, C, KEEP>), grid, dim3(C::THREADS), 0, s, p);
     return hipGetLastError();

@@ -231,13 +231,12 @@ bool fp8_two_at_once(int64_t Ma, int64_t Na, int64_t Ka, int64_t Mb, int64_t Nb,
   return Ma > ROWS_MAX && Mb > ROWS_MAX && fp8_plan(Ma, Na, Ka).splits > 1 && fp8_plan(Mb, Nb, Kb).splits > 1;
 }
 
-// us of a product by itself, as fp8_plan estimates it.
-static double plan_time(int64_t M, int64_t N, const Fp8Plan& plan) {
+double fp8_plan_time(int64_t M, int64_t N, const Fp8Plan& plan, double pass) {
   const bool large = plan.tile == Fp8Plan::LARGE, mid = plan.tile == Fp8Plan::MID;
   const double c = large ? 3.3 : mid ? 1.77 : 0.94, t0 = large ? 8.0 : mid ? 5.0 : 4.0;
   const int64_t tiles = tiles_of(M, N, mid || large ? 256 : 128, large ? 256 : 128) * plan.splits;
   return (double)((tiles + 255) / 256) * (plan.chunk * c + t0) +
-         (plan.splits > 1 ? 4.0 + (double)(M * N) * 8.0 * plan.splits / 4.0e6 : 0.0);
+         (plan.splits > 1 ? pass + (double)(M * N) * 8.0 * plan.splits / 4.0e6 : 0.0);
 }
 
 hipError_t launch_fp8_two(fqt_dtype type, const Fp8GemmParams& a, const Fp8GemmParams& b, bool any_order, hipStream_t s) {
@@ -254,7 +253,7 @@ hipError_t launch_fp8_two(fqt_dtype type, const Fp8GemmParams& a, const Fp8GemmP
       const double shorter = one_a < one_b ? one_a : one_b, longer = one_a < one_b ? one_b : one_a;
       double both = ((double)ta * one_a + (double)tb * one_b) / 256.0 + 0.5 * shorter;
       if (both < longer + 4.0) both = longer + 4.0;
-      const double apart = plan_time(a.M, a.N, fp8_plan(a.M, a.N, a.K)) + plan_time(b.M, b.N, fp8_plan(b.M, b.N, b.K));
+      const double apart = fp8_plan_time(a.M, a.N, fp8_plan(a.M, a.N, a.K)) + fp8_plan_time(b.M, b.N, fp8_plan(b.M, b.N, b.K));
       if (both < apart && ta + tb <= 0x7FFFFF) {
         const bool b_first = nk_b >= nk_a;
         return with_type(type, [&](auto e) {

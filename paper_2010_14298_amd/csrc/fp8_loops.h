@@ -501,7 +501,8 @@ __global__ __launch_bounds__(LargeTile::THREADS) void fp8_gemm_large_kernel(P p)
 // it multiplies the current ones; one barrier a stage of 128 along K.  KG = 2:
 // half of the waves take the first half of each stage along K, half the
 // second, and their sums meet in LDS at the end, so that a wave's tile is
-// twice as large and reads (and widens) less for each product.  NS whole
+// twice as large and reads (and widens) less for each product; then each stores
+// half of its rows, or, of 32 rows a wave, the first half of the waves all.  NS whole
 // stages of 128-byte rows in LDS, the 16-byte chunk index XOR-ed with (r / 2)
 // mod 8.  SPLIT: part by part, `chunk` stages each, which leave float32 sums in
 // p.part.  256 x 256 tiles do not fit this loop: their accumulators and a second
@@ -692,7 +693,29 @@ __device__ __forceinline__ void pipe_tile(const P& p, int chunk, uint32_t tile, 
   for (; t + 2 * C::NS - 1 < nk; t += C::NS) turn(inner);
   for (; t < nk; t += C::NS) turn(last);
   __syncthreads();
-  if constexpr (C::KG == 2) {
+  if constexpr (C::KG == 2 && C::IT == 1) {
+    static_assert(P::GATED && 2 * C::JT * 4096 <= C::CODES, "two waves' sums fit a stage buffer");
+    float4* const sums = reinterpret_cast<float4*>((wave & 2 ? q1 : q0) + (wave & 1) * C::JT * 4096) + lane;
+    if (kg == 1) {
+#pragma unroll
+      for (int j = 0; j < C::JT; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          sums[(j * 4 + r) * 64] = make_float4(acc[0][j][4 * r], acc[0][j][4 * r + 1], acc[0][j][4 * r + 2], acc[0][j][4 * r + 3]);
+    }
+    __syncthreads();
+    if (kg == 1) return;
+#pragma unroll
+    for (int j = 0; j < C::JT; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float4 o = sums[(j * 4 + r) * 64];
+        acc[0][j][4 * r] += o.x;
+        acc[0][j][4 * r + 1] += o.y;
+        acc[0][j][4 * r + 2] += o.z;
+        acc[0][j][4 * r + 3] += o.w;
+      }
+  } else if constexpr (C::KG == 2) {
     // the two halves of K: each wave hands half of its rows to its partner
     constexpr int HI = C::IT / 2, BYTES = HI * C::JT * 4096, FIT = C::CODES / BYTES;
     static_assert(FIT * C::NS >= 8, "the exchange fits the stage buffers");
@@ -730,7 +753,7 @@ __device__ __forceinline__ void pipe_tile(const P& p, int chunk, uint32_t tile, 
       }
     __syncthreads();
   }
-  constexpr int STRIPS = C::IT / C::KG;
+  constexpr int STRIPS = C::IT > 1 ? C::IT / C::KG : 1;
   if constexpr (P::GATED) {
     v16f mine[STRIPS][C::JT];
 #pragma unroll

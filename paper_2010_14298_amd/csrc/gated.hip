@@ -93,9 +93,21 @@ bool gated_rows_raw(int64_t M, int64_t hidden, int64_t K) {
   return M <= 16 || turns * nk < 40 + nk + nk / 2;
 }
 // The tiles of both halves of B, as if they were columns.  A pass over the parts
-// gates them too, and the call's host time pays for its launch: 250, 2048 -> 1001
-// float32 with checkpoints 22.8 us in parts, 23.8 in one launch; as a call 28.7 and 25.5.
-static Fp8Plan gated_plan(int64_t M, int64_t hidden, int64_t K) { return fp8_plan(M, 2 * hidden, K, 8.0); }
+// gates them too, and the call's host time pays for its launch.  Where the small
+// tiles leave half of the units without one they are halved, 64 rows each, 0.63 us a
+// stage of 128; whole / half, in a graph with checkpoints, us: 250, 2048 -> 1001
+// float32 23.9 / 19.4 (in two parts 22.8), 256, 1024 -> 2048 float16 18.1 / 15.2, 2048,
+// 256 -> 512 bfloat16 13.3 / 12.1; in parts / half 250, 2944 -> 1024
+// bfloat16 25.1 / 22.3.  Longer ones stay in parts.
+typedef PipeTile<64, 128, 32, 64, 2, 4> HalfTile;
+static bool halves(const Fp8Plan& plan, int64_t M, int64_t hidden) {
+  return plan.tile == Fp8Plan::SMALL && plan.splits == 1 && tiles_of(M, hidden, SmallTile::BM, SmallTile::BN / 2) <= 128;
+}
+static Fp8Plan gated_plan(int64_t M, int64_t hidden, int64_t K) {
+  const int64_t nk = fp8_blocks(K);
+  const Fp8Plan plan = fp8_plan(M, 2 * hidden, K, 8.0), whole{Fp8Plan::SMALL, 1, (int)nk};
+  return halves(whole, M, hidden) && (double)nk * 0.63 + 4.0 < fp8_plan_time(M, 2 * hidden, plan, 8.0) ? whole : plan;
+}
 int64_t gated_partials(int64_t M, int64_t hidden, int64_t K) {
   const int64_t s = gated_plan(M, hidden, K).splits;
   return s > 1 ? s * M * 2 * hidden : 0;
@@ -123,6 +135,8 @@ static hipError_t gated_tiles(const GatedGemm<SAVE>& p, const Fp8Plan& plan, hip
     }
     return go(fp8_gemm_large_kernel<T, false, false, GatedGemm<SAVE>>, blocks);
   }
+  if (halves(plan, p.M, p.hidden))
+    return go(fp8_gemm_pipe_kernel<T, HalfTile, false, false, GatedGemm<SAVE>>, tiles(HalfTile{}), plan.chunk);
   if (plan.tile == Fp8Plan::MID)
     return go(fp8_gemm_pipe_kernel<T, MidTile, false, false, GatedGemm<SAVE>>, blocks, plan.chunk);
   return go(fp8_gemm_pipe_kernel<T, SmallTile, false, false, GatedGemm<SAVE>>, blocks, plan.chunk);

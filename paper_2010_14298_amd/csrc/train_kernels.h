@@ -215,6 +215,8 @@ struct Fp8Plan {
 };
 // pass: us of a launch that adds the parts.
 Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, double pass = 4.0);
+// us of a product by itself, as fp8_plan estimates it.
+double fp8_plan_time(int64_t M, int64_t N, const Fp8Plan& plan, double pass = 4.0);
 hipError_t launch_fp8_parts(const Fp8GemmParams& p, const Fp8Plan& plan, hipStream_t s);  // to p.part
 fqt_fp8_form fp8_gemm_form(int64_t M, int64_t N, int64_t K, bool masked, bool lines);
 hipError_t launch_fp8_gemm(fqt_dtype type, const Fp8GemmParams& p, hipStream_t s);

@@ -101,7 +101,8 @@ def check_forward(X, W, act, H, kept, K):
 # forward
 # ---------------------------------------------------------------------------
 SHAPES = [(1, 64, 32), (1, 1000, 1001), (2, 129, 33), (7, 100, 1), (16, 256, 512), (17, 130, 96), (64, 384, 200),
-          (65, 512, 131), (130, 4096, 68), (257, 640, 320), (300, 96, 1000), (513, 320, 257)]
+          (65, 512, 131), (130, 4096, 68), (257, 640, 320), (300, 96, 1000), (513, 320, 257), (131, 1200, 70),
+          (190, 1800, 65), (129, 900, 1)]
 
 
 @pytest.mark.parametrize("act", ["silu", "gelu_tanh", "relu"])
@@ -119,7 +120,8 @@ def test_forward(N, d_in, hidden, dtype, act):
 
 
 @pytest.mark.parametrize("N,d_in,hidden,dtype", [(1024, 512, 2048, torch.bfloat16), (2304, 256, 1024, torch.float32),
-                                                 (1000, 1024, 1200, torch.float16), (4100, 130, 900, torch.bfloat16)])
+                                                 (1000, 1024, 1200, torch.float16), (4100, 130, 900, torch.bfloat16),
+                                                 (1030, 1100, 1100, torch.float32)])
 def test_forward_of_many_tiles(N, d_in, hidden, dtype):
     X = matrix(1, N, d_in, dtype)
     W, W8, _ = weights(2, hidden, d_in)

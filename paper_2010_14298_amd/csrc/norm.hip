@@ -19,8 +19,8 @@
 // With a checkpoint of xh in 8 bits, E + 127 and codes of each block of 32 along a
 // row: the forward finds the blocks' scales across neighbouring lanes of the team,
 // the backward reads one byte an element in place of x.  8192 x 1024 bfloat16 (42 MB)
-// forward 11.4 us, 3.7 TB/s; backward 12.7 us, 3.3 TB/s, waits 60 % of the time, and
-// 3.8 us for the partial sums.  8192 x 4096 float32 backward (303 MB): 59 us, 5.1
+// forward 11.4 us, 3.7 TB/s; backward 12.6 us, 3.3 TB/s, and 3.8 us for the partial
+// sums.  8192 x 4096 float32 backward (303 MB): 58 us, 5.2
 // TB/s, a large copy's rate.
 #include "fp8_codes.h"
 

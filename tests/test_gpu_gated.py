@@ -380,6 +380,43 @@ def test_gradients_against_differences():
         assert num @ kernel / np.linalg.norm(num) / np.linalg.norm(kernel) > 0.99
 
 
+@pytest.mark.parametrize("N,d_in,hidden,dtype", [(9, 200, 70, torch.float32), (140, 200, 70, torch.float16),
+                                                 (1024, 512, 2048, torch.float16), (2304, 256, 1024, torch.bfloat16),
+                                                 (8192, 128, 2048, torch.bfloat16)])
+def test_each_output_alone(N, d_in, hidden, dtype):
+    """What a caller of the library may leave out: any of what the forward keeps, either gradient."""
+    f = fqt()
+    lib, stream = f.load(), torch.cuda.current_stream().cuda_stream
+    X, g = matrix(60, N, d_in, dtype), matrix(61, N, hidden, dtype)
+    W, W8, W8t = weights(62, hidden, d_in)
+    H, kept, _ = f.fqt_fp8_gated_forward(X, W8)
+    t, w8 = f.TYPES[dtype], f.Fp8(W8["q"].data_ptr(), W8["exp"].data_ptr(), 0)
+    ws = torch.empty(max(f.fqt_fp8_gated_forward_workspace(N, d_in, hidden), 16), dtype=torch.uint8, device="cuda")
+    for name in ("X8t", "d_gate", "d_up"):
+        out = {k: torch.full_like(kept[name][k].view(torch.uint8), 9) for k in ("q", "exp")}
+        where = (f.Fp8(out["q"].data_ptr(), out["exp"].data_ptr(), 0) if name == "X8t"
+                 else f.Kept(out["q"].data_ptr(), out["exp"].data_ptr()))
+        alone = torch.empty_like(H)
+        assert lib.fqt_fp8_gated_forward(X.data_ptr(), t, N, d_in, d_in, w8, hidden, 0, alone.data_ptr(), hidden,
+                                         *(where if n == name else None for n in ("X8t", "d_gate", "d_up")),
+                                         ws.data_ptr(), ws.numel(), stream) == 0
+        assert torch.equal(out["q"], kept[name]["q"].view(torch.uint8)) and torch.equal(out["exp"], kept[name]["exp"])
+        if name != "X8t":  # (without a checkpoint few rows take another form)
+            assert torch.equal(alone, H)
+    _, gX, ws = f.fqt_fp8_gated_backward(g, kept, W8t, seed=3)
+    c = {n: f.Kept(kept[n]["q"].data_ptr(), kept[n]["exp"].data_ptr()) for n in ("d_gate", "d_up")}
+    w8t, alone = f.Fp8(W8t["q"].data_ptr(), W8t["exp"].data_ptr(), 0), torch.empty_like(gX)
+    assert lib.fqt_fp8_gated_backward(g.data_ptr(), t, N, hidden, hidden, c["d_gate"], c["d_up"], None, w8t, d_in, 1, 3, None,
+                                      alone.data_ptr(), d_in, ws.data_ptr(), ws.numel(), stream) == 0
+    vg, vu = (G.kept_values(bytes_of(kept[n]["q"]), kept[n]["exp"].cpu().numpy(), hidden) for n in ("d_gate", "d_up"))
+    r = G.gradient_operands(host(g), vg, vu, 3)[1]["value"]
+    wt = F.operand(host(W).T, tile=True)["value"]
+    size = np.abs(r) @ np.abs(wt).T
+    # both within 2 hidden U of the exact sums, and each rounded once
+    bound = 4 * hidden * U * size + 2 * HALF[dtype] * (np.abs(host(gX)) + 4 * hidden * U * size) + 2 * TINY[dtype]
+    assert np.all(np.abs(host(alone) - host(gX)) <= bound)
+
+
 # ---------------------------------------------------------------------------
 # refusals of the binding
 # ---------------------------------------------------------------------------

@@ -343,120 +343,6 @@ __global__ __launch_bounds__(C::THREADS) void norm_forward_long_kernel(NormParam
   }
 }
 
-// The sums of a block's teams, added up pairwise in LDS: one partial row (an only
-// block writes the parameter gradients themselves).
-template <class C>
-using ColumnSums = float[C::PER_BLOCK > 1 ? C::PER_BLOCK / 2 : 1][2][C::PER_BLOCK > 1 ? C::COLS : 4];
-template <class C>
-__device__ __forceinline__ void store_columns(const NormParams& p, float (&sg)[C::NV][C::VEC], float (&sb)[C::NV][C::VEC],
-                                              ColumnSums<C>& col_sum, int t, int team) {
-#pragma unroll
-  for (int w = C::PER_BLOCK / 2; w > 0; w /= 2) {  // teams w .. 2 w - 1 hand over to 0 .. w - 1
-    if (team >= w && team < 2 * w) {
-#pragma unroll
-      for (int k = 0; k < C::NV; ++k) {
-        const int col = (k * C::TPR + t) * C::VEC;
-        store_vec<float, C::VEC>(&col_sum[team - w][0][col], sg[k]);
-        store_vec<float, C::VEC>(&col_sum[team - w][1][col], sb[k]);
-      }
-    }
-    __syncthreads();
-    if (team < w) {
-#pragma unroll
-      for (int k = 0; k < C::NV; ++k) {
-        const int col = (k * C::TPR + t) * C::VEC;
-        float a[C::VEC], b[C::VEC];
-        load_vec<float, C::VEC>(&col_sum[team][0][col], a);
-        load_vec<float, C::VEC>(&col_sum[team][1][col], b);
-#pragma unroll
-        for (int i = 0; i < C::VEC; ++i) {
-          sg[k][i] += a[i];
-          sb[k][i] += b[i];
-        }
-      }
-    }
-    __syncthreads();
-  }
-  if (team != 0) return;
-  float* part = p.part + (int64_t)blockIdx.x * 2 * p.cols;
-  float* const to_gamma = gridDim.x == 1 ? p.grad_gamma : part;
-  float* const to_beta = gridDim.x == 1 ? p.grad_beta : part + p.cols;
-#pragma unroll
-  for (int k = 0; k < C::NV; ++k) {
-    const int64_t col = (int64_t)(k * C::TPR + t) * C::VEC;
-    if (to_gamma) store_part<float, C::VEC>(to_gamma + col, p.cols - col, sg[k]);
-    if (to_beta) store_part<float, C::VEC>(to_beta + col, p.cols - col, sb[k]);
-  }
-}
-
-// Backward: one block of 1024 threads a unit, so that there are few partial
-// sums (8192 x 1024 bfloat16: 1024 blocks of four teams leave 8 MB of them, 21.1
-// us in all instead of 17.8; float32 29.5, 27.3).  Each team takes every (teams)-th row and keeps its columns'
-// sums of g xh and g in registers.
-template <class T, class C>
-__global__ __launch_bounds__(C::THREADS) void norm_backward_kernel(NormParams p) {
-  __shared__ float sh[C::PER_BLOCK][C::WAVES][2];
-  __shared__ __attribute__((aligned(16))) ColumnSums<C> col_sum;
-  const int t = threadIdx.x % C::TPR, team = threadIdx.x / C::TPR;
-  const float inv = 1.0f / (float)p.cols;
-  float sg[C::NV][C::VEC], sb[C::NV][C::VEC];
-#pragma unroll
-  for (int k = 0; k < C::NV; ++k)
-#pragma unroll
-    for (int i = 0; i < C::VEC; ++i) sg[k][i] = sb[k][i] = 0.0f;
-  // every team of the block makes the same number of turns (the barriers
-  // inside team_sum meet); a team without a row reads and writes nothing
-  for (int64_t base = (int64_t)blockIdx.x * C::PER_BLOCK; base < p.rows; base += (int64_t)gridDim.x * C::PER_BLOCK) {
-    const bool any = base + team < p.rows;
-    const int64_t row = any ? base + team : 0;
-    const int cols = any ? (int)p.cols : 0;
-    const T* x = static_cast<const T*>(p.x) + row * p.ldx;
-    const T* g = static_cast<const T*>(p.g) + row * p.ldg;
-    float xh[C::NV][C::VEC], gv[C::NV][C::VEC];
-#pragma unroll
-    for (int k = 0; k < C::NV; ++k) {
-      const int col = (k * C::TPR + t) * C::VEC;
-      load_part<T, C::VEC>(x + col, cols - col, xh[k]);
-      load_part<T, C::VEC>(g + col, cols - col, gv[k]);
-    }
-    const float mean = p.mean[row], rstd = p.rstd[row];
-    float s[2] = {0.0f, 0.0f};
-#pragma unroll
-    for (int k = 0; k < C::NV; ++k) {
-      const int col = (k * C::TPR + t) * C::VEC;
-      float ga[C::VEC];
-#pragma unroll
-      for (int i = 0; i < C::VEC; ++i) ga[i] = 1.0f;
-      // read again for every row: from the nearest cache, and the registers
-      // hold more waves instead
-      if (p.gamma) load_part<float, C::VEC>(p.gamma + col, (int)p.cols - col, ga);
-#pragma unroll
-      for (int i = 0; i < C::VEC; ++i) {
-        // no column (or no row): xh is 0 like g, since (0 - mean) rstd may be infinite
-        xh[k][i] = col + i < cols ? (xh[k][i] - mean) * rstd : 0.0f;
-        sg[k][i] = fmaf(gv[k][i], xh[k][i], sg[k][i]);
-        sb[k][i] += gv[k][i];
-        gv[k][i] *= ga[i];
-        s[0] += gv[k][i];
-        s[1] = fmaf(gv[k][i], xh[k][i], s[1]);
-      }
-    }
-    team_sum<C, 2>(s, sh[team]);
-    const float a = s[0] * inv, b = s[1] * inv;
-    T* y = static_cast<T*>(p.y) + row * p.ldy;
-#pragma unroll
-    for (int k = 0; k < C::NV; ++k) {
-      const int64_t col = (int64_t)(k * C::TPR + t) * C::VEC;
-      float o[C::VEC];
-#pragma unroll
-      for (int i = 0; i < C::VEC; ++i) o[i] = rstd * ((gv[k][i] - a) - xh[k][i] * b);
-      store_part<T, C::VEC>(y + col, cols - col, o);
-    }
-  }
-  if (!p.grad_gamma && !p.grad_beta) return;
-  store_columns<C>(p, sg, sb, col_sum, t, team);
-}
-
 // Backward from the checkpoint.  The codes and G wait in registers as they were
 // loaded, a row ahead of the arithmetic, and codes are decoded twice: for the sums
 // and for the output.  Rows of one vector at least.
@@ -498,10 +384,10 @@ struct KeptRow {
   }
 };
 
+// The rows of a team: grad_X, and the sums sg and sb from 0.
 template <class T, class C>
-__global__ __launch_bounds__(C::THREADS) void norm_backward8_kernel(NormParams p) {
-  __shared__ float sh[C::PER_BLOCK][C::WAVES][2];
-  __shared__ __attribute__((aligned(16))) ColumnSums<C> col_sum;
+__device__ __forceinline__ void kept_rows(const NormParams& p, float (&sh)[C::PER_BLOCK][C::WAVES][2],
+                                          float (&sg)[C::NV][C::VEC], float (&sb)[C::NV][C::VEC]) {
   // a team is whole waves: its row's addresses stay scalar
   const int t = threadIdx.x % C::TPR, team = __builtin_amdgcn_readfirstlane(threadIdx.x / C::TPR), cols = (int)p.cols;
   const float inv = 1.0f / (float)p.cols;
@@ -517,14 +403,11 @@ __global__ __launch_bounds__(C::THREADS) void norm_backward8_kernel(NormParams p
 #pragma unroll
     for (int k = 0; k < C::NV; ++k) gamma[k].load(p.gamma, (k * C::TPR + t) * C::VEC, cols);
   }
-  float sg[C::NV][C::VEC], sb[C::NV][C::VEC], ga[C::NV][C::VEC];
+  float ga[C::NV][C::VEC];
 #pragma unroll
   for (int k = 0; k < C::NV; ++k) {
 #pragma unroll
-    for (int i = 0; i < C::VEC; ++i) {
-      sg[k][i] = sb[k][i] = 0.0f;
-      ga[k][i] = 1.0f;
-    }
+    for (int i = 0; i < C::VEC; ++i) ga[k][i] = 1.0f;
     if (p.gamma) gamma[k].value(cols - (k * C::TPR + t) * C::VEC, cols, ga[k]);
   }
   for (int64_t base = (int64_t)blockIdx.x * C::PER_BLOCK; base < p.rows; base += step, row += step) {
@@ -565,8 +448,119 @@ __global__ __launch_bounds__(C::THREADS) void norm_backward8_kernel(NormParams p
       store_part<T, C::VEC>(y + col, row < p.rows ? cols - col : 0, o);
     }
   }
+}
+
+// Backward: one block of 1024 threads a unit, so that there are few partial
+// sums (8192 x 1024 bfloat16: 1024 blocks of four teams leave 8 MB of them, 21.1
+// us in all instead of 17.8; float32 29.5, 27.3).  Each team takes every (teams)-th row and keeps its columns'
+// sums of g xh and g in registers; at the end the block's teams meet in LDS
+// pairwise and one writes the block's partial row (an only block writes the
+// parameter gradients themselves).  KEPT: from the checkpoint.
+template <class T, class C, bool KEPT>
+__global__ __launch_bounds__(C::THREADS) void norm_backward_kernel(NormParams p) {
+  __shared__ float sh[C::PER_BLOCK][C::WAVES][2];
+  __shared__ __attribute__((aligned(16))) float col_sum[C::PER_BLOCK > 1 ? C::PER_BLOCK / 2 : 1][2][C::PER_BLOCK > 1 ? C::COLS : 4];
+  const int t = threadIdx.x % C::TPR, team = threadIdx.x / C::TPR;
+  const float inv = 1.0f / (float)p.cols;
+  float sg[C::NV][C::VEC], sb[C::NV][C::VEC];
+#pragma unroll
+  for (int k = 0; k < C::NV; ++k)
+#pragma unroll
+    for (int i = 0; i < C::VEC; ++i) sg[k][i] = sb[k][i] = 0.0f;
+  // 16 elements of each of a row's 1024 threads do not fit the registers with what kept_rows
+  // holds besides: 2048 x 16000 bfloat16 90 us, row by row 57 (float32 123, 86)
+  constexpr bool AHEAD = KEPT && (C::TPR < 1024 || C::NV * C::VEC <= 8);
+  if constexpr (AHEAD) kept_rows<T, C>(p, sh, sg, sb);
+  // every team of the block makes the same number of turns (the barriers
+  // inside team_sum meet); a team without a row reads and writes nothing
+  for (int64_t base = (int64_t)blockIdx.x * C::PER_BLOCK; !AHEAD && base < p.rows; base += (int64_t)gridDim.x * C::PER_BLOCK) {
+    const bool any = base + team < p.rows;
+    const int64_t row = any ? base + team : 0;
+    const int cols = any ? (int)p.cols : 0;
+    const T* x = static_cast<const T*>(p.x) + row * p.ldx;
+    const T* g = static_cast<const T*>(p.g) + row * p.ldg;
+    float xh[C::NV][C::VEC], gv[C::NV][C::VEC];
+#pragma unroll
+    for (int k = 0; k < C::NV; ++k) {
+      const int col = (k * C::TPR + t) * C::VEC;
+      if constexpr (KEPT)
+        kept_values<C::VEC>(p.q8 + row * kept_pitch(p.cols), p.e8 + row * kept_blocks(p.cols), cols - col, col, xh[k]);
+      else
+        load_part<T, C::VEC>(x + col, cols - col, xh[k]);
+      load_part<T, C::VEC>(g + col, cols - col, gv[k]);
+    }
+    const float mean = KEPT ? 0.0f : p.mean[row], rstd = p.rstd[row];
+    float s[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < C::NV; ++k) {
+      const int col = (k * C::TPR + t) * C::VEC;
+      float ga[C::VEC];
+#pragma unroll
+      for (int i = 0; i < C::VEC; ++i) ga[i] = 1.0f;
+      // read again for every row: from the nearest cache, and the registers
+      // hold more waves instead
+      if (p.gamma) load_part<float, C::VEC>(p.gamma + col, (int)p.cols - col, ga);
+#pragma unroll
+      for (int i = 0; i < C::VEC; ++i) {
+        // no column (or no row): xh is 0 like g, since (0 - mean) rstd may be infinite
+        if constexpr (!KEPT) xh[k][i] = col + i < cols ? (xh[k][i] - mean) * rstd : 0.0f;
+        sg[k][i] = fmaf(gv[k][i], xh[k][i], sg[k][i]);
+        sb[k][i] += gv[k][i];
+        gv[k][i] *= ga[i];
+        s[0] += gv[k][i];
+        s[1] = fmaf(gv[k][i], xh[k][i], s[1]);
+      }
+    }
+    team_sum<C, 2>(s, sh[team]);
+    const float a = s[0] * inv, b = s[1] * inv;
+    T* y = static_cast<T*>(p.y) + row * p.ldy;
+#pragma unroll
+    for (int k = 0; k < C::NV; ++k) {
+      const int64_t col = (int64_t)(k * C::TPR + t) * C::VEC;
+      float o[C::VEC];
+#pragma unroll
+      for (int i = 0; i < C::VEC; ++i) o[i] = rstd * ((gv[k][i] - a) - xh[k][i] * b);
+      store_part<T, C::VEC>(y + col, cols - col, o);
+    }
+  }
   if (!p.grad_gamma && !p.grad_beta) return;
-  store_columns<C>(p, sg, sb, col_sum, t, team);
+#pragma unroll
+  for (int w = C::PER_BLOCK / 2; w > 0; w /= 2) {  // teams w .. 2 w - 1 hand over to 0 .. w - 1
+    if (team >= w && team < 2 * w) {
+#pragma unroll
+      for (int k = 0; k < C::NV; ++k) {
+        const int col = (k * C::TPR + t) * C::VEC;
+        store_vec<float, C::VEC>(&col_sum[team - w][0][col], sg[k]);
+        store_vec<float, C::VEC>(&col_sum[team - w][1][col], sb[k]);
+      }
+    }
+    __syncthreads();
+    if (team < w) {
+#pragma unroll
+      for (int k = 0; k < C::NV; ++k) {
+        const int col = (k * C::TPR + t) * C::VEC;
+        float a[C::VEC], b[C::VEC];
+        load_vec<float, C::VEC>(&col_sum[team][0][col], a);
+        load_vec<float, C::VEC>(&col_sum[team][1][col], b);
+#pragma unroll
+        for (int i = 0; i < C::VEC; ++i) {
+          sg[k][i] += a[i];
+          sb[k][i] += b[i];
+        }
+      }
+    }
+    __syncthreads();
+  }
+  if (team != 0) return;
+  float* part = p.part + (int64_t)blockIdx.x * 2 * p.cols;
+  float* const to_gamma = gridDim.x == 1 ? p.grad_gamma : part;
+  float* const to_beta = gridDim.x == 1 ? p.grad_beta : part + p.cols;
+#pragma unroll
+  for (int k = 0; k < C::NV; ++k) {
+    const int64_t col = (int64_t)(k * C::TPR + t) * C::VEC;
+    if (to_gamma) store_part<float, C::VEC>(to_gamma + col, p.cols - col, sg[k]);
+    if (to_beta) store_part<float, C::VEC>(to_beta + col, p.cols - col, sb[k]);
+  }
 }
 
 // Rows longer than a team's registers: inputs read twice, no parameter sums.
@@ -770,12 +764,12 @@ static hipError_t norm_backward(const NormParams& p, bool sums, int64_t blocks, 
   if (p.q8)
     return with_kept_block<T>(p.cols, [&](auto c) {
       using C = decltype(c);
-      hipLaunchKernelGGL((norm_backward8_kernel<T, C>), grid, dim3(C::THREADS), 0, s, p);
+      hipLaunchKernelGGL((norm_backward_kernel<T, C, true>), grid, dim3(C::THREADS), 0, s, p);
       return hipGetLastError();
     });
   return with_block<T>(p.cols, [&](auto c) {
     using C = decltype(c);
-    hipLaunchKernelGGL((norm_backward_kernel<T, C>), grid, dim3(C::THREADS), 0, s, p);
+    hipLaunchKernelGGL((norm_backward_kernel<T, C, false>), grid, dim3(C::THREADS), 0, s, p);
     return hipGetLastError();
   });
 }

@@ -23,7 +23,7 @@ HALF = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0
 TINY = {torch.float32: 0.0, torch.bfloat16: 0.0, torch.float16: 2.0 ** -25}
 TYPES = [torch.float32, torch.bfloat16, torch.float16]
 SIZES = [(1, 1), (1, 31), (2, 32), (3, 33), (5, 256), (7, 257), (300, 130), (40, 512), (33, 1000), (129, 1024), (20, 2048),
-         (9, 4096), (6, 8192), (3, 16384), (2, 16385), (4, 20011)]
+         (9, 4096), (6, 8192), (3, 16384), (2, 16385), (4, 20011), (600, 6001), (300, 9002)]
 
 
 def fqt():

@@ -82,15 +82,22 @@ __global__ __launch_bounds__(256) void gated_finish_kernel(GatedGemmParams p, in
 // launches
 // ---------------------------------------------------------------------------
 // Few rows that keep nothing (serving) are read as they are, 16 a block, each of
-// which quantizes them for itself; with more blocks or a longer K a quantizer in
-// front and the tiles are faster.  us in a graph, bfloat16, as they are / tiles:
-// 1024 -> 4096 one row 3.9, 16 rows 4.5, 64 10.8 / 16.1, 96 15.6 / 16.0, 128 20 / 15;
-// 2048 -> 1001 48 rows 7.0 / 20, 128 12.4 / 18.8; 4096 -> 4096 17 rows 18.9 / 24.5,
-// 48 31 / 24.
+// which quantizes them for itself and walks all of K; with more blocks or a longer K a
+// quantizer in front and the tiles, in parts along K, are faster.  us in a graph,
+// bfloat16, as they are / tiles: 1024 -> 4096 one row 3.9, 16 rows 4.5, 64 10.8 / 16.1,
+// 96 15.6 / 16.0, 128 20 / 15; 2048 -> 1001 48 rows 7.0 / 20, 128 12.4 / 18.8; 4096 ->
+// 4096 17 rows 18.9 / 24.5, 48 31 / 24; 48 rows -> 2048, two turns of the units, 4096 20.9 /
+// 23.5, 6144 29.7 / 26.4, 8192 37.9 / 28.7; 48 rows -> 512 8192 19.8 / 25.2, 12288 28.1 /
+// 26.8, 32768 69 / 37.  One row and 16, whose tiles wait for the weights of many hidden
+// units: -> 256 12288 19.0 / 22.1 and 27.4 / 25.0, 16384 23.6 / 23.3 and 35.6 / 27.1, 32768
+// 42.6 / 29.9 and 69 / 33; -> 1024 16384 24.8 / 25.9 and 36.4 / 31.6, 32768 44 / 34 and 69 /
+// 38; -> 2048 20480 30.6 / 34.0 and 44.8 / 37.6, 32768 45 / 46 and 70 / 48; -> 4096 32768
+// 53 / 73 and 72 / 78, 65536 110 / 155 and 144 / 156.  (float32 16 rows: -> 256 12288 36 / 26,
+// 16384 47 / 27, -> 4096 32768 93 / 75; the workspace is asked for without a type.)
 bool gated_rows_raw(int64_t M, int64_t hidden, int64_t K) {
-  if (M > 128) return false;
-  const int64_t nk = fp8_blocks(K), turns = ((M + 15) / 16 * ((hidden + 15) / 16) + 255) / 256;
-  return M <= 16 || turns * nk < 40 + nk + nk / 2;
+  const int64_t nk = fp8_blocks(K), blocks = (hidden + 15) / 16, turns = ((M + 15) / 16 * blocks + 255) / 256;
+  if (M <= 16) return nk <= 96 + blocks || blocks >= 192;
+  return M <= 128 && turns * nk < 40 + nk + nk / 2 && turns * nk <= 96;
 }
 // The tiles of both halves of B, as if they were columns.  A pass over the parts
 // gates them too, and the call's host time pays for its launch.  Where the small

@@ -494,8 +494,12 @@ typedef enum { FQT_SILU = 0, FQT_GELU_TANH = 1, FQT_RELU = 2 } fqt_act;
  *   d_gate  checkpoint [N, hidden] of dH/da = b act'(a)
  *   d_up    checkpoint [N, hidden] of dH/db = act(a)
  * Two bytes a hidden unit: the derivatives themselves are kept, not a and b, so
- * that the backward is linear in what was rounded.  hidden < 2^29 (also in the
- * backward), d_in up to 2^23 (FQT_EUNSUPPORTED beyond).                       */
+ * that the backward is linear in what was rounded.  The order of the sums of a
+ * and b depends on N, d_in and hidden, and up to 128 rows on whether a
+ * checkpoint is wanted, so that a row may differ in its last bits from the same
+ * row of another batch; it depends neither on the run, nor on the row's place,
+ * nor on the other rows.  hidden < 2^29 (also in the backward), d_in up to 2^23
+ * (FQT_EUNSUPPORTED beyond).                                                 */
 fqt_status fqt_fp8_gated_forward(const void* X, fqt_dtype type, int64_t N, int64_t d_in, int64_t ldx,
                                  const fqt_fp8* W8, int64_t hidden, fqt_act act, void* H, int64_t ldh,
                                  const fqt_fp8* X8t, const fqt_kept* d_gate, const fqt_kept* d_up, void* ws,

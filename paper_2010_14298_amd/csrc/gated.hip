@@ -107,6 +107,9 @@ bool gated_rows_raw(int64_t M, int64_t hidden, int64_t K) {
 // 256 -> 512 bfloat16 13.3 / 12.1; in parts / half 250, 2944 -> 1024
 // bfloat16 25.1 / 22.3.  Longer ones stay in parts.
 typedef PipeTile<64, 128, 32, 64, 2, 4> HalfTile;
+// The order of a row's sums is the form's: a wave holds both projections of 32 hidden
+// units, 64 columns, so that these tiles, for every type, divide K between two groups
+// of four waves (the plain layer's of 16-bit outputs, 32 columns a wave, need not).
 static bool halves(const Fp8Plan& plan, int64_t M, int64_t hidden) {
   return plan.tile == Fp8Plan::SMALL && plan.splits == 1 && tiles_of(M, hidden, SmallTile::BM, SmallTile::BN / 2) <= 128;
 }

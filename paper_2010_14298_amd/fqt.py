@@ -815,7 +815,8 @@ def fqt_fp8_gated_forward_workspace(N, d_in, hidden, k_major=False, save=True):
 def fqt_fp8_gated_forward(X, W8, act="silu", save=True, H=None, ws=None):
     """H = act(Q(X) W_gate^T) Q(X) W_up^T, W8 the by_row operand (tile=True) of [W_gate; W_up].  save: also what
     fqt_fp8_gated_backward reads, dict(X8t=operand of X^T, d_gate, d_up=checkpoints of H's derivatives by the two
-    products).  Returns (H, kept or None, ws or None: a call of few rows may need none)."""
+    products).  Returns (H, kept or None, ws or None: a call of few rows may need none).  The order of a row's sums
+    depends on the sizes, and up to 128 rows on save: the same row of another batch may differ in its last bits."""
     dev = _device()
     px, dt, N, d_in, ldx = _matrix(X, "X", dev)
     code = ACTS.get(act)

@@ -489,7 +489,7 @@ hipError_t launch_fp8_quantize(fqt_dtype type, const Fp8QuantParams& p, hipStrea
 // the bound, and 16 bits are as many as 16-bit G times a code leaves to round (the
 // layer's own quantizer takes two words of 24 bits, which float32 would need).
 // 8192 x 8192 bfloat16 (268 MB with the second read of G, 24 MB of weights and X to
-// lay out): 78 us, 3.7 TB/s; vector issue 67 % busy, waits 23 % of the time.
+// lay out): 79 us, 3.7 TB/s; vector issue 68 % busy, waits 23 % of the time.
 // ---------------------------------------------------------------------------
 template <class G, int THREADS_>
 struct GatedSource {

@@ -7,11 +7,12 @@
 // a and b stay in registers, so that of them nothing goes to memory but H and two
 // bytes a hidden unit.
 //
-// 8192, 1024 -> 4096 bfloat16 with checkpoints (137 GFLOP, 168 MB): the call 145 us,
-// quantizer 10.4, product about 134 (1.02 PFLOP/s), where a library product of the
-// same size with bfloat16 operands and outputs, without codes, scales and
-// activation, takes 127 - 130 in the same run.  Matrix instructions fill 47 % of the
-// cycles, at a clock that falls below 2 GHz under them; what is left between them is
+// 8192, 1024 -> 4096 bfloat16 with checkpoints (137 GFLOP, 168 MB): the call 145 us by
+// itself, where a library product of the same size with bfloat16 operands and outputs,
+// without codes, scales and activation, takes 127 - 130 in the same run.  In a trace of
+// 90 calls one after another, under which the clock falls, quantizer 10.3 and product
+// 154 on average (0.89 PFLOP/s), 135 at least (1.02).  Matrix instructions fill 47 % of the
+// cycles, at a clock below 2 GHz; what is left between them is
 // the conversions of the codes and each block's activations and stores.
 // Serving: one token of 1024 -> 4096 (8.4 MB of weights) 4.6 us, 1.8 TB/s, 48 of
 // 2048 -> 1001 float16 7.6 us: a launch, and the chain of load, quantize, multiply and
@@ -106,10 +107,10 @@ bool gated_rows_raw(int64_t M, int64_t hidden, int64_t K) {
 // float32 23.9 / 19.4 (in two parts 22.8), 256, 1024 -> 2048 float16 18.1 / 15.2, 2048,
 // 256 -> 512 bfloat16 13.3 / 12.1; in parts / half 250, 2944 -> 1024
 // bfloat16 25.1 / 22.3.  Longer ones stay in parts.
-typedef PipeTile<64, 128, 32, 64, 2, 4> HalfTile;
 // The order of a row's sums is the form's: a wave holds both projections of 32 hidden
 // units, 64 columns, so that these tiles, for every type, divide K between two groups
 // of four waves (the plain layer's of 16-bit outputs, 32 columns a wave, need not).
+typedef PipeTile<64, 128, 32, 64, 2, 4> HalfTile;
 static bool halves(const Fp8Plan& plan, int64_t M, int64_t hidden) {
   return plan.tile == Fp8Plan::SMALL && plan.splits == 1 && tiles_of(M, hidden, SmallTile::BM, SmallTile::BN / 2) <= 128;
 }

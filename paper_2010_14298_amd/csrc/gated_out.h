@@ -131,7 +131,7 @@ __device__ __forceinline__ void gated_store(const P& p, const v16f (&acc)[STRIPS
 
 // A whole block of 128 tokens (WM of each of four waves, which hold 32 hidden units
 // each) by way of LDS, 64 tokens at a time, so that the stores are whole lines:
-// stage[0] 64 rows of 256 bytes of H (16-bit types), stage[1] 64 rows of 128
+// in lds_h 64 rows of 256 bytes of H (16-bit types), in lds_q 64 rows of 128
 // bytes of each checkpoint.  16-byte chunks lie at their index XOR the row, so that
 // neither side meets in a bank.  8192, 1024 -> 4096 bfloat16 with checkpoints 147 us,
 // 151 with the waves' own 32 bytes of a line each.  The codes, which the backward

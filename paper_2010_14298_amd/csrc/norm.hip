@@ -468,7 +468,10 @@ __global__ __launch_bounds__(C::THREADS) void norm_backward_kernel(NormParams p)
 #pragma unroll
     for (int i = 0; i < C::VEC; ++i) sg[k][i] = sb[k][i] = 0.0f;
   // 16 elements of each of a row's 1024 threads do not fit the registers with what kept_rows
-  // holds besides: 2048 x 16000 bfloat16 90 us, row by row 57 (float32 123, 86)
+  // holds besides: 2048 x 16000 bfloat16 90 us, row by row 57 (float32 123, 86).  Of 512
+  // threads (16-bit types, 4097 - 8192 columns) six registers are spilled, and the row ahead
+  // gains all the same, the call in a graph with / row by row: 8192 x 8192 bfloat16 76 / 105, 2048 x 8192 26 / 28,
+  // 8192 x 4104 float16 57 / 73; 300 x 6144, blocks of a row or two, 13.9 / 13.7
   constexpr bool AHEAD = KEPT && (C::TPR < 1024 || C::NV * C::VEC <= 8);
   if constexpr (AHEAD) kept_rows<T, C>(p, sh, sg, sb);
   // every team of the block makes the same number of turns (the barriers
@@ -733,6 +736,8 @@ int64_t norm_backward_partials(int64_t rows, int64_t cols) { return backward_blo
 
 // From a checkpoint: 8 float32 elements a thread, so that the next row's fit the
 // registers (8192 x 4096, 302 MB, with 16 of them and no row ahead 80 us, so 58).
+// The workspace is the plain form's, and so are the blocks: smaller teams make more
+// turns (2048 x 1024: two, on 128 units).
 template <class T, class F>
 static hipError_t with_kept_block(int64_t cols, F f) {
   if constexpr (sizeof(T) == 4) {
